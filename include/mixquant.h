@@ -244,6 +244,76 @@ int bf16_gemm_ws(const void *x_bf16, int64_t ldx, const void *w_bf16, int64_t ld
                  int64_t M, int64_t N, int64_t K, void *y, int64_t ldy, int out,
                  void *workspace, int64_t workspace_bytes, void *stream);
 
+/*
+ * BF16 activations times NVFP4 weights, for the few tokens of a decode step (W4A16; the prefill's weights, read as they are):
+ *    Y[m, n] = alpha_w * sum_k x[m, k] * E4M3(w_scales[n, k/16]) * E2M1(w_codes[n, k])
+ * Every product is exact, sums are accumulated in FP32, alpha_w is applied once to the sum, and the result is written as BF16
+ * (nearest even) or FP32.  Bound by reading W up to about 64 tokens; more are computed 64 at a time, reading W again.
+ * x: [M, K] BF16, row stride ldx.  K % 16 == 0 (K % 64 == 0 for MQ_LAYOUT_KTILE); x, w_codes 16-byte aligned, ldx % 8 == 0,
+ * scale arrays 4-byte aligned when K % 64 == 0; any ldy >= N, y aligned to its element.  M <= 65535, N and K < 2^31.
+ * Results are bit-identical from run to run.
+ */
+int nvfp4_matvec(const void *x_bf16, int64_t ldx, const uint8_t *w_codes, const uint8_t *w_scales, const float *w_alpha_dev,
+                 int64_t M, int64_t N, int64_t K, void *y, int64_t ldy, int out, int layout, void *stream);
+
+/*
+ * The attention half of a decoder block over a paged 8-bit cache (the keys and values that a prefill worker leaves for the
+ * decode worker, Section 3.3, the paragraph on the disaggregated deployment).
+ *
+ * The cache of one layer, all dense:
+ *    k_codes, v_codes   : uint8 [pages, Hkv, P, D]  FP8 E4M3 (OCP); D is 64, 128 or 256, P (tokens a page) 16, 32, 64 or 128
+ *    k_scales, v_scales : uint8 [pages, Hkv]        byte e + 127 for the scale 2^e, -112 <= e <= 119
+ * with value code * 2^e.  Sequence b holds kv_lens[b] tokens, the i-th of them in place i % P of page page_table[b, i / P];
+ * page_table: int32 [B, W], row stride pt_ld.  In a call the tokens cu_q[b] .. cu_q[b + 1] - 1 of T are the last of sequence
+ * b's (kv_lens counts them; a sequence may have none).  cu_q: int32 [B + 1], kv_lens: int32 [B].  All of these are read on the
+ * device.  A page number outside 0 .. pages - 1, or a place beyond the table's W * P, is no place: nothing is stored there and
+ * no query sees it.  Tokens outside cu_q's ranges belong to no sequence, their outputs are unspecified.
+ * W * P <= 2^30, T * Hq < 2^31.  All arrays of codes, BF16 tensors and the table 16-byte aligned, int32 arrays 4-byte aligned,
+ * token strides (elements) multiples of 8; the heads of a token are adjacent.
+ *
+ * mq_rope_table: table[p, i] = gain * cos(p * f_i), table[p, R/2 + i] = gain * sin(p * f_i) for positions p < max_pos, i < R/2,
+ * R = rot_dim a multiple of 16 up to 256, angles in binary64, with f_i = base^(-2i/R) (MQ_ROPE_PLAIN), that divided by factor
+ * (MQ_ROPE_LINEAR), or between the two by how often the pair turns within original_max_pos (MQ_ROPE_YARN):
+ *    f_i = (f_i / factor) * w_i + f_i * (1 - w_i),  w_i = clamp((i - low) / (high - low), 0, 1),
+ *    low = floor(d(beta_fast)), high = ceil(d(beta_slow)), d(t) = R * ln(original_max_pos / (2 pi t)) / (2 ln base), both clamped to 0 .. R - 1
+ *    (high = low + 0.001 where equal);  base > 1, factor >= 1, beta_fast >= beta_slow > 0.
+ * gain multiplies both (what a scaling asks of the scores: 0.1 ln(factor) + 1 for YaRN); 1 otherwise.
+ *
+ * kv8_append: rotates queries and keys and appends keys and values.  The pairs (a, b) of a head's first rot_dim elements are
+ * elements i and R/2 + i, or 2i and 2i + 1 where interleaved is not 0:
+ *    a' = a * c_i - b * s_i,  b' = b * c_i + a * s_i     (each step binary32, unfused, the result rounded once to BF16)
+ * with the table's row at positions[t], or, positions being NULL, at the token's place in its sequence; a position outside
+ * 0 .. max_pos - 1 gives NaN.  q_out receives the queries, dense [T, Hq, D]; rot_dim == 0 (table may be NULL) copies them.
+ * Keys (rotated, BF16) and values go to the cache: a page's e is the smallest of -112 .. 119 with which the largest finite
+ * magnitude among its new tokens is at most 448 * 2^e, and at least what it was where the page holds earlier tokens of the
+ * sequence; those tokens' codes are then brought to the new scale, each rounded once.  code = nearest E4M3 of x / 2^e, ties to
+ * even, clipped to +-448; NaN stays NaN.  Pages that two sequences of the call share must not receive tokens.
+ *
+ * kv8_attention: y[t, h, :] = sum_j p_j v_j, p = softmax_j(sm_scale * (q[t, h, :] . k_j)) over the places j that token t sees:
+ * 0 <= j <= pos, its own place, and j > pos - window where window > 0.  Query head h reads key head h / (Hq / Hkv).  A token that
+ * sees nothing gets zeros.  Products of BF16 numbers, sums and the softmax's maxima and sums in FP32, probabilities rounded to
+ * BF16 for the product with the values, y BF16 (nearest even), [T, Hq, D] with token stride ldy.  Hq % Hkv == 0, sm_scale
+ * finite and > 0.  Places that no query of the call sees may hold anything.
+ * workspace: as in nvfp4_gemm_ws; with mq_kv8_attention_workspace_bytes(...) bytes (at most 64 MiB; less counts as none) long
+ * histories are cut across workgroups, and a second kernel adds the parts in ascending order: bit-identical from run to run.
+ */
+typedef enum {
+    MQ_ROPE_PLAIN = 0,
+    MQ_ROPE_LINEAR = 1,
+    MQ_ROPE_YARN = 2
+} mq_rope;
+int mq_rope_table(float *table, int64_t max_pos, int rot_dim, double base, int scaling, double factor, int64_t original_max_pos,
+                  double beta_fast, double beta_slow, double gain, void *stream);
+int kv8_append(const void *q_bf16, int64_t ldq, const void *k_bf16, int64_t ldk, const void *v_bf16, int64_t ldv, void *q_out,
+               uint8_t *k_codes, uint8_t *k_scales, uint8_t *v_codes, uint8_t *v_scales, int64_t pages, int P, int Hq, int Hkv, int D,
+               const int32_t *page_table, int64_t pt_ld, int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T,
+               const float *table, int64_t max_pos, int rot_dim, const int32_t *positions, int interleaved, void *stream);
+int64_t mq_kv8_attention_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int D);
+int kv8_attention(const void *q_bf16, int64_t ldq, const uint8_t *k_codes, const uint8_t *k_scales, const uint8_t *v_codes,
+                  const uint8_t *v_scales, int64_t pages, int P, int Hq, int Hkv, int D, const int32_t *page_table, int64_t pt_ld,
+                  int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T, float sm_scale, int64_t window,
+                  void *y, int64_t ldy, void *workspace, int64_t workspace_bytes, void *stream);
+
 /* Human-readable name of an mq_status value (static storage). */
 const char *mq_status_string(int status);
 

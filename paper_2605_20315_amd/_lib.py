@@ -13,6 +13,7 @@ LIB_PATH = os.environ.get("MIXQUANT_LIB") or os.path.join(_HERE, "libmixquant.so
 MQ_OK = 0
 MQ_OUT_BF16, MQ_OUT_FP32 = 0, 1
 MQ_LAYOUT_LINEAR, MQ_LAYOUT_KTILE = 0, 1
+MQ_ROPE_PLAIN, MQ_ROPE_LINEAR, MQ_ROPE_YARN = 0, 1, 2
 
 BINDING_PATH = os.path.join(_HERE, "_binding.so")
 
@@ -69,6 +70,19 @@ def load() -> ctypes.CDLL:
     lib.bf16_gemm_ws.argtypes = [vp, i64, vp, i64, i64, i64, i64, vp, i64, ci, vp, i64, vp]
     lib.mq_bf16_gemm_workspace_bytes.restype = i64
     lib.mq_bf16_gemm_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.nvfp4_matvec.restype = ci
+    lib.nvfp4_matvec.argtypes = [vp, i64, vp, vp, vp, i64, i64, i64, vp, i64, ci, ci, vp]
+    f64 = ctypes.c_double
+    lib.mq_rope_table.restype = ci
+    lib.mq_rope_table.argtypes = [vp, i64, ci, f64, ci, f64, i64, f64, f64, f64, vp]
+    lib.kv8_append.restype = ci
+    lib.kv8_append.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, ci, ci, ci, ci, vp, i64, i64, vp, vp, i64, i64,
+                               vp, i64, ci, vp, ci, vp]
+    lib.mq_kv8_attention_workspace_bytes.restype = i64
+    lib.mq_kv8_attention_workspace_bytes.argtypes = [i64, i64, ci, ci, ci]
+    lib.kv8_attention.restype = ci
+    lib.kv8_attention.argtypes = [vp, i64, vp, vp, vp, vp, i64, ci, ci, ci, ci, vp, i64, i64, vp, vp, i64, i64, ctypes.c_float, i64,
+                                  vp, i64, vp, i64, vp]
     lib.mq_mfma_probe.restype = ci
     lib.mq_mfma_probe.argtypes = [vp, ci, vp, ctypes.POINTER(ctypes.c_double)]
     lib.mq_gemm_launches.restype = ci

@@ -1,7 +1,10 @@
 // extern "C" entry points of libmixquant: argument validation on the host, then one or a
 // few kernel launches on the caller's stream.  Nothing here allocates or synchronises.
+#include <algorithm>
 #include <atomic>
+#include <cmath>
 
+#include "kv8.h"
 #include "mq_common.h"
 
 namespace mq {
@@ -42,6 +45,7 @@ static int ensure_device(int *slot_out)
     if (slot_out) *slot_out = dev;
     if (g_device_ready[dev].load(std::memory_order_acquire)) return MQ_OK;
     if (int rc = configure_gemm_kernels()) return rc;
+    if (int rc = configure_kv8_kernels()) return rc;
     void *ptr = nullptr;
     e = hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch));
     if (e != hipSuccess || ptr == nullptr) return note_launch(e != hipSuccess ? e : hipErrorInvalidSymbol);
@@ -309,6 +313,130 @@ int bf16_gemm_ws(const void *x_bf16, int64_t ldx, const void *w_bf16, int64_t ld
     g.ldy = ldy;
     g.out = out;
     return launch_gemm_bf16(g, static_cast<hipStream_t>(stream));
+}
+
+int nvfp4_matvec(const void *x_bf16, int64_t ldx, const uint8_t *w_codes, const uint8_t *w_scales, const float *w_alpha_dev,
+                 int64_t M, int64_t N, int64_t K, void *y, int64_t ldy, int out, int layout, void *stream)
+{
+    if (M < 0 || N < 0 || K <= 0 || K % kBlock != 0 || ldx < K) return MQ_ERR_SHAPE;
+    if (out != MQ_OUT_BF16 && out != MQ_OUT_FP32) return MQ_ERR_ARG;
+    if (layout != MQ_LAYOUT_LINEAR && layout != MQ_LAYOUT_KTILE) return MQ_ERR_ARG;
+    if (layout == MQ_LAYOUT_KTILE && K % 64 != 0) return MQ_ERR_SHAPE;
+    if (M == 0 || N == 0) return MQ_OK;
+    if (ldy < N || M > 65535 || K > 0x7fffffff || N > 0x7fffffff) return MQ_ERR_SHAPE;
+    if (!x_bf16 || !w_codes || !w_scales || !w_alpha_dev || !y) return MQ_ERR_NULL;
+    if (!aligned(x_bf16, 16) || ldx % 8 != 0 || !aligned(w_codes, 16) || !aligned(w_alpha_dev, 4)) return MQ_ERR_ALIGN;
+    if (!aligned(y, out == MQ_OUT_BF16 ? 2 : 4) || (K % 64 == 0 && !aligned(w_scales, 4))) return MQ_ERR_ALIGN;
+    return launch_nvfp4_matvec(static_cast<const uint16_t *>(x_bf16), ldx, w_codes, w_scales, w_alpha_dev, M, N, K, y, ldy, out, layout,
+                               static_cast<hipStream_t>(stream));
+}
+
+int mq_rope_table(float *table, int64_t max_pos, int rot_dim, double base, int scaling, double factor, int64_t original_max_pos,
+                  double beta_fast, double beta_slow, double gain, void *stream)
+{
+    if (max_pos < 0 || max_pos > 0x7fffffff || rot_dim <= 0 || rot_dim > 256 || rot_dim % 16 != 0) return MQ_ERR_SHAPE;
+    if (scaling != MQ_ROPE_PLAIN && scaling != MQ_ROPE_LINEAR && scaling != MQ_ROPE_YARN) return MQ_ERR_ARG;
+    if (!(base > 1.0) || !std::isfinite(base) || !std::isfinite(gain)) return MQ_ERR_ARG;
+    if (scaling != MQ_ROPE_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return MQ_ERR_ARG;
+    if (scaling == MQ_ROPE_YARN && (!(beta_slow > 0.0) || !(beta_fast >= beta_slow) || !std::isfinite(beta_fast))) return MQ_ERR_ARG;
+    if (scaling == MQ_ROPE_YARN && original_max_pos <= 0) return MQ_ERR_SHAPE;
+    if (max_pos == 0) return MQ_OK;
+    if (!table) return MQ_ERR_NULL;
+    if (!aligned(table, 16)) return MQ_ERR_ALIGN;
+    RopeTable r{};
+    r.table = table;
+    r.max_pos = max_pos;
+    r.rot = rot_dim;
+    r.gain = (float)gain;
+    double low = 0.0, high = 1.0;
+    if (scaling == MQ_ROPE_YARN) {
+        // the pair that turns t times within the original context
+        auto pair = [&](double t) { return rot_dim * std::log((double)original_max_pos / (t * 2.0 * M_PI)) / (2.0 * std::log(base)); };
+        low = std::min(std::max(std::floor(pair(beta_fast)), 0.0), rot_dim - 1.0);
+        high = std::min(std::max(std::ceil(pair(beta_slow)), 0.0), rot_dim - 1.0);
+        if (low == high) high += 0.001;
+    }
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / rot_dim);
+        const double w = scaling == MQ_ROPE_PLAIN ? 0.0 : scaling == MQ_ROPE_LINEAR ? 1.0 : std::min(std::max((i - low) / (high - low), 0.0), 1.0);
+        r.freq[i] = w == 0.0 ? f : f / factor * w + f * (1.0 - w);
+    }
+    return launch_rope_table(r, static_cast<hipStream_t>(stream));
+}
+
+// What the two calls on the cache share: sizes, then pointers (of a call that has anything to do)
+static int check_cache(int64_t pages, int P, int Hq, int Hkv, int D, int64_t pt_ld, int64_t W, int64_t B, int64_t T)
+{
+    if (pages < 0 || W < 0 || B < 0 || T < 0 || pages > 0x7fffffff || B > 0x7fffffff - 1) return MQ_ERR_SHAPE;
+    if (P != 16 && P != 32 && P != 64 && P != 128) return MQ_ERR_SHAPE;
+    if (D != 64 && D != 128 && D != 256) return MQ_ERR_SHAPE;
+    if (Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 || pt_ld < W) return MQ_ERR_SHAPE;
+    if (W > ((int64_t)1 << 30) / P || T > 0x7fffffff / Hq) return MQ_ERR_SHAPE;
+    return MQ_OK;
+}
+
+static int check_cache_pointers(const void *kc, const void *ks, const void *vc, const void *vs, const void *pt, const void *cu_q,
+                                const void *kv_lens)
+{
+    if (!kc || !ks || !vc || !vs || !pt || !cu_q || !kv_lens) return MQ_ERR_NULL;
+    if (!aligned(kc, 16) || !aligned(vc, 16) || !aligned(pt, 4) || !aligned(cu_q, 4) || !aligned(kv_lens, 4)) return MQ_ERR_ALIGN;
+    return MQ_OK;
+}
+
+static Kv8Seqs sequences(const int32_t *page_table, int64_t pt_ld, int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B,
+                         int64_t T, int64_t pages, int P)
+{
+    return Kv8Seqs{page_table, cu_q, kv_lens, pt_ld, pages, (int)W, (int)B, (int)T, P == 16 ? 4 : P == 32 ? 5 : P == 64 ? 6 : 7};
+}
+
+int kv8_append(const void *q_bf16, int64_t ldq, const void *k_bf16, int64_t ldk, const void *v_bf16, int64_t ldv, void *q_out,
+               uint8_t *k_codes, uint8_t *k_scales, uint8_t *v_codes, uint8_t *v_scales, int64_t pages, int P, int Hq, int Hkv, int D,
+               const int32_t *page_table, int64_t pt_ld, int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T,
+               const float *table, int64_t max_pos, int rot_dim, const int32_t *positions, int interleaved, void *stream)
+{
+    if (int rc = check_cache(pages, P, Hq, Hkv, D, pt_ld, W, B, T)) return rc;
+    if (rot_dim < 0 || rot_dim > D || rot_dim % 16 != 0 || max_pos < 0) return MQ_ERR_SHAPE;
+    if (ldq < (int64_t)Hq * D || ldk < (int64_t)Hkv * D || ldv < (int64_t)Hkv * D) return MQ_ERR_SHAPE;
+    if (T == 0 || B == 0) return MQ_OK;
+    if (int rc = check_cache_pointers(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens)) return rc;
+    if (!q_bf16 || !k_bf16 || !v_bf16 || !q_out || (rot_dim && !table)) return MQ_ERR_NULL;
+    if (rot_dim && max_pos == 0) return MQ_ERR_SHAPE;
+    if (!aligned(q_bf16, 16) || !aligned(k_bf16, 16) || !aligned(v_bf16, 16) || !aligned(q_out, 16) || !aligned(table, 16) ||
+        !aligned(positions, 4) || ldq % 8 != 0 || ldk % 8 != 0 || ldv % 8 != 0)
+        return MQ_ERR_ALIGN;
+    const Kv8Append a{static_cast<const uint16_t *>(q_bf16), static_cast<const uint16_t *>(k_bf16), static_cast<const uint16_t *>(v_bf16),
+                      ldq, ldk, ldv, static_cast<uint16_t *>(q_out), k_codes, k_scales, v_codes, v_scales, table, positions, max_pos,
+                      rot_dim, interleaved != 0, Hq, Hkv, D, sequences(page_table, pt_ld, W, cu_q, kv_lens, B, T, pages, P)};
+    return launch_kv8_append(a, static_cast<hipStream_t>(stream));
+}
+
+int64_t mq_kv8_attention_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int D)
+{
+    if (T <= 0 || B <= 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 || (D != 64 && D != 128 && D != 256)) return 0;
+    return kv8_attention_workspace(T, B, Hq, Hkv, D);
+}
+
+int kv8_attention(const void *q_bf16, int64_t ldq, const uint8_t *k_codes, const uint8_t *k_scales, const uint8_t *v_codes,
+                  const uint8_t *v_scales, int64_t pages, int P, int Hq, int Hkv, int D, const int32_t *page_table, int64_t pt_ld,
+                  int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T, float sm_scale, int64_t window,
+                  void *y, int64_t ldy, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (int rc = check_cache(pages, P, Hq, Hkv, D, pt_ld, W, B, T)) return rc;
+    if (ldq < (int64_t)Hq * D || ldy < (int64_t)Hq * D || workspace_bytes < 0) return MQ_ERR_SHAPE;
+    if (!(sm_scale > 0.0f) || !std::isfinite(sm_scale)) return MQ_ERR_ARG;
+    if (T == 0 || B == 0) return MQ_OK;
+    if (int rc = check_cache_pointers(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens)) return rc;
+    if (!q_bf16 || !y) return MQ_ERR_NULL;
+    if (!aligned(q_bf16, 16) || !aligned(y, 16) || ldq % 8 != 0 || ldy % 8 != 0 || (workspace && !aligned(workspace, 16)))
+        return MQ_ERR_ALIGN;
+    Kv8Attend a{static_cast<const uint16_t *>(q_bf16), ldq, k_codes, k_scales, v_codes, v_scales, static_cast<uint16_t *>(y), ldy, Hq, Hkv, D,
+                // a window that no place lies outside of is none
+                window <= 0 || window >= W * P ? 0 : (int)window, sm_scale * 1.44269504f, nullptr, 0,
+                sequences(page_table, pt_ld, W, cu_q, kv_lens, B, T, pages, P)};
+    a.ws = workspace_bytes > 0 ? static_cast<float *>(workspace) : nullptr;
+    a.ws_bytes = a.ws ? workspace_bytes : 0;
+    if (int rc = ensure_device(nullptr)) return rc;
+    return launch_kv8_attention(a, static_cast<hipStream_t>(stream));
 }
 
 int mq_mfma_probe(float *scratch_dev, int iters, void *stream, double *flop_out)

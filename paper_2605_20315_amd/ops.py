@@ -11,11 +11,13 @@ device memory and streams; all arithmetic runs in the HIP kernels.
 """
 from __future__ import annotations
 
+import math
+
 import torch
 
 from . import _lib
-from ._lib import (MQ_LAYOUT_KTILE, MQ_LAYOUT_LINEAR, MQ_OUT_BF16, MQ_OUT_FP32,  # noqa: F401
-                   MixQuantError)
+from ._lib import (MQ_LAYOUT_KTILE, MQ_LAYOUT_LINEAR, MQ_OUT_BF16, MQ_OUT_FP32, MQ_ROPE_LINEAR,  # noqa: F401
+                   MQ_ROPE_PLAIN, MQ_ROPE_YARN, MixQuantError)
 
 BLOCK = 16
 
@@ -314,6 +316,133 @@ def nvfp4_linear(x_bf16: torch.Tensor, alpha_x: torch.Tensor, w_codes, w_scales,
         return done
     xc, xs = nvfp4_quantize(x_bf16, alpha_x, codes, scales, layout)
     return nvfp4_gemm_ws(xc, xs, alpha_x, w_codes, w_scales, alpha_w, workspace, out, y, layout)
+
+
+def nvfp4_matvec(x_bf16: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, w_alpha: torch.Tensor,
+                 out: int = MQ_OUT_BF16, y: torch.Tensor | None = None, layout: int = MQ_LAYOUT_LINEAR) -> torch.Tensor:
+    """Y = X . dequant(W)^T for the few tokens of a decode step: BF16 activations as they are, NVFP4 weights, FP32 accumulation."""
+    _need_gpu(x_bf16, w_codes, w_scales, w_alpha)
+    assert x_bf16.dtype == torch.bfloat16 and w_alpha.dtype == torch.float32
+    M, K, ldx = _rows_k_ld(x_bf16)
+    N = w_codes.shape[0]
+    for t in (w_codes, w_scales):
+        assert t.dtype == torch.uint8 and t.is_contiguous()
+    if K % BLOCK:
+        _lib.check(2, "nvfp4_matvec")
+    assert w_codes.shape == (N, K // 2) and w_scales.shape == (N, K // BLOCK)
+    if y is None:
+        y = torch.empty((M, N), dtype=torch.bfloat16 if out == MQ_OUT_BF16 else torch.float32, device=x_bf16.device)
+    assert y.is_cuda and y.shape == (M, N) and (N <= 1 or y.stride(1) == 1)
+    assert y.dtype == (torch.bfloat16 if out == MQ_OUT_BF16 else torch.float32)
+    ldy = y.stride(0) if M > 1 else max(y.stride(0), N)
+    rc = _lib.load().nvfp4_matvec(x_bf16.data_ptr(), ldx, w_codes.data_ptr(), w_scales.data_ptr(), w_alpha.data_ptr(), M, N, K,
+                                  y.data_ptr(), ldy, out, layout, _stream())
+    _lib.check(rc, "nvfp4_matvec")
+    return y
+
+
+def mq_rope_table(max_pos: int, rot_dim: int, base: float = 10000.0, scaling: int = MQ_ROPE_PLAIN, factor: float = 1.0,
+                  original_max_pos: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0, gain: float | None = None,
+                  table: torch.Tensor | None = None, device="cuda") -> torch.Tensor:
+    """Cosines and sines of the position rotation for kv8_append, float32 [max_pos, rot_dim]; gain: 0.1 ln(factor) + 1 for
+    MQ_ROPE_YARN where it is not given, else 1."""
+    if gain is None:
+        gain = 0.1 * math.log(factor) + 1.0 if scaling == MQ_ROPE_YARN and factor > 0 else 1.0
+    if table is None:
+        table = torch.empty((max(max_pos, 0), max(rot_dim, 0)), dtype=torch.float32, device=device)
+    _need_gpu(table)
+    assert table.dtype == torch.float32 and table.shape == (max(max_pos, 0), max(rot_dim, 0)) and table.is_contiguous()
+    rc = _lib.load().mq_rope_table(table.data_ptr(), max_pos, rot_dim, base, scaling, factor, original_max_pos, beta_fast, beta_slow,
+                                   gain, _stream())
+    _lib.check(rc, "mq_rope_table")
+    return table
+
+
+def _heads_ld(x: torch.Tensor):
+    """(tokens, heads, D, token stride) of a [T, H, D] tensor whose heads are adjacent."""
+    if x.dim() != 3 or x.dtype != torch.bfloat16 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]):
+        raise MixQuantError("expected a BF16 [tokens, heads, D] tensor whose heads are adjacent")
+    T, H, D = x.shape
+    return T, H, D, x.stride(0) if T > 1 else max(x.stride(0), H * D)
+
+
+def _cache(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, T, D):
+    """Checks of the cache and of the sequences, and their sizes: (pages, P, Hkv, row stride of the table, W, B)."""
+    _need_gpu(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens)
+    if k_codes.dim() != 4 or k_codes.shape[3] != D:
+        raise MixQuantError("expected a cache of codes [pages, heads, tokens, D]")
+    pages, Hkv, P, _ = k_codes.shape
+    assert v_codes.shape == k_codes.shape and k_scales.shape == (pages, Hkv) and v_scales.shape == (pages, Hkv)
+    for t in (k_codes, k_scales, v_codes, v_scales):
+        assert t.dtype == torch.uint8 and t.is_contiguous()
+    B = kv_lens.shape[0]
+    for t in (page_table, cu_q, kv_lens):
+        assert t.dtype == torch.int32
+    assert kv_lens.shape == (B,) and cu_q.shape == (B + 1,) and kv_lens.is_contiguous() and cu_q.is_contiguous()
+    assert page_table.dim() == 2 and page_table.shape[0] == B and (page_table.shape[1] <= 1 or page_table.stride(1) == 1)
+    W = page_table.shape[1]
+    return pages, P, Hkv, page_table.stride(0) if B > 1 else max(page_table.stride(0), W), W, B
+
+
+def kv8_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tensor,
+               v_codes: torch.Tensor, v_scales: torch.Tensor, page_table: torch.Tensor, cu_q: torch.Tensor, kv_lens: torch.Tensor,
+               table: torch.Tensor | None = None, positions: torch.Tensor | None = None, interleaved: bool = False,
+               q_out: torch.Tensor | None = None) -> torch.Tensor:
+    """Rotates q [T, Hq, D] and k [T, Hkv, D] and appends k and v to the paged FP8 cache; returns the rotated queries.
+    table: what mq_rope_table gives, [max_pos, rot_dim], or None for no rotation.  kv_lens count the new tokens."""
+    _need_gpu(q, k, v)
+    T, Hq, D, ldq = _heads_ld(q)
+    Tk, Hkv, Dk, ldk = _heads_ld(k)
+    Tv, Hv, Dv, ldv = _heads_ld(v)
+    pages, P, heads, pt_ld, W, B = _cache(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, T, D)
+    assert (Tk, Hkv, Dk) == (Tv, Hv, Dv) == (T, heads, D)
+    max_pos, rot = 0, 0
+    if table is not None:
+        _need_gpu(table)
+        assert table.dtype == torch.float32 and table.dim() == 2 and table.is_contiguous()
+        max_pos, rot = table.shape
+    if positions is not None:
+        _need_gpu(positions)
+        assert positions.dtype == torch.int32 and positions.shape == (T,) and positions.is_contiguous()
+    if q_out is None:
+        q_out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=q.device)
+    assert q_out.is_cuda and q_out.dtype == torch.bfloat16 and q_out.shape == (T, Hq, D) and q_out.is_contiguous()
+    rc = _lib.load().kv8_append(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, q_out.data_ptr(), k_codes.data_ptr(),
+                                k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), pages, P, Hq, Hkv, D,
+                                page_table.data_ptr(), pt_ld, W, cu_q.data_ptr(), kv_lens.data_ptr(), B, T,
+                                table.data_ptr() if rot else None, max_pos, rot, positions.data_ptr() if positions is not None else None,
+                                int(bool(interleaved)), _stream())
+    _lib.check(rc, "kv8_append")
+    return q_out
+
+
+def mq_kv8_attention_workspace_bytes(T: int, B: int, Hq: int, Hkv: int, D: int) -> int:
+    """Workspace size that lets kv8_attention cut long histories across workgroups."""
+    return int(_lib.load().mq_kv8_attention_workspace_bytes(T, B, Hq, Hkv, D))
+
+
+def kv8_attention(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor, v_scales: torch.Tensor,
+                  page_table: torch.Tensor, cu_q: torch.Tensor, kv_lens: torch.Tensor, sm_scale: float, window: int = 0,
+                  y: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Causal attention of q [T, Hq, D], the last tokens of their sequences, over the paged FP8 cache; BF16 [T, Hq, D].
+    window > 0: a token sees itself and the window - 1 places before it.  workspace: any contiguous GPU tensor, or None."""
+    _need_gpu(q)
+    T, Hq, D, ldq = _heads_ld(q)
+    pages, P, Hkv, pt_ld, W, B = _cache(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, T, D)
+    if y is None:
+        y = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=q.device)
+    _need_gpu(y)
+    assert y.shape == (T, Hq, D)
+    ldy = _heads_ld(y)[3]
+    ws_ptr, ws_bytes = 0, 0
+    if workspace is not None:
+        assert workspace.is_cuda and workspace.is_contiguous()
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    rc = _lib.load().kv8_attention(q.data_ptr(), ldq, k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(),
+                                   v_scales.data_ptr(), pages, P, Hq, Hkv, D, page_table.data_ptr(), pt_ld, W, cu_q.data_ptr(),
+                                   kv_lens.data_ptr(), B, T, sm_scale, window, y.data_ptr(), ldy, ws_ptr, ws_bytes, _stream())
+    _lib.check(rc, "kv8_attention")
+    return y
 
 
 def mfma_probe(iters: int = 4000) -> float:
