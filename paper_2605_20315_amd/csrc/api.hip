@@ -45,7 +45,6 @@ static int ensure_device(int *slot_out)
     if (slot_out) *slot_out = dev;
     if (g_device_ready[dev].load(std::memory_order_acquire)) return MQ_OK;
     if (int rc = configure_gemm_kernels()) return rc;
-    if (int rc = configure_kv8_kernels()) return rc;
     void *ptr = nullptr;
     e = hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch));
     if (e != hipSuccess || ptr == nullptr) return note_launch(e != hipSuccess ? e : hipErrorInvalidSymbol);
