@@ -189,8 +189,21 @@ static __device__ __forceinline__ float weight_of(float m, float l, float top)
 // 0x01 in the bytes that are NaN codes
 static __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u; }
 
-// 1.0 or 0.0 in BF16 for the lowest two bits
-static __device__ __forceinline__ uint32_t ones(uint32_t bits) { return (bits & 1 ? 0x3f80u : 0u) | (bits & 2 ? 0x3f800000u : 0u); }
+// The order of the instructions since the last such mark: N matrix instructions, an LDS read in front of every RH-th of them,
+// and behind each V vector instructions and T transcendental ones.
+template <int N, int V, int T, int RH>
+static __device__ __forceinline__ void interleave()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (i % RH == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        if (V > 0) __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
+        if (T > 0) __builtin_amdgcn_sched_group_barrier(0x400, T, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 // Four bytes of each of eight tokens' rows (the same four head elements), turned round: out[d] = element d of the eight tokens
 static __device__ __forceinline__ void turn8(const uint32_t (&w)[8], const float (&scale)[2], bf16x8 (&out)[4])
@@ -247,6 +260,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) acc[d] = f32x4{0, 0, 0, 0};
     float mb = kNone, l = 0.0f;  // the running maximum times the scale
+    bool marked = false;         // whether the wave's part of `sums` holds NaN for what rows have seen
 
     const int P = 1 << a.s.page_shift;
     const int64_t unit = (int64_t)P * D;
@@ -309,9 +323,9 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
                                                                __builtin_bit_cast(bf16x8, q[w]), s[h], 0, 0, 0);
         }
         const bool edge = t < all_lo || t + 32 > all_hi || id0 < 0 || id1 < 0;
-        uint32_t seen = 0;
-        bool odd = false;
         if (edge) {
+            uint32_t seen = 0;
+            bool odd = false;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -329,7 +343,28 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
                         odd |= nan_bytes(x.v[4 * h + j][w]) != 0;
                     }
                 }
-            odd = __any(odd);
+            if (__any(odd)) {
+                // NaN values that some rows see and others do not: out of the product, and kept for the rows that see them
+                if (!marked)
+                    for (int i = lane; i < 16 * (D + 4); i += 64) (&sums[wave][0][0])[i] = 0.0f;
+                marked = true;
+#pragma unroll 1
+                for (int r = 0; r < 16; ++r) {
+                    const uint32_t sees = (uint32_t)__shfl((int)seen, r + 16 * g);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll
+                        for (int w = 0; w < VW; ++w)
+                            if (const uint32_t n = nan_bytes(x.v[j][w]); n && (sees >> j & 1))
+#pragma unroll 1
+                                for (int b = 0; b < 4; ++b)
+                                    if (n >> (8 * b) & 1) sums[wave][r][col * (D / 16) + 4 * w + b] = __builtin_nanf("");
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) x.v[j][w] &= ~(nan_bytes(x.v[j][w]) * 0xffu);
+            }
         }
         float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         top = fmaxf(top, __shfl_xor(top, 16));
@@ -352,26 +387,6 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = x.v[j][w];
             bf16x8 turned[4];
-            if (odd) {
-                // NaN values that some rows see and others do not: out of the product, and into the rows that see them by
-                // the product of where they are with who sees them
-                const bf16x8 who = four(ones(seen), ones(seen >> 2), ones(seen >> 4), ones(seen >> 6));
-                const float one[2] = {1.0f, 1.0f};
-                uint32_t where[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t n = nan_bytes(v[j]);
-                    where[j] = n * 0x38u;  // 1.0
-                    v[j] &= ~(n * 0xffu);
-                }
-                turn8(where, one, turned);
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(turned[d], who, f32x4{0, 0, 0, 0}, 0, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[4 * w + d][i] = hit[i] > 0.0f ? __builtin_nanf("") : acc[4 * w + d][i];
-                }
-            }
             turn8(v, v_scale, turned);
 #pragma unroll
             for (int d = 0; d < 4; ++d) acc[4 * w + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(turned[d], pb, acc[4 * w + d], 0, 0, 0);
@@ -404,7 +419,10 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
 #pragma unroll
     for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sums[wave][col][(4 * g + i) * (D / 16) + d] = acc[d][i] * by;
+        for (int i = 0; i < 4; ++i) {
+            float &to = sums[wave][col][(4 * g + i) * (D / 16) + d];
+            to = marked ? fmaf(acc[d][i], by, to) : acc[d][i] * by;
+        }
     __syncthreads();
     // 16 threads a row, D / 16 elements each
     const int orow = tid >> 4, e0 = (tid & 15) * (D / 16), out = it.tile * kFewRows + orow;
@@ -433,288 +451,349 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
 
 // ------------------------------------------------------------------------------------------------ many rows
 
-// One item by NW waves of 32 rows each, a tile of 64 tokens at a time.  The threads expand a tile's codes to BF16 in LDS once
+// One item by four waves of 32 * RH rows, a tile of 64 tokens at a time.  The threads expand a tile's codes to BF16 in LDS once
 // for all waves, in the order in which the matrix instructions take them: a block of 1 KB is one operand of one 32x32x16
-// product, lane l's 16 bytes at 16 l, so that reading is free of bank conflicts and needs no address arithmetic.  Two buffers:
-// tile i + 1 is loaded while tile i is multiplied, expanded behind that, and one barrier a tile is enough.
+// product, lane l's 16 bytes at 16 l, so that reading is free of bank conflicts and needs no address arithmetic.
 //    keys    block (half of the tile, 16 elements): lane (token % 32, k = 8 elements)
 //    values  block (16 tokens s, 32 elements): lane (element, tokens 16s + 4h .. + 3 and 16s + 8 + 4h .. + 3), h = lane / 32:
 //            the tokens whose scores that lane holds after S^T = K Q^T
-template <int D, int NW>
+// 64 rows a wave, because every wave reads the whole tile: at 32 rows the reads alone took as long as the products.  One wave
+// a SIMD has to overlap its own matrix and vector work: the keys of the next 32 tokens are multiplied beside the exponentials of
+// these, and their values beside the next ones' maxima.  So tile i of keys is 32 tokens ahead of tile i of values: tokens
+// t + 32 .. t + 95 and t .. t + 63.  Both of tile i + 1 are loaded when tile i begins and expanded at its end; with two buffers
+// one barrier a tile is enough.
+template <int D, int RH, int NW>
 __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
 {
     constexpr int NT = 64 * NW, kTasks = 4 * D, TN = (kTasks + NT - 1) / NT;  // a task: 32 bytes of codes
+    constexpr int kRows = 32 * RH * NW;
     constexpr int kBlock16 = 1024 + 16;  // the padding spreads a key token's four writes over the banks
-    constexpr int kKeys = 2 * (D / 16), kBlocks = 2 * kKeys;
+    constexpr int kHalf = 2 * (D / 16);  // blocks of a tile's keys, and of its values
     __shared__ PlanLds plan;
-    __shared__ int flags[3];
-    __shared__ __attribute__((aligned(16))) unsigned char tile[2][kBlocks * kBlock16];
+    __shared__ int flags[4];
+    __shared__ uint32_t nans[kTile][D / 32], marks[RH * (D / 32)][NT];  // what set_nan_aside finds, and the rows' elements that see it
+    __shared__ __attribute__((aligned(16))) unsigned char keys[2][kHalf * kBlock16], values[2][kHalf * kBlock16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
     const Item it = item_of<NT>(a, c, blockIdx.x, -1, plan, tid);
     if (!it.found) return;
-    const int G = a.Hq / a.Hkv, rows = it.sp.n * G, tile0 = it.tile * 32 * NW, wave0 = tile0 + 32 * wave;
-    const int r = wave0 + col, row = min(r, rows - 1), token = row / G, head = it.head * G + row - token * G;
-    const int pos = it.sp.start + token;
-    const int first = a.window > 0 ? pos - a.window + 1 : 0;
-    // places that any row of the workgroup sees, that any and that every row of the wave sees
-    const int group_hi = min(it.hi, it.sp.start + (min(tile0 + 32 * NW, rows) - 1) / G + 1);
-    const int group_lo = max(it.lo, a.window > 0 ? it.sp.start + tile0 / G - a.window + 1 : 0);
-    const bool live = wave0 < rows;
-    const int pos_lo = it.sp.start + min(wave0, rows - 1) / G, pos_hi = it.sp.start + (min(wave0 + 32, rows) - 1) / G;
-    const int hi = live ? min(it.hi, pos_hi + 1) : 0, lo = max(it.lo, a.window > 0 ? pos_lo - a.window + 1 : 0);
-    const int all_lo = a.window > 0 ? pos_hi - a.window + 1 : 0, all_hi = min(it.hi, pos_lo + 1);
-
-    bf16x8 q[D / 16];
-    {
-        const uint16_t *const p = a.q + (int64_t)(it.sp.q0 + token) * a.ldq + (int64_t)head * D + 8 * h;
+    const int G = a.Hq / a.Hkv, rows = it.sp.n * G, tile0 = it.tile * kRows, wave0 = tile0 + 32 * RH * wave;
+    int pos[RH], first[RH], token[RH], head[RH];
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) q[s] = *reinterpret_cast<const bf16x8 *>(p + 16 * s);
+    for (int f = 0; f < RH; ++f) {
+        const int row = min(wave0 + 32 * f + col, rows - 1);  // rows beyond the last are computed again and not stored
+        token[f] = row / G;
+        head[f] = it.head * G + row - token[f] * G;
+        pos[f] = it.sp.start + token[f];
+        first[f] = a.window > 0 ? pos[f] - a.window + 1 : 0;
     }
-    f32x16 acc[D / 32];
+    // places that any row of the workgroup sees, that any and that every row of the wave sees
+    const int group_hi = min(it.hi, it.sp.start + (min(tile0 + kRows, rows) - 1) / G + 1);
+    const int group_lo = max(it.lo, a.window > 0 ? it.sp.start + tile0 / G - a.window + 1 : 0);
+    const int pos_lo = it.sp.start + min(wave0, rows - 1) / G, pos_hi = it.sp.start + (min(wave0 + 32 * RH, rows) - 1) / G;
+    const int all_lo = max(group_lo, a.window > 0 ? pos_hi - a.window + 1 : 0), all_hi = min(group_hi, pos_lo + 1);
+    // places that every row of the workgroup sees
+    const int rows_lo = max(group_lo, a.window > 0 ? it.sp.start + (min(tile0 + kRows, rows) - 1) / G - a.window + 1 : 0);
+    const int rows_hi = min(group_hi, it.sp.start + tile0 / G + 1);
+
+    bf16x8 q[RH][D / 16];
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
+    for (int f = 0; f < RH; ++f) {
+        const uint16_t *const p = a.q + (int64_t)(it.sp.q0 + token[f]) * a.ldq + (int64_t)head[f] * D + 8 * h;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
-    float mb = kNone, l = 0.0f;  // the running maximum times the scale
+        for (int s = 0; s < D / 16; ++s) q[f][s] = *reinterpret_cast<const bf16x8 *>(p + 16 * s);
+    }
+    f32x16 acc[RH][D / 32];
+    float mb[RH], l[RH];  // the running maxima times the scale, and the sums
+#pragma unroll
+    for (int f = 0; f < RH; ++f) {
+        mb[f] = kNone, l[f] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[f][d][i] = 0.0f;
+    }
 
     const int P = 1 << a.s.page_shift;
     const int64_t unit = (int64_t)P * D;
     const int32_t *const table = a.s.page_table + it.b * a.s.pt_ld;
+    const int begin = group_lo & ~(kTile - 1), tiles = group_hi > begin ? (group_hi - begin + kTile - 1) / kTile : 0;
 
     // of a thread's tasks: keys (token, 32 elements) below 2 D, values (16 tokens s and half h, 4 elements) from there
     auto is_key = [&](int n) { return tid + n * NT < 2 * D; };
-    auto sub_of = [&](int n) { return is_key(n) ? (tid + n * NT) / (D / 32) / 16 : (tid + n * NT - 2 * D) / (D / 4) / 2; };
-    auto page_of = [&](int t, int n) -> int {  // page of the task's 16 tokens in the tile at t, -1 if there is none
-        const int at = t + 16 * sub_of(n);
-        const int page = at >> a.s.page_shift;
-        if (tid + n * NT >= kTasks || at >= group_hi || page >= a.s.width) return -1;
+    auto page_of = [&](int i, int n) -> int {  // page of the task's 16 tokens in tile i, -1 if there is none
+        const int task = tid + n * NT, sub = is_key(n) ? task / (D / 32) / 16 + 2 : (task - 2 * D) / (D / 4) / 2;
+        const int at = begin + i * kTile + 16 * sub, page = at >> a.s.page_shift;
+        if (task >= kTasks || at < begin || at >= group_hi || page >= a.s.width) return -1;
         const int id = table[page];
         return (unsigned)id < (uint64_t)a.s.pages ? id : -1;
     };
-    uint32_t raw[TN][8];
-    int exps[TN], ids[TN], next_ids[TN];
-    auto load = [&](int t) {
+    struct Codes {
+        uint32_t w[TN][8];
+        int e[TN];  // exponent byte, -1 where there is no page
+    };
+    int ids[TN];
+    Codes x;
+    auto load = [&](int i) {  // tile i, whose pages are in `ids`
 #pragma unroll
         for (int n = 0; n < TN; ++n) {
             const int task = tid + n * NT;
-            exps[n] = 127;
+            x.e[n] = -1;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) raw[n][i] = 0;
+            for (int j = 0; j < 8; ++j) x.w[n][j] = 0;
             if (ids[n] < 0) continue;
             const int64_t u = (int64_t)ids[n] * a.Hkv + it.head;
             if (is_key(n)) {
                 const int tok = task / (D / 32), part = task % (D / 32);
-                exps[n] = a.k_scales[u];
-                const u32x4 *const p = reinterpret_cast<const u32x4 *>(a.k_codes + u * unit + (int64_t)((t + tok) & (P - 1)) * D + 32 * part);
-                const u32x4 x = p[0], y = p[1];
+                x.e[n] = a.k_scales[u];
+                const u32x4 *const p = reinterpret_cast<const u32x4 *>(a.k_codes + u * unit + (int64_t)((begin + i * kTile + 32 + tok) & (P - 1)) * D + 32 * part);
+                const u32x4 y = p[0], z = p[1];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) raw[n][i] = x[i], raw[n][4 + i] = y[i];
+                for (int j = 0; j < 4; ++j) x.w[n][j] = y[j], x.w[n][4 + j] = z[j];
             } else {
                 const int group = (task - 2 * D) / (D / 4), el = (task - 2 * D) % (D / 4), tok = 16 * (group >> 1) + 4 * (group & 1);
-                exps[n] = a.v_scales[u];
-                const uint8_t *const p = a.v_codes + u * unit + (int64_t)((t + tok) & (P - 1)) * D + 4 * el;
+                x.e[n] = a.v_scales[u];
+                const uint8_t *const p = a.v_codes + u * unit + (int64_t)((begin + i * kTile + tok) & (P - 1)) * D + 4 * el;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) raw[n][i] = *reinterpret_cast<const uint32_t *>(p + ((i & 3) + 8 * (i >> 2)) * D);
+                for (int j = 0; j < 8; ++j) x.w[n][j] = *reinterpret_cast<const uint32_t *>(p + ((j & 3) + 8 * (j >> 2)) * D);
             }
         }
     };
-    auto expand = [&](int t, unsigned char *to, int *flag) {
-        int found = 0;
+    auto expand = [&](int i) {
 #pragma unroll
         for (int n = 0; n < TN; ++n) {
             const int task = tid + n * NT;
             if (task >= kTasks) continue;
-            const float scale = exp2_of(min(exps[n], 254) - 127);
+            const float scale = exp2_of(min(max(x.e[n], 1), 254) - 127);
             if (is_key(n)) {
                 const int tok = task / (D / 32), part = task % (D / 32);
-                if (ids[n] < 0) found |= 1 << (tok / 16);
+                if (x.e[n] < 0) atomicOr(&flags[(i + tok / 32) & 3], 1 << ((tok / 16) ^ 2));
+                unsigned char *const to = keys[i & 1] + ((tok / 32) * (D / 16) + 2 * part) * kBlock16 + (tok & 31) * 16;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    *reinterpret_cast<bf16x8 *>(to + ((tok / 32) * (D / 16) + 2 * part + j / 2) * kBlock16 + (j & 1) * 512 + (tok & 31) * 16) =
-                        expand8(raw[n][2 * j], raw[n][2 * j + 1], scale);
+                    *reinterpret_cast<bf16x8 *>(to + (j / 2) * kBlock16 + (j & 1) * 512) = expand8(x.w[n][2 * j], x.w[n][2 * j + 1], scale);
             } else {
                 const int group = (task - 2 * D) / (D / 4), el = (task - 2 * D) % (D / 4), tok = 16 * (group >> 1) + 4 * (group & 1);
+                const int t = begin + i * kTile;
                 // places that no row sees may hold anything, NaN codes among it: a zero probability would not hide those
                 if (t < group_lo || t + kTile > group_hi)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int at = t + tok + (i & 3) + 8 * (i >> 2);
-                        raw[n][i] = at >= group_lo && at < group_hi ? raw[n][i] : 0u;
+                    for (int j = 0; j < 8; ++j) {
+                        const int at = t + tok + (j & 3) + 8 * (j >> 2);
+                        x.w[n][j] = at >= group_lo && at < group_hi ? x.w[n][j] : 0u;
                     }
                 uint32_t odd = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) odd |= nan_bytes(raw[n][i]);
-                if (odd) found |= 16;
+                for (int j = 0; j < 8; ++j) odd |= nan_bytes(x.w[n][j]);
+                if (odd) atomicOr(&flags[i & 3], 16);
                 const float both[2] = {scale, scale};
                 bf16x8 turned[4];
-                turn8(raw[n], both, turned);
+                turn8(x.w[n], both, turned);
+                unsigned char *const to = values[i & 1] + (group >> 1) * (D / 32) * kBlock16 + (group & 1) * 512;
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
                     const int block = D == 64 ? d & 1 : d + 4 * (el / 32), slot = D == 64 ? el + 16 * (d >> 1) : el & 31;
-                    *reinterpret_cast<bf16x8 *>(to + (kKeys + (group >> 1) * (D / 32) + block) * kBlock16 + ((group & 1) * 32 + slot) * 16) = turned[d];
+                    *reinterpret_cast<bf16x8 *>(to + block * kBlock16 + slot * 16) = turned[d];
                 }
             }
         }
-        if (found) atomicOr(flag, found);
     };
-    auto compute = [&](int t, const unsigned char *from, int flag) {
-        const unsigned char *const mine = from + lane * 16;
-        f32x16 s[2];
+    f32x16 s[2][RH];  // of the tile's first and second 32 tokens
+    float top[RH];
+    auto scores = [&](int i, int half, int to) {
+        const unsigned char *const from = keys[i & 1] + lane * 16 + half * (D / 16) * kBlock16;
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
+        for (int f = 0; f < RH; ++f)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[tt][i] = 0.0f;
+            for (int j = 0; j < 16; ++j) s[to][f][j] = 0.0f;
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(mine + (tt * (D / 16) + k) * kBlock16), q[k], s[tt], 0, 0, 0);
+        for (int k = 0; k < D / 16; ++k) {
+            const bf16x8 y = *reinterpret_cast<const bf16x8 *>(from + k * kBlock16);
+#pragma unroll
+            for (int f = 0; f < RH; ++f) s[to][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, q[f][k], s[to][f], 0, 0, 0);
         }
-        const bool edge = t < all_lo || t + kTile > all_hi || (flag & 15);
-        uint32_t seen = ~0u;
+    };
+    auto maxima = [&](int of) {
+#pragma unroll
+        for (int f = 0; f < RH; ++f) {
+            float m = s[of][f][0];
+#pragma unroll
+            for (int j = 1; j < 16; ++j) m = fmaxf(m, s[of][f][j]);
+            const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false));
+            top[f] = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale;
+        }
+    };
+    // whether row f sees the place of the j-th of the lane's scores of 32 tokens from t on
+    auto sees = [&](int t, int flag, int f, int j) {
+        const int off = 8 * (j / 4) + 4 * h + j % 4, at = t + off;
+        return at >= max(first[f], group_lo) && at <= pos[f] && at < group_hi && !(flag >> (j / 8) & 1);
+    };
+    auto half_step = [&](int i, int half, int flag) {
+        const int t = begin + i * kTile + 32 * half, bad = flag >> (2 * half) & 3;
+        const bool edge = t < all_lo || t + 32 > all_hi || bad;
         if (edge) {
-            seen = 0;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const int off = 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * h + i % 4, at = t + off;
-                if (at >= max(first, lo) && at <= pos && at < hi && !(flag >> (off / 16) & 1))
-                    seen |= 1u << i;
-                else
-                    s[i / 16][i % 16] = kNone;
-            }
+            for (int f = 0; f < RH; ++f)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[half][f][j] = sees(t, bad, f, j) ? s[half][f][j] : kNone;
+            maxima(half);
         }
-        float top = s[0][0];
-#pragma unroll
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale;
         // The maximum only follows where a row's scores have outgrown it by 2^8: sums and products hold that in 32 bits, a
         // probability of BF16 has the same relative rounding, and most tiles need no pass over the sums.
-        if (__any(top > mb + 8.0f)) {
-            const float next = fmaxf(mb, top), by = next == kNone ? 1.0f : __builtin_amdgcn_exp2f(mb - next);
-            mb = next;
-            l *= by;
+        bool grown = false;
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d)
+        for (int f = 0; f < RH; ++f) grown |= top[f] > mb[f] + 8.0f;
+        if (__any(grown))
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[d][i] *= by;
-        }
-        const float base = mb == kNone ? 0.0f : mb;
-        bf16x8 p[4];
+            for (int f = 0; f < RH; ++f) {
+                const float next = fmaxf(mb[f], top[f]), by = next == kNone ? 1.0f : __builtin_amdgcn_exp2f(mb[f] - next);
+                mb[f] = next;
+                l[f] *= by;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float e[8];
+                for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[k / 2][8 * (k % 2) + i], a.scale, -base));
-            l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-            p[k] = four(pack2(e[0], e[1]), pack2(e[2], e[3]), pack2(e[4], e[5]), pack2(e[6], e[7]));
-        }
-        const unsigned char *const values = mine + kKeys * kBlock16;
-        if (edge && (flag & 16)) {
-            // NaN values that some rows see and others do not: out of the product, and into the rows that see them by the
-            // product of where they are with who sees them
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t w = seen >> (8 * k);
-                const bf16x8 who = four(ones(w), ones(w >> 2), ones(w >> 4), ones(w >> 6));
-                for (int d = 0; d < D / 32; ++d) {
-                    u32x4 v = *reinterpret_cast<const u32x4 *>(values + (k * (D / 32) + d) * kBlock16), where;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t n = ((v[i] & 0x7fffu) > 0x7f80u ? 0xffffu : 0u) | ((v[i] & 0x7fff0000u) > 0x7f800000u ? 0xffff0000u : 0u);
-                        where[i] = n & 0x3f803f80u;
-                        v[i] &= ~n;
-                    }
-                    f32x16 hit;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) hit[i] = 0.0f;
-                    hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, where), who, hit, 0, 0, 0);
-#pragma unroll
-                    for (int dd = 0; dd < D / 32; ++dd)
-                        if (dd == d) {
-                            acc[dd] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), p[k], acc[dd], 0, 0, 0);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) acc[dd][i] = hit[i] > 0.0f ? __builtin_nanf("") : acc[dd][i];
-                        }
-                }
+                    for (int j = 0; j < 16; ++j) acc[f][d][j] *= by;
             }
-            return;
-        }
+        const unsigned char *const from = values[i & 1] + lane * 16 + 2 * half * (D / 32) * kBlock16;
+        bf16x8 p[RH][2];
+        auto exponentials = [&](int k) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+            for (int f = 0; f < RH; ++f) {
+                const float base = mb[f] == kNone ? 0.0f : mb[f];
+                float e[8];
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d)
-                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(values + (k * (D / 32) + d) * kBlock16), p[k], acc[d], 0, 0, 0);
+                for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(s[half][f][8 * k + j], a.scale, -base));
+                l[f] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+                p[f][k] = four(pack2(e[0], e[1]), pack2(e[2], e[3]), pack2(e[4], e[5]), pack2(e[6], e[7]));
+            }
+        };
+        auto products = [&](int k) {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) {
+                const bf16x8 v = *reinterpret_cast<const bf16x8 *>(from + (k * (D / 32) + d) * kBlock16);
+#pragma unroll
+                for (int f = 0; f < RH; ++f) acc[f][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[f][k], acc[f][d], 0, 0, 0);
+            }
+        };
+        __builtin_amdgcn_sched_barrier(0);
+        scores(i, half, half ^ 1);
+        exponentials(0);
+        interleave<RH * (D / 16), 320 / D, 128 / D, RH>();
+        products(0);
+        exponentials(1);
+        interleave<RH * (D / 32), 640 / D, 256 / D, RH>();
+        products(1);
+        maxima(half ^ 1);
+        if (half) expand(i + 1);
+        interleave<RH * (D / 32), 4, 0, RH>();
     };
 
-    const int begin = group_lo & ~(kTile - 1), tiles = group_hi > begin ? (group_hi - begin + kTile - 1) / kTile : 0;
-    if (tid < 3) flags[tid] = 0;
-    if (tiles > 0) {
-#pragma unroll
-        for (int n = 0; n < TN; ++n) ids[n] = page_of(begin, n);
-        load(begin);
+    // Values of tile i that are NaN and that some rows of the workgroup see and others do not: out of the product, and a bit for
+    // each row and element that sees one.
+    auto set_nan_aside = [&](int i, int flag) {
+        for (int j = tid; j < kTile * (D / 32); j += NT) (&nans[0][0])[j] = 0;
         __syncthreads();
-        expand(begin, tile[0], &flags[0]);
-#pragma unroll
-        for (int n = 0; n < TN; ++n) next_ids[n] = tiles > 1 ? page_of(begin + kTile, n) : -1;
-    }
-    for (int i = 0; i < tiles; ++i) {
-        const int t = begin + i * kTile;
-        __syncthreads();
-        if (tid == 0) flags[(i + 2) % 3] = 0;
-        if (i + 1 < tiles) {
-#pragma unroll
-            for (int n = 0; n < TN; ++n) {
-                ids[n] = next_ids[n];
-                next_ids[n] = i + 2 < tiles ? page_of(t + 2 * kTile, n) : -1;
-            }
-            load(t + kTile);
+        for (int block = wave; block < kHalf; block += NW) {
+            uint16_t *const v = reinterpret_cast<uint16_t *>(values[i & 1] + block * kBlock16 + lane * 16);
+            for (int j = 0; j < 8; ++j)
+                if ((v[j] & 0x7fff) > 0x7f80) {
+                    v[j] = 0;
+                    atomicOr(&nans[16 * (block / (D / 32)) + 4 * h + (j & 3) + 8 * (j >> 2)][block % (D / 32)], 1u << col);
+                }
         }
-        if (t < hi && t + kTile > lo) compute(t, tile[i & 1], __builtin_amdgcn_readfirstlane(flags[i % 3]));
-        if (i + 1 < tiles) expand(t + kTile, tile[(i + 1) & 1], &flags[(i + 1) % 3]);
+        __syncthreads();
+        for (int j = 0; j < kTile; ++j) {
+            const int at = begin + i * kTile + j;
+#pragma unroll
+            for (int f = 0; f < RH; ++f)
+                if (at >= max(first[f], group_lo) && at <= pos[f] && at < group_hi && !(flag >> (j / 16) & 1))
+                    for (int d = 0; d < D / 32; ++d) marks[f * (D / 32) + d][tid] |= nans[j][d];
+        }
+        __syncthreads();
+    };
+
+    if (tid < 4) flags[tid] = 0;
+    for (int j = 0; j < RH * (D / 32); ++j) marks[j][tid] = 0;
+    if (tiles > 0) {
+        auto pages_of = [&](int i) {
+#pragma unroll
+            for (int n = 0; n < TN; ++n) ids[n] = page_of(i, n);
+        };
+        pages_of(-1);
+        load(-1);
+        pages_of(0);
+        __syncthreads();
+        expand(-1);
+        load(0);
+        pages_of(1);
+        __syncthreads();
+        scores(-1, 1, 0);
+        maxima(0);
+        expand(0);
+        for (int i = 0; i < tiles; ++i) {
+            __syncthreads();
+            const int flag = __builtin_amdgcn_readfirstlane(flags[i & 3]);
+            if (tid == 0) flags[(i + 3) & 3] = 0;
+            load(i + 1);
+            pages_of(i + 2);
+            if ((flag & 16) && (begin + i * kTile < rows_lo || begin + (i + 1) * kTile > rows_hi)) set_nan_aside(i, flag);
+            half_step(i, 0, flag);
+            half_step(i, 1, flag);
+        }
     }
 
-    l += __shfl_xor(l, 32);
-    if (r >= rows) return;
-    const bool split = it.chunks > 1;
-    float *const part = slot_at(c, D, it.slot);
-    const int local = 32 * wave + col;
-    if (split && h == 0) part[c.rows * D + local] = mb, part[c.rows * D + c.rows + local] = l;
-    const float inv = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-    uint16_t *const y = a.y + (int64_t)(it.sp.q0 + token) * a.ldy + (int64_t)head * D;
-    // acc[d][i] of the lane is element 4 * e + d % 4 of its row, e = (8 (i / 4) + 4 h + i % 4) + 32 (d / 4); with 64 elements
-    // the rows from 16 on of the product hold the upper two of each four
 #pragma unroll
-    for (int b = 0; b < (D + 127) / 128; ++b)
+    for (int f = 0; f < RH; ++f) {
+        l[f] += __shfl_xor(l[f], 32);
+        const int local = 32 * (RH * wave + f) + col;
+        if (tile0 + local >= rows) continue;
+        const bool split = it.chunks > 1;
+        float *const part = slot_at(c, D, it.slot);
+        if (split && h == 0) part[c.rows * D + local] = mb[f], part[c.rows * D + c.rows + local] = l[f];
+        const float inv = split ? 1.0f : l[f] == 0.0f ? 0.0f : 1.0f / l[f];
+        uint16_t *const y = a.y + (int64_t)(it.sp.q0 + token[f]) * a.ldy + (int64_t)head[f] * D;
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-            if constexpr (D == 64) {
-                const int e = 4 * ((8 * i4 + 4 * h) & 15) + (i4 >= 2 ? 2 : 0);
+        for (int d = 0; d < D / 32; ++d)
+            if (const uint32_t mark = marks[f * (D / 32) + d][tid] >> (4 * h))
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float x = acc[0][4 * i4 + i] * inv, z = acc[1][4 * i4 + i] * inv;
-                    if (split)
-                        *reinterpret_cast<f32x2 *>(part + local * D + e + 4 * i) = f32x2{x, z};
-                    else
-                        *reinterpret_cast<uint32_t *>(y + e + 4 * i) = pack2(x, z);
-                }
-            } else {
-                const int e = 4 * (8 * i4 + 4 * h) + 128 * b;
-                if (split) {
+                for (int i = 0; i < 16; ++i)
+                    if (mark >> (8 * (i / 4) + i % 4) & 1) acc[f][d][i] = __builtin_nanf("");
+        // acc[d][i] of the lane is element 4 e + d % 4 of its row, e = (8 (i / 4) + 4 h + i % 4) + 32 (d / 4); with 64 elements
+        // the product's rows from 16 on hold the upper two of each four
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<f32x4 *>(part + local * D + e + 4 * i) = f32x4{acc[4 * b][4 * i4 + i], acc[4 * b + 1][4 * i4 + i],
-                                                                                         acc[4 * b + 2][4 * i4 + i], acc[4 * b + 3][4 * i4 + i]};
+        for (int b = 0; b < (D + 127) / 128; ++b)
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) {
+                if constexpr (D == 64) {
+                    const int e = 4 * ((8 * i4 + 4 * h) & 15) + (i4 >= 2 ? 2 : 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = acc[f][0][4 * i4 + i] * inv, z = acc[f][1][4 * i4 + i] * inv;
+                        if (split)
+                            *reinterpret_cast<f32x2 *>(part + local * D + e + 4 * i) = f32x2{x, z};
+                        else
+                            *reinterpret_cast<uint32_t *>(y + e + 4 * i) = pack2(x, z);
+                    }
                 } else {
+                    const int e = 4 * (8 * i4 + 4 * h) + 128 * b;
+                    if (split) {
 #pragma unroll
-                    for (int i = 0; i < 4; i += 2) {
-                        u32x4 w;
+                        for (int i = 0; i < 4; ++i)
+                            *reinterpret_cast<f32x4 *>(part + local * D + e + 4 * i) = f32x4{acc[f][4 * b][4 * i4 + i], acc[f][4 * b + 1][4 * i4 + i],
+                                                                                             acc[f][4 * b + 2][4 * i4 + i], acc[f][4 * b + 3][4 * i4 + i]};
+                    } else {
 #pragma unroll
-                        for (int k = 0; k < 2; ++k)
-                            w[2 * k] = pack2(acc[4 * b][4 * i4 + i + k] * inv, acc[4 * b + 1][4 * i4 + i + k] * inv),
-                            w[2 * k + 1] = pack2(acc[4 * b + 2][4 * i4 + i + k] * inv, acc[4 * b + 3][4 * i4 + i + k] * inv);
-                        *reinterpret_cast<u32x4 *>(y + e + 4 * i) = w;
+                        for (int i = 0; i < 4; i += 2) {
+                            u32x4 w;
+#pragma unroll
+                            for (int k = 0; k < 2; ++k)
+                                w[2 * k] = pack2(acc[f][4 * b][4 * i4 + i + k] * inv, acc[f][4 * b + 1][4 * i4 + i + k] * inv),
+                                w[2 * k + 1] = pack2(acc[f][4 * b + 2][4 * i4 + i + k] * inv, acc[f][4 * b + 3][4 * i4 + i + k] * inv);
+                            *reinterpret_cast<u32x4 *>(y + e + 4 * i) = w;
+                        }
                     }
                 }
             }
-        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ partial sums
@@ -793,7 +872,11 @@ int64_t kv8_attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D)
 template <int D>
 static int launch_attention(const Kv8Attend &a, hipStream_t s)
 {
-    constexpr int kWaves = D == 256 ? 4 : 8, kRows = 32 * kWaves;
+    #ifndef VRH
+#define VRH 1
+#define VNW 8
+#endif
+    constexpr int kHalves = D == 256 ? 1 : VRH, kWaves = D == 256 ? 4 : VNW, kRows = 32 * kWaves * kHalves;
     const int64_t G = a.Hq / a.Hkv, T = a.s.T, B = a.s.B;
     const bool ws = a.ws && a.ws_bytes >= kWorkspace;
     // If every sequence has a token, none has more than T - B + 1 of them.  (Where some have none, one may have more: attend_few
@@ -814,7 +897,7 @@ static int launch_attention(const Kv8Attend &a, hipStream_t s)
         if (int rc = go(attend_few<D>, Cut{kFewRows, kFewTarget, 2, 0, many ? kFewMost : INT32_MAX, true, a.ws}, kFewThreads)) return rc;
     if (!many) return MQ_OK;
     const int target = many_target(kRows, D);
-    return go(attend_many<D, kWaves>, Cut{kRows, target, 4, B > 1 ? kFewMost : 0, INT32_MAX, T * G / kRows * a.Hkv < 2 * target, a.ws}, 64 * kWaves);
+    return go(attend_many<D, kHalves, kWaves>, Cut{kRows, target, 4, B > 1 ? kFewMost : 0, INT32_MAX, T * G / kRows * a.Hkv < 2 * target, a.ws}, 64 * kWaves);
 }
 
 int launch_kv8_attention(const Kv8Attend &a, hipStream_t s)
