@@ -189,12 +189,11 @@ static __device__ __forceinline__ float weight_of(float m, float l, float top)
 // 0x01 in the bytes that are NaN codes
 static __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u; }
 
-// The order of the instructions since the last such mark: N matrix instructions, an LDS read in front of every RH-th of them,
-// and behind each V vector instructions and T transcendental ones.
+// The order of instructions: N matrix instructions, behind each V vector instructions and T transcendental ones, and an LDS
+// read behind every RH-th.
 template <int N, int V, int T, int RH>
 static __device__ __forceinline__ void interleave()
 {
-    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -202,7 +201,6 @@ static __device__ __forceinline__ void interleave()
         if (V > 0) __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
         if (T > 0) __builtin_amdgcn_sched_group_barrier(0x400, T, 0);
     }
-    __builtin_amdgcn_sched_barrier(0);
 }
 
 // Four bytes of each of eight tokens' rows (the same four head elements), turned round: out[d] = element d of the eight tokens
@@ -581,10 +579,12 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
                         const int at = t + tok + (j & 3) + 8 * (j >> 2);
                         x.w[n][j] = at >= group_lo && at < group_hi ? x.w[n][j] : 0u;
                     }
-                uint32_t odd = 0;
+                if (t < rows_lo || t + kTile > rows_hi) {  // some rows of the workgroup do not see all of it
+                    uint32_t odd = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) odd |= nan_bytes(x.w[n][j]);
-                if (odd) atomicOr(&flags[i & 3], 16);
+                    for (int j = 0; j < 8; ++j) odd |= nan_bytes(x.w[n][j]);
+                    if (odd) atomicOr(&flags[i & 3], 16);
+                }
                 const float both[2] = {scale, scale};
                 bf16x8 turned[4];
                 turn8(x.w[n], both, turned);
@@ -599,15 +599,23 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
     };
     f32x16 s[2][RH];  // of the tile's first and second 32 tokens
     float top[RH];
-    auto scores = [&](int i, int half, int to) {
-        const unsigned char *const from = keys[i & 1] + lane * 16 + half * (D / 16) * kBlock16;
+    #ifndef KAHEAD
+#define KAHEAD 2
+#endif
+    constexpr int kAhead = KAHEAD;  // LDS reads ahead of their products
+    bf16x8 first_keys[kAhead];
+    auto read_keys = [&](const unsigned char *from) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) first_keys[k] = *reinterpret_cast<const bf16x8 *>(from + k * kBlock16);
+    };
+    auto scores = [&](const unsigned char *from, int to) {
 #pragma unroll
         for (int f = 0; f < RH; ++f)
 #pragma unroll
             for (int j = 0; j < 16; ++j) s[to][f][j] = 0.0f;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-            const bf16x8 y = *reinterpret_cast<const bf16x8 *>(from + k * kBlock16);
+            const bf16x8 y = k < kAhead ? first_keys[k] : *reinterpret_cast<const bf16x8 *>(from + k * kBlock16);
 #pragma unroll
             for (int f = 0; f < RH; ++f) s[to][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, q[f][k], s[to][f], 0, 0, 0);
         }
@@ -627,7 +635,10 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
         const int off = 8 * (j / 4) + 4 * h + j % 4, at = t + off;
         return at >= max(first[f], group_lo) && at <= pos[f] && at < group_hi && !(flag >> (j / 8) & 1);
     };
+    const unsigned char *key_at, *value_at;
     auto half_step = [&](int i, int half, int flag) {
+        const unsigned char *const next = key_at + half * (D / 16) * kBlock16, *const from = value_at + 2 * half * (D / 32) * kBlock16;
+        read_keys(next);
         const int t = begin + i * kTile + 32 * half, bad = flag >> (2 * half) & 3;
         const bool edge = t < all_lo || t + 32 > all_hi || bad;
         if (edge) {
@@ -653,7 +664,6 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
 #pragma unroll
                     for (int j = 0; j < 16; ++j) acc[f][d][j] *= by;
             }
-        const unsigned char *const from = values[i & 1] + lane * 16 + 2 * half * (D / 32) * kBlock16;
         bf16x8 p[RH][2];
         auto exponentials = [&](int k) {
 #pragma unroll
@@ -675,7 +685,7 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
             }
         };
         __builtin_amdgcn_sched_barrier(0);
-        scores(i, half, half ^ 1);
+        scores(next, half ^ 1);
         exponentials(0);
         interleave<RH * (D / 16), 320 / D, 128 / D, RH>();
         products(0);
@@ -683,8 +693,8 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
         interleave<RH * (D / 32), 640 / D, 256 / D, RH>();
         products(1);
         maxima(half ^ 1);
-        if (half) expand(i + 1);
         interleave<RH * (D / 32), 4, 0, RH>();
+        if (half) expand(i + 1);
     };
 
     // Values of tile i that are NaN and that some rows of the workgroup see and others do not: out of the product, and a bit for
@@ -726,16 +736,19 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
         load(0);
         pages_of(1);
         __syncthreads();
-        scores(-1, 1, 0);
+        read_keys(keys[1] + lane * 16 + (D / 16) * kBlock16);
+        scores(keys[1] + lane * 16 + (D / 16) * kBlock16, 0);
         maxima(0);
         expand(0);
         for (int i = 0; i < tiles; ++i) {
             __syncthreads();
-            const int flag = __builtin_amdgcn_readfirstlane(flags[i & 3]);
+            const int own_flag = flags[i & 3];
             if (tid == 0) flags[(i + 3) & 3] = 0;
             load(i + 1);
             pages_of(i + 2);
-            if ((flag & 16) && (begin + i * kTile < rows_lo || begin + (i + 1) * kTile > rows_hi)) set_nan_aside(i, flag);
+            const int flag = __builtin_amdgcn_readfirstlane(own_flag);
+            if (flag & 16) set_nan_aside(i, flag);
+            key_at = keys[i & 1] + lane * 16, value_at = values[i & 1] + lane * 16;
             half_step(i, 0, flag);
             half_step(i, 1, flag);
         }
