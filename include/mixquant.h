@@ -55,7 +55,8 @@ typedef enum {
     MQ_ERR_ALIGN = 3,  /* a pointer or leading dimension breaks the stated alignment */
     MQ_ERR_ARG = 4,    /* unknown enum value */
     MQ_ERR_HIP = 5,    /* kernel launch failed; see mq_last_hip_error() */
-    MQ_ERR_SCRATCH = 6 /* nvfp4_gemm_noalloc: the problem wants more scratch than its static array holds */
+    MQ_ERR_SCRATCH = 6 /* nvfp4_gemm_noalloc: the problem wants more scratch than its static array holds;
+                          nvfp4_matvec: than the workspace holds */
 } mq_status;
 
 typedef enum {
@@ -247,14 +248,20 @@ int bf16_gemm_ws(const void *x_bf16, int64_t ldx, const void *w_bf16, int64_t ld
 /*
  * BF16 activations times NVFP4 weights, for the few tokens of a decode step (W4A16; the prefill's weights, read as they are):
  *    Y[m, n] = alpha_w * sum_k x[m, k] * E4M3(w_scales[n, k/16]) * E2M1(w_codes[n, k])
- * Every product is exact, sums are accumulated in FP32, alpha_w is applied once to the sum, and the result is written as BF16
- * (nearest even) or FP32.  Bound by reading W up to about 64 tokens; more are computed 64 at a time, reading W again.
+ * Products are formed in FP16 of x * 2^e, e bringing the token's largest finite magnitude to 2^14 .. 2^15, and of the exact
+ * weights: exact for every element of x down to 2^-29 of that magnitude, below that the element is off by at most 2^-38 of it
+ * (K % 64 != 0: exact in FP32).  Sums are accumulated in FP32, alpha_w is applied once to the sum, and the result is written as
+ * BF16 (nearest even) or FP32.  Bound by reading W up to about 64 tokens; more are computed 64 at a time, reading W again.
  * x: [M, K] BF16, row stride ldx.  K % 16 == 0 (K % 64 == 0 for MQ_LAYOUT_KTILE); x, w_codes 16-byte aligned, ldx % 8 == 0,
  * scale arrays 4-byte aligned when K % 64 == 0; any ldy >= N, y aligned to its element.  M <= 65535, N and K < 2^31.
+ * workspace: device memory, 16-byte aligned, of mq_nvfp4_matvec_workspace_bytes(M, N, K) bytes (0 for up to four tokens of
+ * at most 32768 elements in all, K rounded up to a multiple of 128, and where K % 64 != 0), or the call is refused with MQ_ERR_SCRATCH; otherwise as in nvfp4_gemm_ws.
  * Results are bit-identical from run to run.
  */
+int64_t mq_nvfp4_matvec_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int nvfp4_matvec(const void *x_bf16, int64_t ldx, const uint8_t *w_codes, const uint8_t *w_scales, const float *w_alpha_dev,
-                 int64_t M, int64_t N, int64_t K, void *y, int64_t ldy, int out, int layout, void *stream);
+                 int64_t M, int64_t N, int64_t K, void *y, int64_t ldy, int out, int layout, void *workspace,
+                 int64_t workspace_bytes, void *stream);
 
 /*
  * The attention half of a decoder block over a paged 8-bit cache (the keys and values that a prefill worker leaves for the

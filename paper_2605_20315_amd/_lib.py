@@ -71,7 +71,9 @@ def load() -> ctypes.CDLL:
     lib.mq_bf16_gemm_workspace_bytes.restype = i64
     lib.mq_bf16_gemm_workspace_bytes.argtypes = [i64, i64, i64]
     lib.nvfp4_matvec.restype = ci
-    lib.nvfp4_matvec.argtypes = [vp, i64, vp, vp, vp, i64, i64, i64, vp, i64, ci, ci, vp]
+    lib.nvfp4_matvec.argtypes = [vp, i64, vp, vp, vp, i64, i64, i64, vp, i64, ci, ci, vp, i64, vp]
+    lib.mq_nvfp4_matvec_workspace_bytes.restype = i64
+    lib.mq_nvfp4_matvec_workspace_bytes.argtypes = [i64, i64, i64]
     f64 = ctypes.c_double
     lib.mq_rope_table.restype = ci
     lib.mq_rope_table.argtypes = [vp, i64, ci, f64, ci, f64, i64, f64, f64, f64, vp]

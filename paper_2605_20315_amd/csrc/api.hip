@@ -45,6 +45,7 @@ static int ensure_device(int *slot_out)
     if (slot_out) *slot_out = dev;
     if (g_device_ready[dev].load(std::memory_order_acquire)) return MQ_OK;
     if (int rc = configure_gemm_kernels()) return rc;
+    if (int rc = configure_matvec_kernels()) return rc;
     void *ptr = nullptr;
     e = hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch));
     if (e != hipSuccess || ptr == nullptr) return note_launch(e != hipSuccess ? e : hipErrorInvalidSymbol);
@@ -315,9 +316,10 @@ int bf16_gemm_ws(const void *x_bf16, int64_t ldx, const void *w_bf16, int64_t ld
 }
 
 int nvfp4_matvec(const void *x_bf16, int64_t ldx, const uint8_t *w_codes, const uint8_t *w_scales, const float *w_alpha_dev,
-                 int64_t M, int64_t N, int64_t K, void *y, int64_t ldy, int out, int layout, void *stream)
+                 int64_t M, int64_t N, int64_t K, void *y, int64_t ldy, int out, int layout, void *workspace,
+                 int64_t workspace_bytes, void *stream)
 {
-    if (M < 0 || N < 0 || K <= 0 || K % kBlock != 0 || ldx < K) return MQ_ERR_SHAPE;
+    if (M < 0 || N < 0 || K <= 0 || K % kBlock != 0 || ldx < K || workspace_bytes < 0) return MQ_ERR_SHAPE;
     if (out != MQ_OUT_BF16 && out != MQ_OUT_FP32) return MQ_ERR_ARG;
     if (layout != MQ_LAYOUT_LINEAR && layout != MQ_LAYOUT_KTILE) return MQ_ERR_ARG;
     if (layout == MQ_LAYOUT_KTILE && K % 64 != 0) return MQ_ERR_SHAPE;
@@ -326,8 +328,17 @@ int nvfp4_matvec(const void *x_bf16, int64_t ldx, const uint8_t *w_codes, const 
     if (!x_bf16 || !w_codes || !w_scales || !w_alpha_dev || !y) return MQ_ERR_NULL;
     if (!aligned(x_bf16, 16) || ldx % 8 != 0 || !aligned(w_codes, 16) || !aligned(w_alpha_dev, 4)) return MQ_ERR_ALIGN;
     if (!aligned(y, out == MQ_OUT_BF16 ? 2 : 4) || (K % 64 == 0 && !aligned(w_scales, 4))) return MQ_ERR_ALIGN;
+    if (workspace && !aligned(workspace, 16)) return MQ_ERR_ALIGN;
+    if (matvec_workspace(M, N, K) > (workspace ? workspace_bytes : 0)) return MQ_ERR_SCRATCH;
+    if (int rc = ensure_device(nullptr)) return rc;
     return launch_nvfp4_matvec(static_cast<const uint16_t *>(x_bf16), ldx, w_codes, w_scales, w_alpha_dev, M, N, K, y, ldy, out, layout,
-                               static_cast<hipStream_t>(stream));
+                               workspace, static_cast<hipStream_t>(stream));
+}
+
+int64_t mq_nvfp4_matvec_workspace_bytes(int64_t M, int64_t N, int64_t K)
+{
+    if (M <= 0 || N <= 0 || K <= 0 || K % kBlock != 0) return 0;
+    return matvec_workspace(M, N, K);
 }
 
 int mq_rope_table(float *table, int64_t max_pos, int rot_dim, double base, int scaling, double factor, int64_t original_max_pos,
@@ -481,7 +492,7 @@ const char *mq_status_string(int status)
     case MQ_ERR_HIP: return "MQ_ERR_HIP: kernel launch failed (see mq_last_hip_error)";
     case MQ_ERR_SCRATCH:
         return "MQ_ERR_SCRATCH: the problem wants more scratch memory than the static array of "
-               "nvfp4_gemm_noalloc holds (use nvfp4_gemm_ws with a workspace)";
+               "nvfp4_gemm_noalloc holds (use nvfp4_gemm_ws with a workspace), or than the workspace given to nvfp4_matvec";
     default: return "unknown mq_status";
     }
 }

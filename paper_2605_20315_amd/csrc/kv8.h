@@ -59,7 +59,9 @@ int launch_kv8_append(const Kv8Append &a, hipStream_t s);
 int launch_kv8_attention(const Kv8Attend &a, hipStream_t s);
 int64_t kv8_attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D);
 int launch_nvfp4_matvec(const uint16_t *x, int64_t ldx, const uint8_t *codes, const uint8_t *scales, const float *alpha, int64_t M,
-                        int64_t N, int64_t K, void *y, int64_t ldy, int out, int layout, hipStream_t s);
+                        int64_t N, int64_t K, void *y, int64_t ldy, int out, int layout, void *ws, hipStream_t s);
+int64_t matvec_workspace(int64_t M, int64_t N, int64_t K);
+int configure_matvec_kernels();
 
 #if defined(__HIPCC__)
 // One sequence as the kernels see it: its new tokens q0 .. q0 + n, the place `start` of the first of them (negative where the

@@ -318,9 +318,17 @@ def nvfp4_linear(x_bf16: torch.Tensor, alpha_x: torch.Tensor, w_codes, w_scales,
     return nvfp4_gemm_ws(xc, xs, alpha_x, w_codes, w_scales, alpha_w, workspace, out, y, layout)
 
 
+def mq_nvfp4_matvec_workspace_bytes(M: int, N: int, K: int) -> int:
+    """Workspace size that nvfp4_matvec needs (0: none)."""
+    return int(_lib.load().mq_nvfp4_matvec_workspace_bytes(M, N, K))
+
+
 def nvfp4_matvec(x_bf16: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, w_alpha: torch.Tensor,
-                 out: int = MQ_OUT_BF16, y: torch.Tensor | None = None, layout: int = MQ_LAYOUT_LINEAR) -> torch.Tensor:
-    """Y = X . dequant(W)^T for the few tokens of a decode step: BF16 activations as they are, NVFP4 weights, FP32 accumulation."""
+                 out: int = MQ_OUT_BF16, y: torch.Tensor | None = None, layout: int = MQ_LAYOUT_LINEAR,
+                 workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Y = X . dequant(W)^T for the few tokens of a decode step: BF16 activations, NVFP4 weights, FP32 accumulation.
+    workspace: any contiguous GPU tensor of mq_nvfp4_matvec_workspace_bytes; where that is not 0 and none is given, one is
+    taken from torch's allocator for the call."""
     _need_gpu(x_bf16, w_codes, w_scales, w_alpha)
     assert x_bf16.dtype == torch.bfloat16 and w_alpha.dtype == torch.float32
     M, K, ldx = _rows_k_ld(x_bf16)
@@ -335,8 +343,15 @@ def nvfp4_matvec(x_bf16: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Te
     assert y.is_cuda and y.shape == (M, N) and (N <= 1 or y.stride(1) == 1)
     assert y.dtype == (torch.bfloat16 if out == MQ_OUT_BF16 else torch.float32)
     ldy = y.stride(0) if M > 1 else max(y.stride(0), N)
+    ws_bytes = mq_nvfp4_matvec_workspace_bytes(M, N, K)
+    if workspace is None and ws_bytes:
+        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=x_bf16.device)
+    ws_ptr = 0
+    if workspace is not None:
+        assert workspace.is_cuda and workspace.is_contiguous()
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     rc = _lib.load().nvfp4_matvec(x_bf16.data_ptr(), ldx, w_codes.data_ptr(), w_scales.data_ptr(), w_alpha.data_ptr(), M, N, K,
-                                  y.data_ptr(), ldy, out, layout, _stream())
+                                  y.data_ptr(), ldy, out, layout, ws_ptr, ws_bytes, _stream())
     _lib.check(rc, "nvfp4_matvec")
     return y
 
