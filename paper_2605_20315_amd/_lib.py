@@ -124,7 +124,8 @@ def load_binding():
                       "with `python -m paper_2605_20315_amd.build`", RuntimeWarning)
         return NoBinding()
     names = ("nvfp4_global_scale", "nvfp4_quantize", "nvfp4_quantize_silu_mul", "nvfp4_quantize_rmsnorm",
-             "nvfp4_relayout", "nvfp4_gemm_ws", "bf16_gemm_ws")
+             "nvfp4_relayout", "nvfp4_gemm_ws", "bf16_gemm_ws", "nvfp4_matvec", "mq_nvfp4_matvec_workspace_bytes", "kv8_append",
+             "kv8_attention")
     _binding.bind(check, {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names})
     return _binding
 

@@ -33,6 +33,10 @@ decltype(&::nvfp4_quantize_rmsnorm) p_quantize_rmsnorm;
 decltype(&::nvfp4_relayout) p_relayout;
 decltype(&::nvfp4_gemm_ws) p_gemm_ws;
 decltype(&::bf16_gemm_ws) p_bf16_gemm_ws;
+decltype(&::nvfp4_matvec) p_matvec;
+decltype(&::mq_nvfp4_matvec_workspace_bytes) p_matvec_workspace;
+decltype(&::kv8_append) p_append;
+decltype(&::kv8_attention) p_attention;
 PyObject *g_check;
 
 // "Not of the plain form" is a return value (false, a null pointer, None) and no C++ exception: one of those takes 3.7 us, as
@@ -395,6 +399,149 @@ PyObject *bf16_gemm_ws(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+PyObject *matvec(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 8, [&]() -> PyObject * {
+        // x, w_codes, w_scales, w_alpha, out, y, layout, workspace
+        const at::Tensor *x = typed(a[0], at::kBFloat16), *alpha = typed(a[3], at::kFloat);
+        Rows r;
+        Packed w;
+        Product p;
+        int layout;
+        if (!x || !alpha || !r.read(*x) || !w.read(a[1], a[2]) || w.K != r.K || r.K % 16 || !integer(a[6], layout)) return general();
+        if (!p.read(a[7], a[4], a[5]) || (p.out != MQ_OUT_BF16 && p.out != MQ_OUT_FP32)) return general();
+        const int64_t M = r.rows, N = w.rows, K = r.K;
+        if (p.y.obj) {
+            const at::Tensor &y = *p.y.t;
+            if (y.scalar_type() != (p.out == MQ_OUT_BF16 ? at::kBFloat16 : at::kFloat) || y.dim() != 2 || y.size(0) != M || y.size(1) != N ||
+                (N > 1 && y.stride(1) != 1))
+                return general();
+        }
+        p.allocate_y(M, N, *x);
+        at::Tensor made;
+        if (!p.ws && a[7] == Py_None) {
+            if (const int64_t bytes = p_matvec_workspace(M, N, K)) {
+                made = at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(x->device()));
+                p.ws = made.data_ptr(), p.ws_bytes = bytes;
+            }
+        }
+        void *const st = current_stream(), *const y = p.y.t->data_ptr();
+        const void *xp = x->data_ptr();
+        const uint8_t *c = w.codes(), *s = w.scales();
+        const float *ap = static_cast<const float *>(alpha->data_ptr());
+        if (!enqueue("nvfp4_matvec", [&] { return p_matvec(xp, r.ld, c, s, ap, M, N, K, y, p.ldy, p.out, layout, p.ws, p.ws_bytes, st); }))
+            return nullptr;
+        return give(p.y);
+    });
+}
+
+// a BF16 [tokens, heads, D] tensor whose heads are adjacent
+struct Heads {
+    const at::Tensor *t;
+    int64_t T, H, D, ld;
+    bool read(PyObject *o)
+    {
+        if (!(t = typed(o, at::kBFloat16)) || t->dim() != 3 || t->stride(2) != 1) return false;
+        T = t->size(0), H = t->size(1), D = t->size(2);
+        if (H > 1 && t->stride(1) != D) return false;
+        ld = T > 1 ? t->stride(0) : std::max(t->stride(0), H * D);
+        return true;
+    }
+};
+
+// the cache and the sequences of a call: k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens
+struct Cache {
+    const at::Tensor *kc, *ks, *vc, *vs, *pt, *cu, *lens;
+    int64_t pages, Hkv, P, D, B, W, pt_ld;
+    bool read(PyObject *const *a)
+    {
+        if (!(kc = typed(a[0], at::kByte)) || !(ks = typed(a[1], at::kByte)) || !(vc = typed(a[2], at::kByte)) || !(vs = typed(a[3], at::kByte)))
+            return false;
+        if (!(pt = typed(a[4], at::kInt)) || !(cu = typed(a[5], at::kInt)) || !(lens = typed(a[6], at::kInt))) return false;
+        if (kc->dim() != 4 || ks->dim() != 2 || pt->dim() != 2 || lens->dim() != 1 || cu->dim() != 1) return false;
+        pages = kc->size(0), Hkv = kc->size(1), P = kc->size(2), D = kc->size(3), B = lens->size(0), W = pt->size(1);
+        if (vc->sizes() != kc->sizes() || ks->size(0) != pages || ks->size(1) != Hkv || vs->sizes() != ks->sizes()) return false;
+        if (pt->size(0) != B || cu->size(0) != B + 1 || (W > 1 && pt->stride(1) != 1)) return false;
+        for (const at::Tensor *t : {kc, ks, vc, vs, cu, lens})
+            if (!t->is_contiguous()) return false;
+        pt_ld = B > 1 ? pt->stride(0) : std::max(pt->stride(0), W);
+        return Hkv <= INT32_MAX;
+    }
+    static uint8_t *bytes(const at::Tensor *t) { return static_cast<uint8_t *>(t->data_ptr()); }
+    static const int32_t *ints(const at::Tensor *t) { return static_cast<const int32_t *>(t->data_ptr()); }
+};
+
+at::Tensor make_heads(const Heads &h)
+{
+    return at::empty({h.T, h.H, h.D}, at::TensorOptions().dtype(at::kBFloat16).device(h.t->device()));
+}
+
+PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 14, [&]() -> PyObject * {
+        // q, k, v, cache and sequences (7), table, positions, interleaved, q_out
+        Heads q, k, v;
+        Cache c;
+        Out out;
+        int interleaved;
+        const bool has_table = a[10] != Py_None, has_positions = a[11] != Py_None;
+        const at::Tensor *table = has_table ? typed(a[10], at::kFloat) : nullptr, *positions = has_positions ? typed(a[11], at::kInt) : nullptr;
+        if (!q.read(a[0]) || !k.read(a[1]) || !v.read(a[2]) || !c.read(a + 3) || !integer(a[12], interleaved) || !out.read(a[13])) return general();
+        if (has_table && (!table || table->dim() != 2 || !table->is_contiguous() || table->size(1) > INT32_MAX)) return general();
+        if (has_positions && (!positions || positions->dim() != 1 || positions->size(0) != q.T || !positions->is_contiguous())) return general();
+        if (q.D != c.D || k.T != q.T || v.T != q.T || k.H != c.Hkv || v.H != c.Hkv || k.D != c.D || v.D != c.D || q.H > INT32_MAX) return general();
+        if (out.obj && (out.t->scalar_type() != at::kBFloat16 || out.t->sizes() != q.t->sizes() || !out.t->is_contiguous())) return general();
+        if (!out.obj) out.made = make_heads(q), out.t = &out.made;
+        void *const st = current_stream(), *const op = out.t->data_ptr();
+        const void *qp = q.t->data_ptr(), *kp = k.t->data_ptr(), *vp = v.t->data_ptr();
+        const int rot = has_table ? (int)table->size(1) : 0;
+        const float *tp = rot ? static_cast<const float *>(table->data_ptr()) : nullptr;
+        const int64_t max_pos = has_table ? table->size(0) : 0;
+        const int32_t *pp = has_positions ? Cache::ints(positions) : nullptr;
+        if (!enqueue("kv8_append", [&] {
+                return p_append(qp, q.ld, kp, k.ld, vp, v.ld, op, Cache::bytes(c.kc), Cache::bytes(c.ks), Cache::bytes(c.vc), Cache::bytes(c.vs),
+                                c.pages, (int)std::min<int64_t>(c.P, INT32_MAX), (int)q.H, (int)c.Hkv, (int)std::min<int64_t>(c.D, INT32_MAX),
+                                Cache::ints(c.pt), c.pt_ld, c.W, Cache::ints(c.cu), Cache::ints(c.lens), c.B, q.T, tp, max_pos, rot, pp,
+                                interleaved != 0, st);
+            }))
+            return nullptr;
+        return give(out);
+    });
+}
+
+PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 12, [&]() -> PyObject * {
+        // q, cache and sequences (7), sm_scale, window, y, workspace
+        Heads q, y;
+        Cache c;
+        Out out;
+        float scale;
+        int window;
+        if (!q.read(a[0]) || !c.read(a + 1) || !real(a[8], scale) || !integer(a[9], window) || !out.read(a[10])) return general();
+        if (q.D != c.D || q.H > INT32_MAX) return general();
+        if (out.obj && (!y.read(a[10]) || out.t->sizes() != q.t->sizes())) return general();
+        void *ws = nullptr;
+        int64_t ws_bytes = 0;
+        if (a[11] != Py_None) {
+            const at::Tensor *t = tensor(a[11]);
+            if (!t || !t->is_contiguous()) return general();
+            ws = t->data_ptr(), ws_bytes = t->numel() * t->element_size();
+        }
+        if (!out.obj) out.made = make_heads(q), out.t = &out.made, y.ld = q.H * q.D;
+        void *const st = current_stream(), *const op = out.t->data_ptr();
+        const void *qp = q.t->data_ptr();
+        if (!enqueue("kv8_attention", [&] {
+                return p_attention(qp, q.ld, Cache::bytes(c.kc), Cache::bytes(c.ks), Cache::bytes(c.vc), Cache::bytes(c.vs), c.pages,
+                                   (int)std::min<int64_t>(c.P, INT32_MAX), (int)q.H, (int)c.Hkv, (int)std::min<int64_t>(c.D, INT32_MAX),
+                                   Cache::ints(c.pt), c.pt_ld, c.W, Cache::ints(c.cu), Cache::ints(c.lens), c.B, q.T, scale, window, op, y.ld, ws,
+                                   ws_bytes, st);
+            }))
+            return nullptr;
+        return give(out);
+    });
+}
+
 // bind(check, addresses by name): where the library's functions are
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -414,6 +561,10 @@ PyObject *bind(PyObject *, PyObject *args)
     get("nvfp4_relayout", p_relayout);
     get("nvfp4_gemm_ws", p_gemm_ws);
     get("bf16_gemm_ws", p_bf16_gemm_ws);
+    get("nvfp4_matvec", p_matvec);
+    get("mq_nvfp4_matvec_workspace_bytes", p_matvec_workspace);
+    get("kv8_append", p_append);
+    get("kv8_attention", p_attention);
     if (!ok) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "bind: a function of the library is missing");
         return nullptr;
@@ -425,6 +576,7 @@ PyObject *bind(PyObject *, PyObject *args)
 #define MQ_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MQ_FAST(global_scale), MQ_FAST(quantize), MQ_FAST(quantize_silu_mul), MQ_FAST(quantize_rmsnorm),
                          MQ_FAST(relayout),     MQ_FAST(gemm_ws),  MQ_FAST(linear),            MQ_FAST(bf16_gemm_ws),
+                         MQ_FAST(matvec),       MQ_FAST(append),  MQ_FAST(attention),
                          {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Plain-form calls of the mixquant library.", -1, methods};
 

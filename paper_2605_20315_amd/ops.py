@@ -329,6 +329,9 @@ def nvfp4_matvec(x_bf16: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Te
     """Y = X . dequant(W)^T for the few tokens of a decode step: BF16 activations, NVFP4 weights, FP32 accumulation.
     workspace: any contiguous GPU tensor of mq_nvfp4_matvec_workspace_bytes; where that is not 0 and none is given, one is
     taken from torch's allocator for the call."""
+    done = _fast.matvec(x_bf16, w_codes, w_scales, w_alpha, out, y, layout, workspace)
+    if done is not None:
+        return done
     _need_gpu(x_bf16, w_codes, w_scales, w_alpha)
     assert x_bf16.dtype == torch.bfloat16 and w_alpha.dtype == torch.float32
     M, K, ldx = _rows_k_ld(x_bf16)
@@ -405,6 +408,9 @@ def kv8_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_codes: torch
                q_out: torch.Tensor | None = None) -> torch.Tensor:
     """Rotates q [T, Hq, D] and k [T, Hkv, D] and appends k and v to the paged FP8 cache; returns the rotated queries.
     table: what mq_rope_table gives, [max_pos, rot_dim], or None for no rotation.  kv_lens count the new tokens."""
+    done = _fast.append(q, k, v, k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, table, positions, interleaved, q_out)
+    if done is not None:
+        return done
     _need_gpu(q, k, v)
     T, Hq, D, ldq = _heads_ld(q)
     Tk, Hkv, Dk, ldk = _heads_ld(k)
@@ -441,6 +447,9 @@ def kv8_attention(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tensor
                   y: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Causal attention of q [T, Hq, D], the last tokens of their sequences, over the paged FP8 cache; BF16 [T, Hq, D].
     window > 0: a token sees itself and the window - 1 places before it.  workspace: any contiguous GPU tensor, or None."""
+    done = _fast.attention(q, k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, sm_scale, window, y, workspace)
+    if done is not None:
+        return done
     _need_gpu(q)
     T, Hq, D, ldq = _heads_ld(q)
     pages, P, Hkv, pt_ld, W, B = _cache(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, T, D)
