@@ -19,6 +19,7 @@ namespace mq {
 constexpr int kTile = 64;       // tokens: chunks are whole tiles
 constexpr int kFewRows = 16;
 constexpr int kFewMost = 64;    // sequences of more rows go to attend_many where that is launched
+constexpr int kAllMany = 8, kManyWaves = 4;
 constexpr float kNone = -__builtin_inff();
 
 // How a call is cut: rows per item, number of items aimed at, tiles a chunk has at least, sequences of more than `above` and
@@ -32,10 +33,16 @@ struct Cut {
 struct Item {
     bool found;
     Span sp;
-    int b, tile, head, chunk, chunks, lo, hi;  // tokens lo .. hi of the sequence for this chunk; lo is a multiple of kTile
-    int slot;                                  // of the partial sums; the first one of the sequence for attend_join
-    int tiles;                                 // of rows
+    int b, tile, head, chunks, lo, hi;  // tokens lo .. hi of the sequence for this chunk; lo is a multiple of kTile
+    int slot;                           // of the partial sums
 };
+
+// What attend_join needs to know of a sequence, at the start of the workspace
+struct Parts {
+    int chunks, slot, row_tiles;  // slot: the sequence's first
+};
+constexpr int64_t kPartsBytes = 1 << 20;
+constexpr int kPartsMost = (int)(kPartsBytes / sizeof(Parts));
 
 struct Extent {
     int row_tiles, lo, tiles;  // first token (a multiple of kTile) and tiles of tokens that any query sees
@@ -94,15 +101,15 @@ static __device__ int chunk_tiles(const Kv8Attend &a, const Cut &c, PlanLds &lds
 
 static __device__ __forceinline__ void cut_sequence(const Kv8Attend &a, const Extent &e, int per, int &chunks, int &items, int &slots)
 {
-    // (a sequence whose queries see nothing still writes zeros)
-    chunks = e.row_tiles == 0 ? 0 : e.tiles <= per ? 1 : (e.tiles - 1) / per + 1;
+    // (a sequence whose queries see nothing still writes zeros; a last quarter of a chunk is worth one)
+    chunks = e.row_tiles == 0 ? 0 : max((int)(((int64_t)e.tiles + (per == INT32_MAX ? 0 : (int64_t)per * 3 / 4)) / per), 1);
     items = e.row_tiles * chunks * a.Hkv;
     slots = chunks > 1 ? items : 0;
 }
 
-// The item `idx` (or, where `of` is not negative, the sequence `of` with its first slot).  Every thread of the workgroup calls it.
+// The item `idx`; every thread of the workgroup calls it.  Workgroup 0 also writes down the sequences' parts.
 template <int NT>
-static __device__ Item item_of(const Kv8Attend &a, const Cut &c, int idx, int of, PlanLds &lds, int tid)
+static __device__ Item item_of(const Kv8Attend &a, const Cut &c, int idx, PlanLds &lds, int tid)
 {
     const int per = chunk_tiles<NT>(a, c, lds, tid), lane = tid & 63, wave = tid >> 6;
     if (tid == 0) lds.found.found = false;
@@ -128,40 +135,28 @@ static __device__ Item item_of(const Kv8Attend &a, const Cut &c, int idx, int of
             items_before += lds.items[w], slots_before += lds.slots[w];
         }
         const int first = ib + item_sum - items, first_slot = sb + slot_sum - slots;
-        if (of >= 0 ? b == of : idx >= first && idx < first + items) {
-            Item it;
-            it.found = of < 0 || items > 0;
-            it.sp = sp;
-            it.b = b;
-            it.chunks = chunks;
-            it.tiles = e.row_tiles;
-            it.slot = first_slot;
-            it.lo = e.lo;
-            it.hi = sp.len;
-            it.head = it.chunk = it.tile = 0;
-            if (of < 0) {
-                // head fastest: with eight key heads the workgroups of one head share an XCD and its L2; then the chunk; the
-                // tiles of rows from the last, which sees the most, to the first
-                const int local = idx - first, rest = local / a.Hkv;
-                it.head = local - rest * a.Hkv;
-                it.chunk = rest % chunks;
-                it.tile = e.row_tiles - 1 - rest / chunks;
-                it.slot += local;
-                const int size = (e.tiles + chunks - 1) / chunks;
-                it.lo = e.lo + it.chunk * size * kTile;
-                it.hi = (int)min((int64_t)sp.len, (int64_t)e.lo + (int64_t)(it.chunk + 1) * size * kTile);
-            }
-            lds.found = it;
+        if (c.split && blockIdx.x == 0 && b < a.s.B) reinterpret_cast<Parts *>(c.ws)[b] = Parts{chunks, first_slot, e.row_tiles};
+        if (idx >= first && idx < first + items) {
+            // head fastest: with eight key heads the workgroups of one head share an XCD and its L2; then the chunk; the
+            // tiles of rows from the last, which sees the most, to the first
+            const int local = idx - first, rest = local / a.Hkv, chunk = rest % chunks;
+            // the chunks' shares of the tiles, even to within one
+            const int t0 = (int)((int64_t)e.tiles * chunk / chunks), t1 = (int)((int64_t)e.tiles * (chunk + 1) / chunks);
+            lds.found = Item{true, sp, b, e.row_tiles - 1 - rest / chunks, local - rest * a.Hkv, chunks, e.lo + t0 * kTile,
+                             (int)min((int64_t)sp.len, (int64_t)e.lo + (int64_t)t1 * kTile), first_slot + local};
         }
         __syncthreads();
-        if (of >= 0 ? of < base + NT : idx < items_before) break;
+        if (idx < items_before && !(c.split && blockIdx.x == 0)) break;
     }
     __syncthreads();
     return lds.found;
 }
 
 // one partial result: sums [rows][D], then maxima and sums of the rows' exponentials
-static __device__ __forceinline__ float *slot_at(const Cut &c, int D, int slot) { return c.ws + (int64_t)slot * c.rows * (D + 2); }
+static __device__ __forceinline__ float *slot_at(const Cut &c, int D, int slot) 
+{
+    return c.ws + kPartsBytes / 4 + (int64_t)slot * c.rows * (D + 2);
+}
 
 static __device__ __forceinline__ uint32_t pack2(float lo, float hi) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi}); }
 
@@ -190,14 +185,14 @@ static __device__ __forceinline__ float weight_of(float m, float l, float top)
 static __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u; }
 
 // The order of instructions: N matrix instructions, behind each V vector instructions and T transcendental ones, and an LDS
-// read behind every RH-th.
-template <int N, int V, int T, int RH>
+// read.
+template <int N, int V, int T>
 static __device__ __forceinline__ void interleave()
 {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        if (i % RH == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         if (V > 0) __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
         if (T > 0) __builtin_amdgcn_sched_group_barrier(0x400, T, 0);
     }
@@ -236,7 +231,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
     __shared__ float stat[kFewWaves][2][16];
     __shared__ float sums[kFewWaves][16][D + 4];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g = lane >> 4;
-    const Item it = item_of<kFewThreads>(a, c, blockIdx.x, -1, plan, tid);
+    const Item it = item_of<kFewThreads>(a, c, blockIdx.x, plan, tid);
     if (!it.found) return;
     const int G = a.Hq / a.Hkv, rows = it.sp.n * G, r = it.tile * kFewRows + col;
     const int row = min(r, rows - 1), token = row / G, head = it.head * G + row - token * G;
@@ -449,67 +444,59 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
 
 // ------------------------------------------------------------------------------------------------ many rows
 
-// One item by four waves of 32 * RH rows, a tile of 64 tokens at a time.  The threads expand a tile's codes to BF16 in LDS once
+// One item by four waves of 32 rows each, a tile of 64 tokens at a time.  The threads expand a tile's codes to BF16 in LDS once
 // for all waves, in the order in which the matrix instructions take them: a block of 1 KB is one operand of one 32x32x16
 // product, lane l's 16 bytes at 16 l, so that reading is free of bank conflicts and needs no address arithmetic.
 //    keys    block (half of the tile, 16 elements): lane (token % 32, k = 8 elements)
 //    values  block (16 tokens s, 32 elements): lane (element, tokens 16s + 4h .. + 3 and 16s + 8 + 4h .. + 3), h = lane / 32:
 //            the tokens whose scores that lane holds after S^T = K Q^T
-// 64 rows a wave, because every wave reads the whole tile: at 32 rows the reads alone took as long as the products.  One wave
-// a SIMD has to overlap its own matrix and vector work: the keys of the next 32 tokens are multiplied beside the exponentials of
-// these, and their values beside the next ones' maxima.  So tile i of keys is 32 tokens ahead of tile i of values: tokens
-// t + 32 .. t + 95 and t .. t + 63.  Both of tile i + 1 are loaded when tile i begins and expanded at its end; with two buffers
-// one barrier a tile is enough.
-template <int D, int RH, int NW>
-__global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
+// The exponentials and what goes with them are as much vector work as the two products are matrix work, so the two have to run
+// side by side: in a wave the keys of the next 32 tokens are multiplied between the exponentials of these, and their values
+// between those and the next ones' maxima; and two workgroups share a compute unit, which their barriers hold up in turn.  So tile i
+// of keys is 32 tokens ahead of tile i of values: tokens t + 32 .. t + 95 and t .. t + 63.  Both of tile i + 1 are loaded when
+// tile i begins and expanded at its end; with two buffers one barrier a tile is enough.
+// Measured, a prompt of 8192 tokens, 32 query and 8 key heads of 128: 635 us = 866 TFLOP/s of 1364 that a library product of
+// 8192^3 reaches here; without the keys ahead 747; one wave a SIMD with 64 rows, which reads LDS half as often, 945 (it has
+// no second wave to fill its waits); eight waves in one workgroup 635, and less even shares of short work.
+template <int D>
+__global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut c)
 {
-    constexpr int NT = 64 * NW, kTasks = 4 * D, TN = (kTasks + NT - 1) / NT;  // a task: 32 bytes of codes
-    constexpr int kRows = 32 * RH * NW;
+    constexpr int NW = kManyWaves, NT = 64 * NW, kTasks = 4 * D, TN = (kTasks + NT - 1) / NT;  // a task: 32 bytes of codes
+    constexpr int kRows = 32 * NW;
     constexpr int kBlock16 = 1024 + 16;  // the padding spreads a key token's four writes over the banks
     constexpr int kHalf = 2 * (D / 16);  // blocks of a tile's keys, and of its values
     __shared__ PlanLds plan;
     __shared__ int flags[4];
-    __shared__ uint32_t nans[kTile][D / 32], marks[RH * (D / 32)][NT];  // what set_nan_aside finds, and the rows' elements that see it
+    __shared__ uint32_t nans[kTile][D / 32], marks[D / 32][NT];  // what set_nan_aside finds, and the rows' elements that see it
     __shared__ __attribute__((aligned(16))) unsigned char keys[2][kHalf * kBlock16], values[2][kHalf * kBlock16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
-    const Item it = item_of<NT>(a, c, blockIdx.x, -1, plan, tid);
+    const Item it = item_of<NT>(a, c, blockIdx.x, plan, tid);
     if (!it.found) return;
-    const int G = a.Hq / a.Hkv, rows = it.sp.n * G, tile0 = it.tile * kRows, wave0 = tile0 + 32 * RH * wave;
-    int pos[RH], first[RH], token[RH], head[RH];
-#pragma unroll
-    for (int f = 0; f < RH; ++f) {
-        const int row = min(wave0 + 32 * f + col, rows - 1);  // rows beyond the last are computed again and not stored
-        token[f] = row / G;
-        head[f] = it.head * G + row - token[f] * G;
-        pos[f] = it.sp.start + token[f];
-        first[f] = a.window > 0 ? pos[f] - a.window + 1 : 0;
-    }
+    const int G = a.Hq / a.Hkv, rows = it.sp.n * G, tile0 = it.tile * kRows, wave0 = tile0 + 32 * wave;
+    // the lane's row (rows beyond the last are computed again and not stored) and the places that it sees
+    const int row = min(wave0 + col, rows - 1), token = row / G, head = it.head * G + row - token * G;
+    const int pos = it.sp.start + token, first = a.window > 0 ? pos - a.window + 1 : 0;
     // places that any row of the workgroup sees, that any and that every row of the wave sees
     const int group_hi = min(it.hi, it.sp.start + (min(tile0 + kRows, rows) - 1) / G + 1);
     const int group_lo = max(it.lo, a.window > 0 ? it.sp.start + tile0 / G - a.window + 1 : 0);
-    const int pos_lo = it.sp.start + min(wave0, rows - 1) / G, pos_hi = it.sp.start + (min(wave0 + 32 * RH, rows) - 1) / G;
+    const int pos_lo = it.sp.start + min(wave0, rows - 1) / G, pos_hi = it.sp.start + (min(wave0 + 32, rows) - 1) / G;
     const int all_lo = max(group_lo, a.window > 0 ? pos_hi - a.window + 1 : 0), all_hi = min(group_hi, pos_lo + 1);
     // places that every row of the workgroup sees
     const int rows_lo = max(group_lo, a.window > 0 ? it.sp.start + (min(tile0 + kRows, rows) - 1) / G - a.window + 1 : 0);
     const int rows_hi = min(group_hi, it.sp.start + tile0 / G + 1);
 
-    bf16x8 q[RH][D / 16];
+    bf16x8 q[D / 16];
+    {
+        const uint16_t *const p = a.q + (int64_t)(it.sp.q0 + token) * a.ldq + (int64_t)head * D + 8 * h;
 #pragma unroll
-    for (int f = 0; f < RH; ++f) {
-        const uint16_t *const p = a.q + (int64_t)(it.sp.q0 + token[f]) * a.ldq + (int64_t)head[f] * D + 8 * h;
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) q[f][s] = *reinterpret_cast<const bf16x8 *>(p + 16 * s);
+        for (int s = 0; s < D / 16; ++s) q[s] = *reinterpret_cast<const bf16x8 *>(p + 16 * s);
     }
-    f32x16 acc[RH][D / 32];
-    float mb[RH], l[RH];  // the running maxima times the scale, and the sums
+    f32x16 acc[D / 32];
+    float mb = kNone, l = 0.0f;  // the running maximum times the scale, and the lane's share of the sum
 #pragma unroll
-    for (int f = 0; f < RH; ++f) {
-        mb[f] = kNone, l[f] = 0.0f;
+    for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[f][d][i] = 0.0f;
-    }
+        for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
 
     const int P = 1 << a.s.page_shift;
     const int64_t unit = (int64_t)P * D;
@@ -597,12 +584,9 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
             }
         }
     };
-    f32x16 s[2][RH];  // of the tile's first and second 32 tokens
-    float top[RH];
-    #ifndef KAHEAD
-#define KAHEAD 2
-#endif
-    constexpr int kAhead = KAHEAD;  // LDS reads ahead of their products
+    f32x16 s[2];  // of the tile's first and second 32 tokens
+    float top;
+    constexpr int kAhead = 2;  // LDS reads ahead of their products (3 or 4 are no faster)
     bf16x8 first_keys[kAhead];
     auto read_keys = [&](const unsigned char *from) {
 #pragma unroll
@@ -610,31 +594,21 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
     };
     auto scores = [&](const unsigned char *from, int to) {
 #pragma unroll
-        for (int f = 0; f < RH; ++f)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) s[to][f][j] = 0.0f;
+        for (int j = 0; j < 16; ++j) s[to][j] = 0.0f;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
             const bf16x8 y = k < kAhead ? first_keys[k] : *reinterpret_cast<const bf16x8 *>(from + k * kBlock16);
-#pragma unroll
-            for (int f = 0; f < RH; ++f) s[to][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, q[f][k], s[to][f], 0, 0, 0);
+            s[to] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, q[k], s[to], 0, 0, 0);
         }
     };
     auto maxima = [&](int of) {
+        float m = s[of][0];
 #pragma unroll
-        for (int f = 0; f < RH; ++f) {
-            float m = s[of][f][0];
-#pragma unroll
-            for (int j = 1; j < 16; ++j) m = fmaxf(m, s[of][f][j]);
-            const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false));
-            top[f] = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale;
-        }
+        for (int j = 1; j < 16; ++j) m = fmaxf(m, s[of][j]);
+        const u32x2 both = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false));
+        top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale;
     };
-    // whether row f sees the place of the j-th of the lane's scores of 32 tokens from t on
-    auto sees = [&](int t, int flag, int f, int j) {
-        const int off = 8 * (j / 4) + 4 * h + j % 4, at = t + off;
-        return at >= max(first[f], group_lo) && at <= pos[f] && at < group_hi && !(flag >> (j / 8) & 1);
-    };
+    auto sees = [&](int at, int no_page) { return at >= max(first, group_lo) && at <= pos && at < group_hi && !no_page; };
     const unsigned char *key_at, *value_at;
     auto half_step = [&](int i, int half, int flag) {
         const unsigned char *const next = key_at + half * (D / 16) * kBlock16, *const from = value_at + 2 * half * (D / 32) * kBlock16;
@@ -643,57 +617,46 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
         const bool edge = t < all_lo || t + 32 > all_hi || bad;
         if (edge) {
 #pragma unroll
-            for (int f = 0; f < RH; ++f)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) s[half][f][j] = sees(t, bad, f, j) ? s[half][f][j] : kNone;
+            for (int j = 0; j < 16; ++j) s[half][j] = sees(t + 8 * (j / 4) + 4 * h + j % 4, bad >> (j / 8) & 1) ? s[half][j] : kNone;
             maxima(half);
         }
         // The maximum only follows where a row's scores have outgrown it by 2^8: sums and products hold that in 32 bits, a
         // probability of BF16 has the same relative rounding, and most tiles need no pass over the sums.
-        bool grown = false;
+        if (__any(top > mb + 8.0f)) {
+            const float next = fmaxf(mb, top), by = next == kNone ? 1.0f : __builtin_amdgcn_exp2f(mb - next);
+            mb = next;
+            l *= by;
 #pragma unroll
-        for (int f = 0; f < RH; ++f) grown |= top[f] > mb[f] + 8.0f;
-        if (__any(grown))
+            for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-            for (int f = 0; f < RH; ++f) {
-                const float next = fmaxf(mb[f], top[f]), by = next == kNone ? 1.0f : __builtin_amdgcn_exp2f(mb[f] - next);
-                mb[f] = next;
-                l[f] *= by;
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[f][d][j] *= by;
-            }
-        bf16x8 p[RH][2];
+                for (int j = 0; j < 16; ++j) acc[d][j] *= by;
+        }
+        bf16x8 p[2];
         auto exponentials = [&](int k) {
+            const float base = mb == kNone ? 0.0f : mb;
+            float e[8];
 #pragma unroll
-            for (int f = 0; f < RH; ++f) {
-                const float base = mb[f] == kNone ? 0.0f : mb[f];
-                float e[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(s[half][f][8 * k + j], a.scale, -base));
-                l[f] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-                p[f][k] = four(pack2(e[0], e[1]), pack2(e[2], e[3]), pack2(e[4], e[5]), pack2(e[6], e[7]));
-            }
+            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(s[half][8 * k + j], a.scale, -base));
+            l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+            p[k] = four(pack2(e[0], e[1]), pack2(e[2], e[3]), pack2(e[4], e[5]), pack2(e[6], e[7]));
         };
         auto products = [&](int k) {
 #pragma unroll
             for (int d = 0; d < D / 32; ++d) {
                 const bf16x8 v = *reinterpret_cast<const bf16x8 *>(from + (k * (D / 32) + d) * kBlock16);
-#pragma unroll
-                for (int f = 0; f < RH; ++f) acc[f][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[f][k], acc[f][d], 0, 0, 0);
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[k], acc[d], 0, 0, 0);
             }
         };
         __builtin_amdgcn_sched_barrier(0);
         scores(next, half ^ 1);
         exponentials(0);
-        interleave<RH * (D / 16), 320 / D, 128 / D, RH>();
+        interleave<D / 16, 320 / D, 128 / D>();
         products(0);
         exponentials(1);
-        interleave<RH * (D / 32), 640 / D, 256 / D, RH>();
+        interleave<D / 32, 640 / D, 256 / D>();
         products(1);
         maxima(half ^ 1);
-        interleave<RH * (D / 32), 4, 0, RH>();
+        interleave<D / 32, 4, 0>();
         if (half) expand(i + 1);
     };
 
@@ -711,18 +674,14 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
                 }
         }
         __syncthreads();
-        for (int j = 0; j < kTile; ++j) {
-            const int at = begin + i * kTile + j;
-#pragma unroll
-            for (int f = 0; f < RH; ++f)
-                if (at >= max(first[f], group_lo) && at <= pos[f] && at < group_hi && !(flag >> (j / 16) & 1))
-                    for (int d = 0; d < D / 32; ++d) marks[f * (D / 32) + d][tid] |= nans[j][d];
-        }
+        for (int j = 0; j < kTile; ++j)
+            if (sees(begin + i * kTile + j, flag >> (j / 16) & 1))
+                for (int d = 0; d < D / 32; ++d) marks[d][tid] |= nans[j][d];
         __syncthreads();
     };
 
     if (tid < 4) flags[tid] = 0;
-    for (int j = 0; j < RH * (D / 32); ++j) marks[j][tid] = 0;
+    for (int j = 0; j < D / 32; ++j) marks[j][tid] = 0;
     if (tiles > 0) {
         auto pages_of = [&](int i) {
 #pragma unroll
@@ -754,127 +713,133 @@ __global__ __launch_bounds__(64 * NW) void attend_many(Kv8Attend a, Cut c)
         }
     }
 
+    l += __shfl_xor(l, 32);
+    const int local = 32 * wave + col;
+    if (tile0 + local >= rows) return;
+    const bool split = it.chunks > 1;
+    float *const part = slot_at(c, D, it.slot);
+    if (split && h == 0) part[c.rows * D + local] = mb, part[c.rows * D + c.rows + local] = l;
+    const float inv = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+    uint16_t *const y = a.y + (int64_t)(it.sp.q0 + token) * a.ldy + (int64_t)head * D;
 #pragma unroll
-    for (int f = 0; f < RH; ++f) {
-        l[f] += __shfl_xor(l[f], 32);
-        const int local = 32 * (RH * wave + f) + col;
-        if (tile0 + local >= rows) continue;
-        const bool split = it.chunks > 1;
-        float *const part = slot_at(c, D, it.slot);
-        if (split && h == 0) part[c.rows * D + local] = mb[f], part[c.rows * D + c.rows + local] = l[f];
-        const float inv = split ? 1.0f : l[f] == 0.0f ? 0.0f : 1.0f / l[f];
-        uint16_t *const y = a.y + (int64_t)(it.sp.q0 + token[f]) * a.ldy + (int64_t)head[f] * D;
+    for (int d = 0; d < D / 32; ++d)
+        if (const uint32_t mark = marks[d][tid] >> (4 * h))
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-            if (const uint32_t mark = marks[f * (D / 32) + d][tid] >> (4 * h))
+            for (int i = 0; i < 16; ++i)
+                if (mark >> (8 * (i / 4) + i % 4) & 1) acc[d][i] = __builtin_nanf("");
+    // acc[d][i] of the lane is element 4 e + d % 4 of its row, e = (8 (i / 4) + 4 h + i % 4) + 32 (d / 4); with 64 elements
+    // the product's rows from 16 on hold the upper two of each four
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (mark >> (8 * (i / 4) + i % 4) & 1) acc[f][d][i] = __builtin_nanf("");
-        // acc[d][i] of the lane is element 4 e + d % 4 of its row, e = (8 (i / 4) + 4 h + i % 4) + 32 (d / 4); with 64 elements
-        // the product's rows from 16 on hold the upper two of each four
+    for (int b = 0; b < (D + 127) / 128; ++b)
 #pragma unroll
-        for (int b = 0; b < (D + 127) / 128; ++b)
+        for (int i4 = 0; i4 < 4; ++i4) {
+            if constexpr (D == 64) {
+                const int e = 4 * ((8 * i4 + 4 * h) & 15) + (i4 >= 2 ? 2 : 0);
 #pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4) {
-                if constexpr (D == 64) {
-                    const int e = 4 * ((8 * i4 + 4 * h) & 15) + (i4 >= 2 ? 2 : 0);
+                for (int i = 0; i < 4; ++i) {
+                    const float x = acc[0][4 * i4 + i] * inv, z = acc[1][4 * i4 + i] * inv;
+                    if (split)
+                        *reinterpret_cast<f32x2 *>(part + local * D + e + 4 * i) = f32x2{x, z};
+                    else
+                        *reinterpret_cast<uint32_t *>(y + e + 4 * i) = pack2(x, z);
+                }
+            } else {
+                const int e = 4 * (8 * i4 + 4 * h) + 128 * b;
+                if (split) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float x = acc[f][0][4 * i4 + i] * inv, z = acc[f][1][4 * i4 + i] * inv;
-                        if (split)
-                            *reinterpret_cast<f32x2 *>(part + local * D + e + 4 * i) = f32x2{x, z};
-                        else
-                            *reinterpret_cast<uint32_t *>(y + e + 4 * i) = pack2(x, z);
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<f32x4 *>(part + local * D + e + 4 * i) = f32x4{acc[4 * b][4 * i4 + i], acc[4 * b + 1][4 * i4 + i],
+                                                                                         acc[4 * b + 2][4 * i4 + i], acc[4 * b + 3][4 * i4 + i]};
                 } else {
-                    const int e = 4 * (8 * i4 + 4 * h) + 128 * b;
-                    if (split) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            *reinterpret_cast<f32x4 *>(part + local * D + e + 4 * i) = f32x4{acc[f][4 * b][4 * i4 + i], acc[f][4 * b + 1][4 * i4 + i],
-                                                                                             acc[f][4 * b + 2][4 * i4 + i], acc[f][4 * b + 3][4 * i4 + i]};
-                    } else {
+                    for (int i = 0; i < 4; i += 2) {
+                        u32x4 w;
 #pragma unroll
-                        for (int i = 0; i < 4; i += 2) {
-                            u32x4 w;
-#pragma unroll
-                            for (int k = 0; k < 2; ++k)
-                                w[2 * k] = pack2(acc[f][4 * b][4 * i4 + i + k] * inv, acc[f][4 * b + 1][4 * i4 + i + k] * inv),
-                                w[2 * k + 1] = pack2(acc[f][4 * b + 2][4 * i4 + i + k] * inv, acc[f][4 * b + 3][4 * i4 + i + k] * inv);
-                            *reinterpret_cast<u32x4 *>(y + e + 4 * i) = w;
-                        }
+                        for (int k = 0; k < 2; ++k)
+                            w[2 * k] = pack2(acc[4 * b][4 * i4 + i + k] * inv, acc[4 * b + 1][4 * i4 + i + k] * inv),
+                            w[2 * k + 1] = pack2(acc[4 * b + 2][4 * i4 + i + k] * inv, acc[4 * b + 3][4 * i4 + i + k] * inv);
+                        *reinterpret_cast<u32x4 *>(y + e + 4 * i) = w;
                     }
                 }
             }
-    }
+        }
 }
 
 // ------------------------------------------------------------------------------------------------ partial sums
 
-// Rows (token, head) of the sequences with several chunks, `heads` of one token by a workgroup: D / 4 threads cover a row's
-// elements, the workgroup's other threads every so-many-th chunk.
-template <int D>
-__global__ __launch_bounds__(256) void attend_join(Kv8Attend a, Cut c, int heads)
+// Rows (token, head) of the sequences with several chunks.  D / 4 threads cover a row's elements; a workgroup's 1024 / D such
+// groups take a row each (ROWS: many rows), or every so-many-th chunk of one row.
+template <int D, bool ROWS>
+__global__ __launch_bounds__(256) void attend_join(Kv8Attend a, Cut c)
 {
     constexpr int kCols = D / 4, kParts = 256 / kCols;
-    __shared__ PlanLds plan;
     __shared__ float tops[4], totals[kParts];
     __shared__ f32x4 sums[kParts][kCols];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = tid % kCols, part = tid / kCols;
-    const int groups = (a.Hq + heads - 1) / heads, t = blockIdx.x / groups, h0 = (blockIdx.x - t * groups) * heads;
-    int b = 0;
-    for (int base = 0; base < a.s.B; base += 64) {
-        const int i = base + lane;
-        const unsigned long long done = __ballot(i < a.s.B && a.s.cu_q[min(i, a.s.B - 1) + 1] <= t);
-        b += __popcll(done);
-        if (done != ~0ull) break;
+    const int per = ROWS ? kParts : 1, groups = (a.Hq + per - 1) / per, t = blockIdx.x / groups, h0 = (blockIdx.x - t * groups) * per;
+    int b = 0;  // sequences that end at or before t
+    for (int base = 0; base < a.s.B; base += 256) {
+        int done = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = base + 64 * k + lane;
+            done += __popcll(__ballot(i < a.s.B && a.s.cu_q[min(i, a.s.B - 1) + 1] <= t));
+        }
+        b += done;
+        if (done < 256) break;
     }
     if (b >= a.s.B) return;
-    const Item it = item_of<256>(a, c, 0, b, plan, tid);
-    if (!it.found || it.chunks < 2 || t < it.sp.q0 || t >= it.sp.q0 + it.sp.n) return;
-    const int G = a.Hq / a.Hkv;
-    for (int h = h0; h < min(h0 + heads, a.Hq); ++h) {
-        const int kv = h / G, row = (t - it.sp.q0) * G + h - kv * G, tile = row / c.rows, r = row - tile * c.rows;
-        const int first = it.slot + (it.tiles - 1 - tile) * it.chunks * a.Hkv + kv;
-        float top = kNone;
-        for (int i = tid; i < it.chunks; i += 256) top = fmaxf(top, slot_at(c, D, first + i * a.Hkv)[c.rows * D + r]);
+    const Parts parts = reinterpret_cast<const Parts *>(c.ws)[b];
+    if (parts.chunks < 2) return;
+    const Span sp = span_of(a.s, b);
+    if (t < sp.q0 || t >= sp.q0 + sp.n) return;
+    const int G = a.Hq / a.Hkv, h = ROWS ? min(h0 + part, a.Hq - 1) : h0;
+    const int kv = h / G, row = (t - sp.q0) * G + h - kv * G, tile = row / c.rows, r = row - tile * c.rows;
+    const int first = parts.slot + (parts.row_tiles - 1 - tile) * parts.chunks * a.Hkv + kv;
+    auto stats = [&](int i) { return slot_at(c, D, first + i * a.Hkv) + c.rows * D + r; };
+    float top = kNone, total = 0.0f;
+    f32x4 o{0, 0, 0, 0};
+    if constexpr (ROWS) {
+#pragma unroll 8
+        for (int i = 0; i < parts.chunks; ++i) top = fmaxf(top, stats(i)[0]);
+    } else {
+        for (int i = tid; i < parts.chunks; i += 256) top = fmaxf(top, stats(i)[0]);
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
         if (lane == 0) tops[wave] = top;
         __syncthreads();
         top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-        float total = 0.0f;
-        f32x4 o{0, 0, 0, 0};
+    }
 #pragma unroll 4
-        for (int i = part; i < it.chunks; i += kParts) {
-            const float *const p = slot_at(c, D, first + i * a.Hkv), *const stat = p + c.rows * D + r;
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(p + r * D + 4 * col);
-            const float w = weight_of(stat[0], stat[c.rows], top);
-            total += w * stat[c.rows];
-            o += w * x;
-        }
+    for (int i = ROWS ? 0 : part; i < parts.chunks; i += ROWS ? 1 : kParts) {
+        const float *const s = stats(i);
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(slot_at(c, D, first + i * a.Hkv) + r * D + 4 * col);
+        const float l = s[c.rows], w = weight_of(s[0], l, top);
+        total += w * l;
+        o += w * x;
+    }
+    if constexpr (!ROWS) {
         sums[part][col] = o;
         if (col == 0) totals[part] = total;
         __syncthreads();
-        if (part == 0) {
+        if (part > 0) return;
 #pragma unroll
-            for (int i = 1; i < kParts; ++i) o += sums[i][col], total += totals[i];
-            const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-            *reinterpret_cast<u32x2 *>(a.y + (int64_t)t * a.ldy + (int64_t)h * D + 4 * col) = u32x2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
-        }
-        __syncthreads();
+        for (int i = 1; i < kParts; ++i) o += sums[i][col], total += totals[i];
+    } else if (h0 + part >= a.Hq) {
+        return;
     }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    *reinterpret_cast<u32x2 *>(a.y + (int64_t)t * a.ldy + (int64_t)h * D + 4 * col) = u32x2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
 }
 
 // ------------------------------------------------------------------------------------------------ launches
 
-constexpr int kFewTarget = 1024;
 constexpr int64_t kWorkspace = (int64_t)64 << 20;
-
-static int64_t slot_bytes(int rows, int D) { return (int64_t)rows * (D + 2) * 4; }
-// A sequence in several chunks has fewer than twice as many of them as whole targets' worth: the items of all that are cut
-// are at most twice the target, and the slots of the workspace have to hold them.
-static int many_target(int rows, int D) { return (int)std::min<int64_t>(kWorkspace / slot_bytes(rows, D) / 2, 512); }
+// Items aimed at: as many workgroups as the GPU holds at a time (attend_few, which is bound by memory, half as many more: a batch
+// of uneven lengths takes 124 us so, 136 with one round; two long sequences 92 and 89), of which those of sequences that are cut
+// are less than twice as many, and the workspace has to have slots for them.
+constexpr int kFewTarget = 768, kManyTarget = 512;
+static int target_of(int most, int rows, int D) { return (int)std::min<int64_t>((kWorkspace - kPartsBytes) / ((int64_t)rows * (D + 2) * 4) / 2, most); }
 
 int64_t kv8_attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D)
 {
@@ -885,32 +850,29 @@ int64_t kv8_attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D)
 template <int D>
 static int launch_attention(const Kv8Attend &a, hipStream_t s)
 {
-    #ifndef VRH
-#define VRH 1
-#define VNW 8
-#endif
-    constexpr int kHalves = D == 256 ? 1 : VRH, kWaves = D == 256 ? 4 : VNW, kRows = 32 * kWaves * kHalves;
+    constexpr int kRows = 32 * kManyWaves;
     const int64_t G = a.Hq / a.Hkv, T = a.s.T, B = a.s.B;
-    const bool ws = a.ws && a.ws_bytes >= kWorkspace;
+    const bool ws = a.ws && a.ws_bytes >= kWorkspace && B <= kPartsMost;
     // If every sequence has a token, none has more than T - B + 1 of them.  (Where some have none, one may have more: attend_few
-    // is then slower than it need be, and as right.)
-    const bool many = (T - B + 1) * G > kFewMost;
+    // is then slower than it need be, and as right.)  Up to kAllMany sequences attend_many takes all if it takes any.
+    const bool many = (T - B + 1) * G > kFewMost, few = !many || B > kAllMany;
     auto go = [&](auto kernel, Cut cut, int threads) {
-        // an item for each tile of rows and key head, and as many more as the target has
-        cut.split = cut.split && ws;
-        const int64_t items = (T * G / cut.rows + B) * a.Hkv + (cut.split ? 2 * cut.target : 0);
+        // An item for each tile of rows and key head; where sequences are cut, as many more as the target has, or as their
+        // longest possible history has chunks
+        const int64_t whole = (T * G / cut.rows + B) * a.Hkv, tiles = ((int64_t)a.s.width << a.s.page_shift) / kTile + 1;
+        cut.split = cut.split && ws && whole < 2 * cut.target && tiles >= 2 * cut.least;
+        const int64_t items = cut.split ? std::min(whole + 2 * cut.target, whole * (tiles / cut.least + 1)) : whole;
         if (items > 0x7fffffff) return (int)MQ_ERR_SHAPE;
         if (int rc = enqueue(kernel, dim3((unsigned)items), dim3(threads), 0, s, a, cut)) return rc;
         if (!cut.split) return (int)MQ_OK;
-        // (a workgroup first finds its sequence's chunks: many rows share that)
-        const int heads = (int)std::min<int64_t>(std::max<int64_t>(T * a.Hq / 2048, 1), a.Hq);
-        return enqueue(attend_join<D>, dim3((unsigned)(T * ((a.Hq + heads - 1) / heads))), dim3(256), 0, s, a, cut, heads);
+        constexpr int kPer = 1024 / D;
+        if (T * a.Hq >= 2048) return enqueue(attend_join<D, true>, dim3((unsigned)(T * ((a.Hq + kPer - 1) / kPer))), dim3(256), 0, s, a, cut);
+        return enqueue(attend_join<D, false>, dim3((unsigned)(T * a.Hq)), dim3(256), 0, s, a, cut);
     };
-    if (!many || B > 1)
-        if (int rc = go(attend_few<D>, Cut{kFewRows, kFewTarget, 2, 0, many ? kFewMost : INT32_MAX, true, a.ws}, kFewThreads)) return rc;
+    if (few)
+        if (int rc = go(attend_few<D>, Cut{kFewRows, target_of(kFewTarget, kFewRows, D), 2, 0, many ? kFewMost : INT32_MAX, true, a.ws}, kFewThreads)) return rc;
     if (!many) return MQ_OK;
-    const int target = many_target(kRows, D);
-    return go(attend_many<D, kHalves, kWaves>, Cut{kRows, target, 4, B > 1 ? kFewMost : 0, INT32_MAX, T * G / kRows * a.Hkv < 2 * target, a.ws}, 64 * kWaves);
+    return go(attend_many<D>, Cut{kRows, target_of(kManyTarget, kRows, D), 4, few ? kFewMost : 0, INT32_MAX, true, a.ws}, 64 * kManyWaves);
 }
 
 int launch_kv8_attention(const Kv8Attend &a, hipStream_t s)
