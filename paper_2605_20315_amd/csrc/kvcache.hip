@@ -156,7 +156,8 @@ static __device__ Run run_of(const Kv8Seqs &s, int idx, int lane)
     return r;
 }
 
-// One (page, head) of keys or values by NW waves: the new tokens' largest magnitude, the scale, their codes, and the codes of
+// One (page, head) of keys or values by NW waves, in one pass over the new tokens where registers hold them (kKeep loads a
+// thread), in two otherwise: their largest magnitude, the scale, their codes, and the codes of
 // the tokens that were there before where the scale has grown.
 template <int D, int NW>
 static __device__ void store_unit(const Kv8Append &a, const Run &r, bool key, int head, int tid, uint32_t *part)
@@ -269,6 +270,9 @@ static __device__ void rotate_queries(const Kv8Append &a, int t, int h0, int lan
     }
 }
 
+// One launch for keys, values and queries.  Bound by HBM for prompts (8111 tokens of 32 query and 8 key heads of 128: 187 MB in
+// 45.5 us = 4.1 TB/s, a large copy reaches 4.8), by three dependent trips to memory (lengths, page number, codes' scale) for
+// single tokens: 200 of them 7.1 us.
 // Workgroups below `stores` take (page, head) units of keys and values, the others four waves of queries each.
 template <int D, int NW>
 __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8Append a, int stores, int units)
@@ -297,8 +301,10 @@ int launch_kv8_append(const Kv8Append &a, hipStream_t s)
     // pages touched: at most one for each new token, and n / P + 2 for a sequence of n
     const int64_t T = a.s.T, runs = std::min<int64_t>(T, (T >> a.s.page_shift) + 2 * (int64_t)a.s.B);
     const int64_t units = runs * 2 * a.Hkv;
-    // a few tokens a sequence are one or two loads of a wave; a page of them is four waves' work
-    const bool few = T <= 4 * (int64_t)a.s.B;
+    // One wave a unit for a few tokens a sequence, and for pages of which it can keep all in registers (8 loads of 512 elements:
+    // a mixed batch with pages of 16 x 64 takes 14.5 us so, 22.5 with four waves); else four waves share a unit (pages of
+    // 64 x 128, 8111 tokens: 45.5 us, 58.9 with one wave, which would read them twice).
+    const bool few = T <= 4 * (int64_t)a.s.B || (a.D << a.s.page_shift) <= 4096;
     const int64_t stores = few ? (units + 3) / 4 : units;
     const int heads = 4 * 512 / a.D;
     const int64_t queries = (T * ((a.Hq + heads - 1) / heads) + 3) / 4;
