@@ -26,7 +26,7 @@ constexpr float kNone = -__builtin_inff();
 // at most `most` rows
 struct Cut {
     int rows, target, least, above, most;
-    bool split;
+    bool split, fit;
     float *ws;
 };
 
@@ -79,32 +79,43 @@ struct PlanLds {
     Item found;
 };
 
-// tokens per chunk, in tiles, that make the call about c.target items
-template <int NT>
-static __device__ int chunk_tiles(const Kv8Attend &a, const Cut &c, PlanLds &lds, int tid)
-{
-    if (!c.split) return INT32_MAX;
-    int64_t work = 0;
-    if (a.s.B == 1) {
-        const Extent e = extent_of(a, c, span_of(a.s, 0));
-        work = (int64_t)e.row_tiles * e.tiles;
-    } else {
-        for (int b = tid; b < a.s.B; b += NT) {
-            const Extent e = extent_of(a, c, span_of(a.s, b));
-            work += (int64_t)e.row_tiles * e.tiles;
-        }
-        work = block_sum<NT>(work, lds.sums, tid);
-    }
-    const int64_t per = (work * a.Hkv + c.target - 1) / c.target;
-    return (int)min(max(per, (int64_t)c.least), (int64_t)INT32_MAX);
-}
-
 static __device__ __forceinline__ void cut_sequence(const Kv8Attend &a, const Extent &e, int per, int &chunks, int &items, int &slots)
 {
     // (a sequence whose queries see nothing still writes zeros; a last quarter of a chunk is worth one)
     chunks = e.row_tiles == 0 ? 0 : max((int)(((int64_t)e.tiles + (per == INT32_MAX ? 0 : (int64_t)per * 3 / 4)) / per), 1);
     items = e.row_tiles * chunks * a.Hkv;
     slots = chunks > 1 ? items : 0;
+}
+
+// sum over the sequences of what `of` makes of their extents
+template <int NT, class F>
+static __device__ __forceinline__ int64_t sum_of(const Kv8Attend &a, const Cut &c, PlanLds &lds, int tid, F &&of)
+{
+    if (a.s.B == 1) return of(extent_of(a, c, span_of(a.s, 0)));
+    int64_t sum = 0;
+    for (int b = tid; b < a.s.B; b += NT) sum += of(extent_of(a, c, span_of(a.s, b)));
+    return block_sum<NT>(sum, lds.sums, tid);
+}
+
+// Tokens per chunk, in tiles, that make the call about c.target items; no more than that where c.fit: one workgroup too many
+// is a second round of all (39 sequences in 530 items for 512 places 325 us, in fewer and longer ones 250).
+template <int NT>
+static __device__ int chunk_tiles(const Kv8Attend &a, const Cut &c, PlanLds &lds, int tid)
+{
+    if (!c.split) return INT32_MAX;
+    const int64_t work = sum_of<NT>(a, c, lds, tid, [](const Extent &e) { return (int64_t)e.row_tiles * e.tiles; });
+    int per = (int)min(max((work * a.Hkv + c.target - 1) / c.target, (int64_t)c.least), (int64_t)1 << 28);
+    if (c.fit)
+        for (int i = 0; i < 8; ++i) {
+            const int64_t items = sum_of<NT>(a, c, lds, tid, [&](const Extent &e) {
+                int chunks, n, slots;
+                cut_sequence(a, e, per, chunks, n, slots);
+                return (int64_t)n;
+            });
+            if (items <= c.target) break;
+            per += per / 8 + 1;
+        }
+    return per;
 }
 
 // The item `idx`; every thread of the workgroup calls it.  Workgroup 0 also writes down the sequences' parts.
@@ -137,12 +148,12 @@ static __device__ Item item_of(const Kv8Attend &a, const Cut &c, int idx, PlanLd
         const int first = ib + item_sum - items, first_slot = sb + slot_sum - slots;
         if (c.split && blockIdx.x == 0 && b < a.s.B) reinterpret_cast<Parts *>(c.ws)[b] = Parts{chunks, first_slot, e.row_tiles};
         if (idx >= first && idx < first + items) {
-            // head fastest: with eight key heads the workgroups of one head share an XCD and its L2; then the chunk; the
-            // tiles of rows from the last, which sees the most, to the first
-            const int local = idx - first, rest = local / a.Hkv, chunk = rest % chunks;
+            // head fastest: with eight key heads the workgroups of one head share an XCD and its L2; then the tiles of rows that
+            // read the same tokens, from the last, which sees the most, to the first
+            const int local = idx - first, rest = local / a.Hkv, chunk = rest / e.row_tiles;
             // the chunks' shares of the tiles, even to within one
             const int t0 = (int)((int64_t)e.tiles * chunk / chunks), t1 = (int)((int64_t)e.tiles * (chunk + 1) / chunks);
-            lds.found = Item{true, sp, b, e.row_tiles - 1 - rest / chunks, local - rest * a.Hkv, chunks, e.lo + t0 * kTile,
+            lds.found = Item{true, sp, b, e.row_tiles - 1 - rest % e.row_tiles, local - rest * a.Hkv, chunks, e.lo + t0 * kTile,
                              (int)min((int64_t)sp.len, (int64_t)e.lo + (int64_t)t1 * kTile), first_slot + local};
         }
         __syncthreads();
@@ -391,6 +402,13 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
         look_up(t0);
         const int count = min(32, (hi - t0 + kStride - 1) / kStride);
         Tokens x[2];
+        if constexpr (D == 256) {  // two sets of registers would leave one wave a SIMD (146 sequences of 200 tokens 77 us, 45 so)
+            for (int i = 0; i < count; ++i) {
+                load(t0 + i * kStride, i, x[0]);
+                compute(t0 + i * kStride, i, x[0]);
+            }
+            continue;
+        }
         load(t0, 0, x[0]);
         for (int i = 0; i < count; i += 2) {
             if (i + 1 < count) load(t0 + (i + 1) * kStride, i + 1, x[1]);
@@ -795,8 +813,8 @@ __global__ __launch_bounds__(256) void attend_join(Kv8Attend a, Cut c)
     if (t < sp.q0 || t >= sp.q0 + sp.n) return;
     const int G = a.Hq / a.Hkv, h = ROWS ? min(h0 + part, a.Hq - 1) : h0;
     const int kv = h / G, row = (t - sp.q0) * G + h - kv * G, tile = row / c.rows, r = row - tile * c.rows;
-    const int first = parts.slot + (parts.row_tiles - 1 - tile) * parts.chunks * a.Hkv + kv;
-    auto stats = [&](int i) { return slot_at(c, D, first + i * a.Hkv) + c.rows * D + r; };
+    const int first = parts.slot + (parts.row_tiles - 1 - tile) * a.Hkv + kv, next = parts.row_tiles * a.Hkv;
+    auto stats = [&](int i) { return slot_at(c, D, first + i * next) + c.rows * D + r; };
     float top = kNone, total = 0.0f;
     f32x4 o{0, 0, 0, 0};
     if constexpr (ROWS) {
@@ -813,7 +831,7 @@ __global__ __launch_bounds__(256) void attend_join(Kv8Attend a, Cut c)
 #pragma unroll 4
     for (int i = ROWS ? 0 : part; i < parts.chunks; i += ROWS ? 1 : kParts) {
         const float *const s = stats(i);
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(slot_at(c, D, first + i * a.Hkv) + r * D + 4 * col);
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(slot_at(c, D, first + i * next) + r * D + 4 * col);
         const float l = s[c.rows], w = weight_of(s[0], l, top);
         total += w * l;
         o += w * x;
@@ -838,7 +856,9 @@ constexpr int64_t kWorkspace = (int64_t)64 << 20;
 // Items aimed at: as many workgroups as the GPU holds at a time (attend_few, which is bound by memory, half as many more: a batch
 // of uneven lengths takes 124 us so, 136 with one round; two long sequences 92 and 89), of which those of sequences that are cut
 // are less than twice as many, and the workspace has to have slots for them.
-constexpr int kFewTarget = 768, kManyTarget = 512;
+constexpr int kFewTarget = 768;
+// workgroups of attend_many that a compute unit holds, by registers and LDS: three, two and one
+static int many_target(int D) { return 256 * (D == 64 ? 3 : D == 128 ? 2 : 1); }
 static int target_of(int most, int rows, int D) { return (int)std::min<int64_t>((kWorkspace - kPartsBytes) / ((int64_t)rows * (D + 2) * 4) / 2, most); }
 
 int64_t kv8_attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D)
@@ -853,9 +873,11 @@ static int launch_attention(const Kv8Attend &a, hipStream_t s)
     constexpr int kRows = 32 * kManyWaves;
     const int64_t G = a.Hq / a.Hkv, T = a.s.T, B = a.s.B;
     const bool ws = a.ws && a.ws_bytes >= kWorkspace && B <= kPartsMost;
-    // If every sequence has a token, none has more than T - B + 1 of them.  (Where some have none, one may have more: attend_few
-    // is then slower than it need be, and as right.)  Up to kAllMany sequences attend_many takes all if it takes any.
-    const bool many = (T - B + 1) * G > kFewMost, few = !many || B > kAllMany;
+    // If every sequence has a token, none has more than T - B + 1 of them, and where there are few tokens a sequence (a decode
+    // batch, drafted tokens among it) a second kernel that finds nothing to do costs more than a longer prompt loses in
+    // attend_few.  (Every split of the work is right: it is only slower than it need be.)  Up to kAllMany sequences attend_many takes
+    // all if it takes any.
+    const bool many = T > 4 * B && (T - B + 1) * G > kFewMost, few = !many || B > kAllMany;
     auto go = [&](auto kernel, Cut cut, int threads) {
         // An item for each tile of rows and key head; where sequences are cut, as many more as the target has, or as their
         // longest possible history has chunks
@@ -870,9 +892,9 @@ static int launch_attention(const Kv8Attend &a, hipStream_t s)
         return enqueue(attend_join<D, false>, dim3((unsigned)(T * a.Hq)), dim3(256), 0, s, a, cut);
     };
     if (few)
-        if (int rc = go(attend_few<D>, Cut{kFewRows, target_of(kFewTarget, kFewRows, D), 2, 0, many ? kFewMost : INT32_MAX, true, a.ws}, kFewThreads)) return rc;
+        if (int rc = go(attend_few<D>, Cut{kFewRows, target_of(kFewTarget, kFewRows, D), 2, 0, many ? kFewMost : INT32_MAX, true, false, a.ws}, kFewThreads)) return rc;
     if (!many) return MQ_OK;
-    return go(attend_many<D>, Cut{kRows, target_of(kManyTarget, kRows, D), 4, few ? kFewMost : 0, INT32_MAX, true, a.ws}, 64 * kManyWaves);
+    return go(attend_many<D>, Cut{kRows, target_of(many_target(D), kRows, D), 4, few ? kFewMost : 0, INT32_MAX, true, true, a.ws}, 64 * kManyWaves);
 }
 
 int launch_kv8_attention(const Kv8Attend &a, hipStream_t s)
