@@ -2,8 +2,8 @@
 //
 // Queries of one sequence and one key head are rows: row r is head r % G of the group, token r / G, so the G query heads that
 // share a key head read its cache once.  One pass over the keys with a running maximum and sum.  Two kernels:
-//   attend_few    tiles of 16 rows, no LDS in its loop: bound by reading the cache
-//   attend_many   tiles of 256 rows (128 of 256 elements), the cache's tiles expanded once per workgroup into LDS: bound by the matrix pipe
+//   attend_few    tiles of 16 or 32 rows, no LDS in its loop: bound by reading the cache
+//   attend_many   tiles of 128 rows, the cache's tiles expanded once per workgroup into LDS: bound by the matrix and vector pipes
 // Both compute the transposes S^T = K Q^T and O^T = V^T P^T: a lane then holds, of one row, the very scores that it has to
 // supply as its slots of P^T in the second product, so the probabilities never move between lanes.  MFMA slots are matched
 // to tokens and head elements by whatever order the loads have; both operands of a product only have to agree.
@@ -28,6 +28,7 @@ struct Cut {
     int rows, target, least, above, most;
     bool split, fit;
     float *ws;
+    int slots;  // that the workspace holds
 };
 
 struct Item {
@@ -153,8 +154,10 @@ static __device__ Item item_of(const Kv8Attend &a, const Cut &c, int idx, PlanLd
             const int local = idx - first, rest = local / a.Hkv, chunk = rest / e.row_tiles;
             // the chunks' shares of the tiles, even to within one
             const int t0 = (int)((int64_t)e.tiles * chunk / chunks), t1 = (int)((int64_t)e.tiles * (chunk + 1) / chunks);
-            lds.found = Item{true, sp, b, e.row_tiles - 1 - rest % e.row_tiles, local - rest * a.Hkv, chunks, e.lo + t0 * kTile,
-                             (int)min((int64_t)sp.len, (int64_t)e.lo + (int64_t)t1 * kTile), first_slot + local};
+            // (ranges of tokens that overlap, which cu_q must not have, could ask for more slots than there are)
+            const int slot = first_slot + local;
+            lds.found = Item{chunks == 1 || (unsigned)slot < (unsigned)c.slots, sp, b, e.row_tiles - 1 - rest % e.row_tiles, local - rest * a.Hkv, chunks, e.lo + t0 * kTile,
+                             (int)min((int64_t)sp.len, (int64_t)e.lo + (int64_t)t1 * kTile), slot};
         }
         __syncthreads();
         if (idx < items_before && !(c.split && blockIdx.x == 0)) break;
@@ -233,38 +236,43 @@ constexpr int kFewWaves = 4, kFewThreads = 64 * kFewWaves;
 // One item by four waves, each with every fourth group of 32 tokens.  Lane (c = lane % 16, g = lane / 16) of a wave reads, of
 // the keys, bytes g * D / 4 .. of token c of each half; of the values, bytes c * D / 16 .. of tokens 4g .. 4g + 3 of each half:
 // whole rows of the page in one instruction, operands without any exchange between lanes.
-template <int D>
+// Measured, heads of 128, 32 on 8: 64 tokens after 100 to 8000 each, 600 MB, 118 us = 5.1 TB/s (a large copy 4.8), all of it
+// waiting for memory (vector instructions 15 % of the time); two sequences of 105000, 435 MB, 86 us.
+// RT tiles of 16 rows: what a wave has expanded serves all of them (109 sequences of 23000, 52 rows each: 365 us with one, 233 with two).
+template <int D, int RT>
 __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
 {
     constexpr int KW = D / 16;  // dwords of a key row's quarter, and MFMA steps over the head elements per 2 of them
     constexpr int VW = D / 64;  // dwords of a value row's sixteenth
     __shared__ PlanLds plan;
-    __shared__ float stat[kFewWaves][2][16];
-    __shared__ float sums[kFewWaves][16][D + 4];
+    constexpr int kRows = 16 * RT;
+    __shared__ float stat[kFewWaves][2][kRows];
+    __shared__ float sums[kFewWaves][kRows][D + 4];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g = lane >> 4;
     const Item it = item_of<kFewThreads>(a, c, blockIdx.x, plan, tid);
     if (!it.found) return;
-    const int G = a.Hq / a.Hkv, rows = it.sp.n * G, r = it.tile * kFewRows + col;
-    const int row = min(r, rows - 1), token = row / G, head = it.head * G + row - token * G;
-    const int pos = it.sp.start + token;  // the last place that this row sees
-    const int first = a.window > 0 ? pos - a.window + 1 : 0;
-    // what every row of the tile, and what any of them sees
-    const int last_token = (min((it.tile + 1) * kFewRows, rows) - 1) / G;
-    const int pos_lo = it.sp.start + it.tile * kFewRows / G, pos_hi = it.sp.start + last_token;
-    const int hi = min(it.hi, pos_hi + 1), lo = max(it.lo, a.window > 0 ? pos_lo - a.window + 1 : 0);
-    const int all_lo = a.window > 0 ? pos_hi - a.window + 1 : 0, all_hi = min(it.hi, pos_lo + 1);
-
-    u32x4 q[D / 32];
-    {
+    const int G = a.Hq / a.Hkv, rows = it.sp.n * G, row0 = it.tile * kRows;
+    int pos[RT], first[RT];  // the places that the lane's row of each tile sees: from first to pos
+    u32x4 q[RT][D / 32];
+    f32x4 acc[RT][D / 16];
+    float mb[RT], l[RT];  // the running maximum times the scale, and the lane's share of the sum
+#pragma unroll
+    for (int f = 0; f < RT; ++f) {
+        const int row = min(row0 + 16 * f + col, rows - 1), token = row / G, head = it.head * G + row - token * G;
+        pos[f] = it.sp.start + token;
+        first[f] = a.window > 0 ? pos[f] - a.window + 1 : 0;
         const uint16_t *const p = a.q + (int64_t)(it.sp.q0 + token) * a.ldq + (int64_t)head * D + g * (D / 4);
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) q[s] = *reinterpret_cast<const u32x4 *>(p + 8 * s);
-    }
-    f32x4 acc[D / 16];
+        for (int s = 0; s < D / 32; ++s) q[f][s] = *reinterpret_cast<const u32x4 *>(p + 8 * s);
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d) acc[d] = f32x4{0, 0, 0, 0};
-    float mb = kNone, l = 0.0f;  // the running maximum times the scale
-    bool marked = false;         // whether the wave's part of `sums` holds NaN for what rows have seen
+        for (int d = 0; d < D / 16; ++d) acc[f][d] = f32x4{0, 0, 0, 0};
+        mb[f] = kNone, l[f] = 0.0f;
+    }
+    // what every row of the item, and what any of them sees
+    const int pos_lo = it.sp.start + row0 / G, pos_hi = it.sp.start + (min(row0 + kRows, rows) - 1) / G;
+    const int hi = min(it.hi, pos_hi + 1), lo = max(it.lo, a.window > 0 ? pos_lo - a.window + 1 : 0);
+    const int all_lo = a.window > 0 ? pos_hi - a.window + 1 : 0, all_hi = min(it.hi, pos_lo + 1);
+    bool marked = false;  // whether the wave's part of `sums` holds NaN for what rows have seen
 
     const int P = 1 << a.s.page_shift;
     const int64_t unit = (int64_t)P * D;
@@ -317,29 +325,38 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
                                   __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), 2 * i + 1))};
         const float v_scale[2] = {__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), 2 * i)),
                                   __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), 2 * i + 1))};
-        f32x4 s[2];
+        f32x4 s[RT][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            s[h] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int w = 0; w < D / 32; ++w)
-                s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(expand8(x.k[h][w / 2][2 * (w % 2)], x.k[h][w / 2][2 * (w % 2) + 1], k_scale[h]),
-                                                               __builtin_bit_cast(bf16x8, q[w]), s[h], 0, 0, 0);
+            for (int f = 0; f < RT; ++f) s[f][h] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < D / 32; ++w) {
+                const bf16x8 k = expand8(x.k[h][w / 2][2 * (w % 2)], x.k[h][w / 2][2 * (w % 2) + 1], k_scale[h]);
+#pragma unroll
+                for (int f = 0; f < RT; ++f)
+                    s[f][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(bf16x8, q[f][w]), s[f][h], 0, 0, 0);
+            }
         }
         const bool edge = t < all_lo || t + 32 > all_hi || id0 < 0 || id1 < 0;
         if (edge) {
-            uint32_t seen = 0;
+            uint32_t seen[RT];
             bool odd = false;
+#pragma unroll
+            for (int f = 0; f < RT; ++f) seen[f] = 0;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int at = t + 16 * h + 4 * g + j;
                     const bool there = at >= lo && at < hi && (h ? id1 : id0) >= 0;
-                    if (there && at >= first && at <= pos)
-                        seen |= 1u << (4 * h + j);
-                    else
-                        s[h][j] = kNone;
+#pragma unroll
+                    for (int f = 0; f < RT; ++f) {
+                        if (there && at >= first[f] && at <= pos[f])
+                            seen[f] |= 1u << (4 * h + j);
+                        else
+                            s[f][h][j] = kNone;
+                    }
                     // places that no row sees may hold anything, NaN codes among it: a zero probability would not hide those
 #pragma unroll
                     for (int w = 0; w < VW; ++w) {
@@ -350,11 +367,11 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
             if (__any(odd)) {
                 // NaN values that some rows see and others do not: out of the product, and kept for the rows that see them
                 if (!marked)
-                    for (int i = lane; i < 16 * (D + 4); i += 64) (&sums[wave][0][0])[i] = 0.0f;
+                    for (int i = lane; i < kRows * (D + 4); i += 64) (&sums[wave][0][0])[i] = 0.0f;
                 marked = true;
 #pragma unroll 1
-                for (int r = 0; r < 16; ++r) {
-                    const uint32_t sees = (uint32_t)__shfl((int)seen, r + 16 * g);
+                for (int r = 0; r < kRows; ++r) {
+                    const uint32_t own = RT == 1 || r < 16 ? seen[0] : seen[RT - 1], sees = (uint32_t)__shfl((int)own, (r & 15) + 16 * g);
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -370,21 +387,34 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
                     for (int w = 0; w < VW; ++w) x.v[j][w] &= ~(nan_bytes(x.v[j][w]) * 0xffu);
             }
         }
-        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale;
-        if (__any(top > mb)) {
-            const float next = fmaxf(mb, top), by = next == kNone ? 1.0f : __builtin_amdgcn_exp2f(mb - next);
-            mb = next;
-            l *= by;
+        float top[RT];
+        bool grown = false;
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d) acc[d] *= by;
+        for (int f = 0; f < RT; ++f) {
+            const f32x4 u = s[f][0], v = s[f][1];
+            top[f] = fmaxf(fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3])), fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
+            top[f] = fmaxf(top[f], __shfl_xor(top[f], 16));
+            top[f] = fmaxf(top[f], __shfl_xor(top[f], 32)) * a.scale;
+            grown |= top[f] > mb[f];
         }
-        const float base = mb == kNone ? 0.0f : mb;
-        float p[8];
+        if (__any(grown))
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[j / 4][j % 4], a.scale, -base)), l += p[j];
-        const bf16x8 pb = four(pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7]));
+            for (int f = 0; f < RT; ++f) {
+                const float next = fmaxf(mb[f], top[f]), by = next == kNone ? 1.0f : __builtin_amdgcn_exp2f(mb[f] - next);
+                mb[f] = next;
+                l[f] *= by;
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) acc[f][d] *= by;
+            }
+        bf16x8 pb[RT];
+#pragma unroll
+        for (int f = 0; f < RT; ++f) {
+            const float base = mb[f] == kNone ? 0.0f : mb[f];
+            float p[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[f][j / 4][j % 4], a.scale, -base)), l[f] += p[j];
+            pb[f] = four(pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7]));
+        }
 #pragma unroll
         for (int w = 0; w < VW; ++w) {
             uint32_t v[8];
@@ -393,7 +423,9 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
             bf16x8 turned[4];
             turn8(v, v_scale, turned);
 #pragma unroll
-            for (int d = 0; d < 4; ++d) acc[4 * w + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(turned[d], pb, acc[4 * w + d], 0, 0, 0);
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int f = 0; f < RT; ++f) acc[f][4 * w + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(turned[d], pb[f], acc[f][4 * w + d], 0, 0, 0);
         }
     };
 
@@ -402,7 +434,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
         look_up(t0);
         const int count = min(32, (hi - t0 + kStride - 1) / kStride);
         Tokens x[2];
-        if constexpr (D == 256) {  // two sets of registers would leave one wave a SIMD (146 sequences of 200 tokens 77 us, 45 so)
+        if constexpr (D == 256 || RT > 1) {  // two sets of registers would leave one wave a SIMD (146 sequences of 200 tokens 77 us, 45 so)
             for (int i = 0; i < count; ++i) {
                 load(t0 + i * kStride, i, x[0]);
                 compute(t0 + i * kStride, i, x[0]);
@@ -419,45 +451,55 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
     }
 
     // the four waves' results: lane (col, g) holds, of row col, the elements (4g + i) * D / 16 + d for i < 4, d < D / 16
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (g == 0) stat[wave][0][col] = mb, stat[wave][1][col] = l;
+#pragma unroll
+    for (int f = 0; f < RT; ++f) {
+        l[f] += __shfl_xor(l[f], 16);
+        l[f] += __shfl_xor(l[f], 32);
+        if (g == 0) stat[wave][0][16 * f + col] = mb[f], stat[wave][1][16 * f + col] = l[f];
+    }
     __syncthreads();
-    float top = kNone;
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, stat[w][0][col]);
-    const float by = weight_of(mb, l, top);
+    for (int f = 0; f < RT; ++f) {
+        const int r = 16 * f + col;
+        float top = kNone;
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d)
+        for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, stat[w][0][r]);
+        const float by = weight_of(mb[f], l[f], top);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float &to = sums[wave][col][(4 * g + i) * (D / 16) + d];
-            to = marked ? fmaf(acc[d][i], by, to) : acc[d][i] * by;
-        }
+        for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float &to = sums[wave][r][(4 * g + i) * (D / 16) + d];
+                to = marked ? fmaf(acc[f][d][i], by, to) : acc[f][d][i] * by;
+            }
+    }
     __syncthreads();
     // 16 threads a row, D / 16 elements each
-    const int orow = tid >> 4, e0 = (tid & 15) * (D / 16), out = it.tile * kFewRows + orow;
-    if (out >= rows) return;
-    float best = kNone, total = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) best = fmaxf(best, stat[w][0][orow]);
+    for (int f = 0; f < RT; ++f) {
+        const int r = 16 * f + (tid >> 4), e0 = (tid & 15) * (D / 16), row = row0 + r;
+        if (row >= rows) return;
+        float best = kNone, total = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) total += stat[w][1][orow] * weight_of(stat[w][0][orow], stat[w][1][orow], best);
-    float o[D / 16];
+        for (int w = 0; w < kFewWaves; ++w) best = fmaxf(best, stat[w][0][r]);
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) o[e] = ((sums[0][orow][e0 + e] + sums[1][orow][e0 + e]) + sums[2][orow][e0 + e]) + sums[3][orow][e0 + e];
-    if (it.chunks > 1) {
-        float *const p = slot_at(c, D, it.slot);
+        for (int w = 0; w < kFewWaves; ++w) total += stat[w][1][r] * weight_of(stat[w][0][r], stat[w][1][r], best);
+        float o[D / 16];
 #pragma unroll
-        for (int e = 0; e < D / 16; e += 4) *reinterpret_cast<f32x4 *>(p + orow * D + e0 + e) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
-        if ((tid & 15) == 0) p[kFewRows * D + orow] = best, p[kFewRows * D + kFewRows + orow] = total;
-        return;
+        for (int e = 0; e < D / 16; ++e) o[e] = ((sums[0][r][e0 + e] + sums[1][r][e0 + e]) + sums[2][r][e0 + e]) + sums[3][r][e0 + e];
+        if (it.chunks > 1) {
+            float *const p = slot_at(c, D, it.slot);
+#pragma unroll
+            for (int e = 0; e < D / 16; e += 4) *reinterpret_cast<f32x4 *>(p + r * D + e0 + e) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
+            if ((tid & 15) == 0) p[kRows * D + r] = best, p[kRows * D + kRows + r] = total;
+            continue;
+        }
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        const int token = row / G;
+        uint32_t *const y = reinterpret_cast<uint32_t *>(a.y + (int64_t)(it.sp.q0 + token) * a.ldy + (int64_t)(it.head * G + row - token * G) * D + e0);
+#pragma unroll
+        for (int e = 0; e < D / 16; e += 2) y[e / 2] = pack2(o[e] * inv, o[e + 1] * inv);
     }
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    const int t = out / G;
-    uint32_t *const y = reinterpret_cast<uint32_t *>(a.y + (int64_t)(it.sp.q0 + t) * a.ldy + (int64_t)(it.head * G + out - t * G) * D + e0);
-#pragma unroll
-    for (int e = 0; e < D / 16; e += 2) y[e / 2] = pack2(o[e] * inv, o[e + 1] * inv);
 }
 
 // ------------------------------------------------------------------------------------------------ many rows
@@ -808,7 +850,7 @@ __global__ __launch_bounds__(256) void attend_join(Kv8Attend a, Cut c)
     }
     if (b >= a.s.B) return;
     const Parts parts = reinterpret_cast<const Parts *>(c.ws)[b];
-    if (parts.chunks < 2) return;
+    if (parts.chunks < 2 || parts.slot < 0 || (int64_t)parts.slot + (int64_t)parts.chunks * parts.row_tiles * a.Hkv > c.slots) return;
     const Span sp = span_of(a.s, b);
     if (t < sp.q0 || t >= sp.q0 + sp.n) return;
     const int G = a.Hq / a.Hkv, h = ROWS ? min(h0 + part, a.Hq - 1) : h0;
@@ -859,7 +901,8 @@ constexpr int64_t kWorkspace = (int64_t)64 << 20;
 constexpr int kFewTarget = 768;
 // workgroups of attend_many that a compute unit holds, by registers and LDS: three, two and one
 static int many_target(int D) { return 256 * (D == 64 ? 3 : D == 128 ? 2 : 1); }
-static int target_of(int most, int rows, int D) { return (int)std::min<int64_t>((kWorkspace - kPartsBytes) / ((int64_t)rows * (D + 2) * 4) / 2, most); }
+static int slots_of(int rows, int D) { return (int)((kWorkspace - kPartsBytes) / ((int64_t)rows * (D + 2) * 4)); }
+static int target_of(int most, int rows, int D) { return std::min(slots_of(rows, D) / 2, most); }
 
 int64_t kv8_attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D)
 {
@@ -891,10 +934,17 @@ static int launch_attention(const Kv8Attend &a, hipStream_t s)
         if (T * a.Hq >= 2048) return enqueue(attend_join<D, true>, dim3((unsigned)(T * ((a.Hq + kPer - 1) / kPer))), dim3(256), 0, s, a, cut);
         return enqueue(attend_join<D, false>, dim3((unsigned)(T * a.Hq)), dim3(256), 0, s, a, cut);
     };
-    if (few)
-        if (int rc = go(attend_few<D>, Cut{kFewRows, target_of(kFewTarget, kFewRows, D), 2, 0, many ? kFewMost : INT32_MAX, true, false, a.ws}, kFewThreads)) return rc;
+    if (few) {
+        auto cut = [&](int rows) { return Cut{rows, target_of(kFewTarget, rows, D), 2, 0, many ? kFewMost : INT32_MAX, true, false, a.ws, slots_of(rows, D)}; };
+        int rc;
+        if constexpr (D <= 128)  // (heads of 256 have no registers for two tiles)
+            rc = T * G > B * kFewRows ? go(attend_few<D, 2>, cut(2 * kFewRows), kFewThreads) : go(attend_few<D, 1>, cut(kFewRows), kFewThreads);
+        else
+            rc = go(attend_few<D, 1>, cut(kFewRows), kFewThreads);
+        if (rc) return rc;
+    }
     if (!many) return MQ_OK;
-    return go(attend_many<D>, Cut{kRows, target_of(many_target(D), kRows, D), 4, few ? kFewMost : 0, INT32_MAX, true, true, a.ws}, 64 * kManyWaves);
+    return go(attend_many<D>, Cut{kRows, target_of(many_target(D), kRows, D), 4, few ? kFewMost : 0, INT32_MAX, true, true, a.ws, slots_of(kRows, D)}, 64 * kManyWaves);
 }
 
 int launch_kv8_attention(const Kv8Attend &a, hipStream_t s)

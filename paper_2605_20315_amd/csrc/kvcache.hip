@@ -164,6 +164,7 @@ static __device__ void store_unit(const Kv8Append &a, const Run &r, bool key, in
 {
     constexpr int kSubs = D / 8, kRows = 64 * NW / kSubs, kKeep = 8;
     const int lane = tid & 63, sub = tid % kSubs, row = tid / kSubs, P = 1 << a.s.page_shift;
+    if ((unsigned)r.page >= (unsigned)a.s.width) return;
     const int id = a.s.page_table[r.b * a.s.pt_ld + r.page];
     if ((unsigned)id >= (uint64_t)a.s.pages) return;  // (the same for every wave of the unit)
     const int first = r.page << a.s.page_shift, s0 = max(r.start - first, 0), s1 = min(r.end - first, P);

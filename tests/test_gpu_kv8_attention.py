@@ -243,3 +243,36 @@ def test_other_stream_and_graph_replays():
         torch.cuda.synchronize()
         got = out.clone()
         assert torch.equal(got, mq.kv8_attention(*args, p.scale, 0, None, ws))
+
+
+@pytest.mark.parametrize("window", [0, 1, 5, 17, 64, 200])
+@pytest.mark.parametrize("Hq,Hkv,D,P", [(4, 2, 64, 16), (8, 1, 128, 64), (24, 2, 128, 16), (20, 1, 64, 128), (6, 1, 256, 32), (32, 4, 256, 16)])
+def test_a_batch_of_drafted_tokens(Hq, Hkv, D, P, window):
+    """One to four tokens a sequence: rows of one, two and more tiles, masks that end inside them, cut and whole histories."""
+    Problem(window + D, [1, 4, 2, 3] * 3, [0, 1, 14, 29, 31, 62, 65, 127, 190, 333, 1500, 700], Hq, Hkv, D, P, window).check()
+
+
+@pytest.mark.parametrize("Hq,D", [(2, 64), (5, 128), (12, 128), (9, 256)])
+def test_a_nan_value_among_drafted_tokens(Hq, D):
+    for window in (0, 3):
+        p = Problem(D + Hq, [4, 1, 3, 4, 4], [30, 0, 61, 300, 15], Hq, 1, D, 16, window)
+        for b, (n, start) in enumerate(zip([4, 1, 3, 4, 4], [30, 0, 61, 300, 15])):
+            for place, d in ((start + n - 1, 1), (start + n // 2, D - 1), (start, 6)):
+                p.vc[p.pt[b, place // 16], 0, place % 16, d] = 0x7F if place % 2 else 0xFF
+        assert np.isnan(p.reference()[0]).any()
+        with np.errstate(invalid="ignore"):
+            p.check()
+
+
+def test_drafted_tokens_that_see_nothing_and_pages_that_are_none():
+    p = Problem(20, [4, 3, 2, 4, 1], [0, 60, 9, 40, 5], 8, 1, 128, 16)
+    p.lens[0] = 2             # two of four lie before the first place
+    p.lens[2] = 0
+    p.pt[1, 1], p.pt[3, 2] = -1, 10 ** 6
+    p.pt[4, 0] = len(p.kc)
+    p.check()
+
+
+def test_one_long_prompt_among_single_tokens():
+    # few tokens a sequence on the whole: the prompt goes the same way as the others
+    Problem(21, [1] * 60 + [170] + [1] * 20, [int(n) for n in np.random.default_rng(1).integers(0, 90, 81)], 4, 2, 64, 32).check()
