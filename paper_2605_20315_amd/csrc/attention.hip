@@ -521,7 +521,8 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
 template <int D>
 __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut c)
 {
-    constexpr int NW = kManyWaves, NT = 64 * NW, kTasks = 4 * D, TN = (kTasks + NT - 1) / NT;  // a task: 32 bytes of codes
+    constexpr int NW = kManyWaves, NT = 64 * NW, TN = 4 * D / NT;  // tasks of a thread: 32 bytes of codes each
+    static_assert(TN * NT == 4 * D && (TN > 1 || NT == 2 * 2 * D), "every thread has the same tasks, or half of the waves those of keys");
     constexpr int kRows = 32 * NW;
     constexpr int kBlock16 = 1024 + 16;  // the padding spreads a key token's four writes over the banks
     constexpr int kHalf = 2 * (D / 16);  // blocks of a tile's keys, and of its values
@@ -561,43 +562,51 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
     const int P = 1 << a.s.page_shift;
     const int64_t unit = (int64_t)P * D;
     const int32_t *const table = a.s.page_table + it.b * a.s.pt_ld;
-    const int begin = group_lo & ~(kTile - 1), tiles = group_hi > begin ? (group_hi - begin + kTile - 1) / kTile : 0;
+    const int begin = group_lo & ~(kTile - 1), tiles = group_hi > begin && a.s.pages > 0 ? (group_hi - begin + kTile - 1) / kTile : 0;
 
-    // of a thread's tasks: keys (token, 32 elements) below 2 D, values (16 tokens s and half h, 4 elements) from there
-    auto is_key = [&](int n) { return tid + n * NT < 2 * D; };
-    auto page_of = [&](int i, int n) -> int {  // page of the task's 16 tokens in tile i, -1 if there is none
-        const int task = tid + n * NT, sub = is_key(n) ? task / (D / 32) / 16 + 2 : (task - 2 * D) / (D / 4) / 2;
-        const int at = begin + i * kTile + 16 * sub, page = at >> a.s.page_shift;
-        if (task >= kTasks || at < begin || at >= group_hi || page >= a.s.width) return -1;
-        const int id = table[page];
-        return (unsigned)id < (uint64_t)a.s.pages ? id : -1;
-    };
+    // A thread's tasks: first of keys (token, 32 elements), then of values (16 tokens and a half of them, 4 elements); with one
+    // task a thread the first waves take the keys.
+    auto is_key = [&](int n) { return TN > 1 ? n < TN / 2 : wave < NW / 2; };
+    auto task_of = [&](int n) { return TN > 1 ? tid + n % (TN / 2 ? TN / 2 : 1) * NT : tid % (NT / 2); };
+    auto key_token = [&](int n) { return task_of(n) / (D / 32); };
+    auto key_part = [&](int n) { return task_of(n) % (D / 32); };
+    auto group_of = [&](int n) { return task_of(n) / (D / 4); };  // 16 tokens s and half h, as 2 s + h
+    auto element_of = [&](int n) { return task_of(n) % (D / 4); };
+    auto value_token = [&](int n) { return 16 * (group_of(n) >> 1) + 4 * (group_of(n) & 1); };
+    auto place_of = [&](int i, int n) { return begin + i * kTile + (is_key(n) ? 32 + (key_token(n) & ~15) : 16 * (group_of(n) >> 1)); };
     struct Codes {
         uint32_t w[TN][8];
-        int e[TN];  // exponent byte, -1 where there is no page
+        int e[TN];      // the exponent byte
+        bool there[TN];  // whether there is a page (else these are page 0's, to be taken for nothing)
     };
+    // Page numbers are read an iteration before they are needed, and looked at only then; and no load is conditional: a comparison
+    // at once, or a branch around a load, would wait for everything that is on its way (a prompt of 8192 took 9 % longer).
+    // The index is clamped, as the place may lie beyond the history.
     int ids[TN];
     Codes x;
+    auto pages_of = [&](int i) {
+#pragma unroll
+        for (int n = 0; n < TN; ++n) ids[n] = table[min(max(place_of(i, n), 0) >> a.s.page_shift, a.s.width - 1)];
+    };
     auto load = [&](int i) {  // tile i, whose pages are in `ids`
+        int64_t u[TN];
 #pragma unroll
         for (int n = 0; n < TN; ++n) {
-            const int task = tid + n * NT;
-            x.e[n] = -1;
+            const int at = place_of(i, n);
+            x.there[n] = at >= begin && at < group_hi && (unsigned)ids[n] < (uint64_t)a.s.pages;
+            u[n] = (int64_t)(x.there[n] ? ids[n] : 0) * a.Hkv + it.head;
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x.w[n][j] = 0;
-            if (ids[n] < 0) continue;
-            const int64_t u = (int64_t)ids[n] * a.Hkv + it.head;
+        for (int n = 0; n < TN; ++n) {
             if (is_key(n)) {
-                const int tok = task / (D / 32), part = task % (D / 32);
-                x.e[n] = a.k_scales[u];
-                const u32x4 *const p = reinterpret_cast<const u32x4 *>(a.k_codes + u * unit + (int64_t)((begin + i * kTile + 32 + tok) & (P - 1)) * D + 32 * part);
+                x.e[n] = a.k_scales[u[n]];
+                const u32x4 *const p = reinterpret_cast<const u32x4 *>(a.k_codes + u[n] * unit + (int64_t)((begin + i * kTile + 32 + key_token(n)) & (P - 1)) * D + 32 * key_part(n));
                 const u32x4 y = p[0], z = p[1];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x.w[n][j] = y[j], x.w[n][4 + j] = z[j];
             } else {
-                const int group = (task - 2 * D) / (D / 4), el = (task - 2 * D) % (D / 4), tok = 16 * (group >> 1) + 4 * (group & 1);
-                x.e[n] = a.v_scales[u];
-                const uint8_t *const p = a.v_codes + u * unit + (int64_t)((begin + i * kTile + tok) & (P - 1)) * D + 4 * el;
+                x.e[n] = a.v_scales[u[n]];
+                const uint8_t *const p = a.v_codes + u[n] * unit + (int64_t)((begin + i * kTile + value_token(n)) & (P - 1)) * D + 4 * element_of(n);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x.w[n][j] = *reinterpret_cast<const uint32_t *>(p + ((j & 3) + 8 * (j >> 2)) * D);
             }
@@ -606,25 +615,22 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
     auto expand = [&](int i) {
 #pragma unroll
         for (int n = 0; n < TN; ++n) {
-            const int task = tid + n * NT;
-            if (task >= kTasks) continue;
             const float scale = exp2_of(min(max(x.e[n], 1), 254) - 127);
             if (is_key(n)) {
-                const int tok = task / (D / 32), part = task % (D / 32);
-                if (x.e[n] < 0) atomicOr(&flags[(i + tok / 32) & 3], 1 << ((tok / 16) ^ 2));
-                unsigned char *const to = keys[i & 1] + ((tok / 32) * (D / 16) + 2 * part) * kBlock16 + (tok & 31) * 16;
+                const int tok = key_token(n);
+                if (!x.there[n]) atomicOr(&flags[(i + tok / 32) & 3], 1 << ((tok / 16) ^ 2));
+                unsigned char *const to = keys[i & 1] + ((tok / 32) * (D / 16) + 2 * key_part(n)) * kBlock16 + (tok & 31) * 16;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     *reinterpret_cast<bf16x8 *>(to + (j / 2) * kBlock16 + (j & 1) * 512) = expand8(x.w[n][2 * j], x.w[n][2 * j + 1], scale);
             } else {
-                const int group = (task - 2 * D) / (D / 4), el = (task - 2 * D) % (D / 4), tok = 16 * (group >> 1) + 4 * (group & 1);
-                const int t = begin + i * kTile;
+                const int group = group_of(n), el = element_of(n), t = begin + i * kTile;
                 // places that no row sees may hold anything, NaN codes among it: a zero probability would not hide those
-                if (t < group_lo || t + kTile > group_hi)
+                if (t < group_lo || t + kTile > group_hi || !x.there[n])
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const int at = t + tok + (j & 3) + 8 * (j >> 2);
-                        x.w[n][j] = at >= group_lo && at < group_hi ? x.w[n][j] : 0u;
+                        const int at = t + value_token(n) + (j & 3) + 8 * (j >> 2);
+                        x.w[n][j] = x.there[n] && at >= group_lo && at < group_hi ? x.w[n][j] : 0u;
                     }
                 if (t < rows_lo || t + kTile > rows_hi) {  // some rows of the workgroup do not see all of it
                     uint32_t odd = 0;
@@ -743,10 +749,6 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
     if (tid < 4) flags[tid] = 0;
     for (int j = 0; j < D / 32; ++j) marks[j][tid] = 0;
     if (tiles > 0) {
-        auto pages_of = [&](int i) {
-#pragma unroll
-            for (int n = 0; n < TN; ++n) ids[n] = page_of(i, n);
-        };
         pages_of(-1);
         load(-1);
         pages_of(0);
