@@ -434,19 +434,28 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
         look_up(t0);
         const int count = min(32, (hi - t0 + kStride - 1) / kStride);
         Tokens x[2];
-        if constexpr (D == 256 || RT > 1) {  // two sets of registers would leave one wave a SIMD (146 sequences of 200 tokens 77 us, 45 so)
+        if constexpr (D * RT >= 256) {  // two sets of registers would leave one wave a SIMD (146 sequences of 200 tokens 77 us, 45 so)
             for (int i = 0; i < count; ++i) {
                 load(t0 + i * kStride, i, x[0]);
                 compute(t0 + i * kStride, i, x[0]);
             }
             continue;
         }
+        // (no load is conditional: where one may have been left out the compiler waits for all of them)
         load(t0, 0, x[0]);
-        for (int i = 0; i < count; i += 2) {
-            if (i + 1 < count) load(t0 + (i + 1) * kStride, i + 1, x[1]);
+        int i = 0;
+        for (; i + 2 < count; i += 2) {
+            load(t0 + (i + 1) * kStride, i + 1, x[1]);
             compute(t0 + i * kStride, i, x[0]);
-            if (i + 2 < count) load(t0 + (i + 2) * kStride, i + 2, x[0]);
-            if (i + 1 < count) compute(t0 + (i + 1) * kStride, i + 1, x[1]);
+            load(t0 + (i + 2) * kStride, i + 2, x[0]);
+            compute(t0 + (i + 1) * kStride, i + 1, x[1]);
+        }
+        if (i + 1 < count) {
+            load(t0 + (i + 1) * kStride, i + 1, x[1]);
+            compute(t0 + i * kStride, i, x[0]);
+            compute(t0 + (i + 1) * kStride, i + 1, x[1]);
+        } else {
+            compute(t0 + i * kStride, i, x[0]);
         }
     }
 
