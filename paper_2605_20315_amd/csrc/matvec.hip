@@ -223,6 +223,7 @@ __global__ __launch_bounds__(64 * NW) void matvec_kernel(MatvecArgs a)
         for (int u = 0; u < 4; ++u) {
             if (!more && i0 + u >= end) break;
             if (more || u < 3) load_x((u + 1) & 1, i0 + u + 1);
+            __builtin_amdgcn_sched_barrier(0);  // (the compiler would move the loads down to where they are needed)
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 const uint32_t sigma[2] = {__builtin_amdgcn_perm(0u, sb[s][u], low) << 7, __builtin_amdgcn_perm(0u, sb[s][u], high) << 7};
@@ -235,6 +236,7 @@ __global__ __launch_bounds__(64 * NW) void matvec_kernel(MatvecArgs a)
                 }
             }
             // (two iterations' codes together: of a canonical row they share lines)
+            __builtin_amdgcn_sched_barrier(0);
             if (more && (u & 1)) load_codes(u - 1, i0 + u + 3), load_codes(u, i0 + u + 4);
         }
     };
@@ -312,13 +314,18 @@ __global__ __launch_bounds__(64) void matvec_simple_kernel(MatvecArgs a)
     if (lane == 0) store_one(a, blockIdx.y, n, sum * *a.alpha);
 }
 
-static bool in_lds(int64_t M, int64_t K) { return M <= kLdsTokens && M * ((K + 127) / 128) * 256 <= kLdsBytes; }
-static int64_t packed_bytes(int64_t M, int64_t K) { return (K + 127) / 128 * ((M + 15) / 16) * 4096; }
-
 // Strips of a workgroup: four share an activation operand ([9, 4096 -> 28672] 22 us, with two 25), two where four would leave
 // compute units without a workgroup ([16, 4096 -> 4096] 11.6 and 13.0 us).  A single strip and eight waves for up to four tokens
 // of a narrow layer ([1, 4096 -> 6144] 7.3 us, four strips 9.4; [1, 14336 -> 4096] 12.5 and 24).
 static int strips_of(int64_t N) { return N >= 8192 ? 4 : 2; }
+// Activations in every workgroup's LDS instead of a launch in front: for so few workgroups that each can afford it
+// ([4, 4096 -> 6144] 9.5 us, packed 11.5; [4, 5120 -> 51200] 46 and 41; nine tokens of 4096 would be 39 instead of 21)
+static bool in_lds(int64_t M, int64_t N, int64_t K)
+{
+    return M <= (strips_of(N) == 4 ? kLdsTokens / 2 : kLdsTokens) && M * ((K + 127) / 128) * 256 <= kLdsBytes;
+}
+static int64_t packed_bytes(int64_t M, int64_t K) { return (K + 127) / 128 * ((M + 15) / 16) * 4096; }
+
 // K slabs that give the GPU two workgroups for each compute unit, of 16 iterations at least ([40, 25600 -> 5120] 44 us with
 // three of them, 52 with none)
 static int slabs_of(int64_t M, int64_t N, int64_t K)
@@ -329,7 +336,7 @@ static int slabs_of(int64_t M, int64_t N, int64_t K)
 
 int64_t matvec_workspace(int64_t M, int64_t N, int64_t K)
 {
-    if (K % 64 || in_lds(M, K)) return 0;
+    if (K % 64 || in_lds(M, N, K)) return 0;
     const int slabs = slabs_of(M, N, K);
     return packed_bytes(M, K) + 16 * ((M + 3) / 4) + (slabs > 1 ? 4 * slabs * M * N : 0);
 }
@@ -358,7 +365,7 @@ int launch_nvfp4_matvec(const uint16_t *x, int64_t ldx, const uint8_t *codes, co
     MatvecArgs a{x, ldx, codes, scales, alpha, K / 2, 32, K / 16, 4, M, N, K, y, ldy, out, (int)((M + 15) / 16), nullptr, nullptr, nullptr, 1};
     if (layout == MQ_LAYOUT_KTILE) a.c_row = 32, a.c_step = 32 * N, a.s_row = 4, a.s_step = 4 * N;
     if (K % 64) return enqueue(matvec_simple_kernel, dim3((unsigned)N, (unsigned)M), dim3(64), 0, s, a);
-    if (in_lds(M, K)) return strips_of(N) == 4 ? launch<true, 1, 4, 4>(a, s) : launch<true, 1, 1, 8>(a, s);
+    if (in_lds(M, N, K)) return strips_of(N) == 4 ? launch<true, 1, 4, 4>(a, s) : launch<true, 1, 1, 8>(a, s);
     a.packed = static_cast<const u32x4 *>(ws);
     a.exps = reinterpret_cast<const int *>(static_cast<const char *>(ws) + packed_bytes(M, K));
     if (int rc = enqueue(matvec_pack_kernel, dim3((unsigned)M), dim3(1024), 0, s, a)) return rc;

@@ -118,3 +118,9 @@ def test_tensors_on_the_cpu_are_refused():
         mq.kv8_attention(h, codes, scales, codes, scales, i.view(1, 2), i, i[:1], 0.125)
     with pytest.raises(mq.MixQuantError, match="GPU"):
         mq.mq_rope_table(16, 64, device="cpu")
+
+
+def test_matvec_workspace_of_wide_layers(lib):
+    # where many workgroups would each bring the activations into their LDS, a launch in front does it once
+    w = lib.mq_nvfp4_matvec_workspace_bytes
+    assert w(2, 28672, 4096) == 0 and w(3, 28672, 4096) > 0 and w(4, 8191, 4096) == 0
