@@ -8,8 +8,8 @@
 // to 2^14 .. 2^15: exact for every element down to 2^-29 of that one, below that off by at most 2^-38 of it.  Sums are FP32.
 //
 // The activations are laid out once in the order in which the matrix instructions take them, so that an operand is 1 KB of
-// contiguous memory or LDS: up to kLdsTokens tokens by every workgroup in its LDS, more of them by a kernel in front into the
-// workspace.  (Read in rows, 40 tokens of 25600 took 36 us of 68 for themselves.)
+// contiguous memory or LDS: up to kLdsTokens tokens by every workgroup in its LDS (in_lds), more of them by a kernel in front
+// into the workspace.  (Read in rows, 40 tokens of 25600 took 36 us of 68 for themselves.)
 //
 // A wave owns S strips of 16 rows of W and a range of K, and up to 16 MT tokens: of each 128 elements of K (an iteration) a
 // lane (row = lane % 16, g = lane / 16) loads the 16 bytes of codes at element 32 g, its slots of four 16x16x32 products.
@@ -319,19 +319,27 @@ __global__ __launch_bounds__(64) void matvec_simple_kernel(MatvecArgs a)
 // of a narrow layer ([1, 4096 -> 6144] 7.3 us, four strips 9.4; [1, 14336 -> 4096] 12.5 and 24).
 static int strips_of(int64_t N) { return N >= 8192 ? 4 : 2; }
 // Activations in every workgroup's LDS instead of a launch in front: for so few workgroups that each can afford it
-// ([4, 4096 -> 6144] 9.5 us, packed 11.5; [4, 5120 -> 51200] 46 and 41; nine tokens of 4096 would be 39 instead of 21)
+// ([2, 14336 -> 4096] 14.5 us, packed 20.5; [4, 5120 -> 51200] 46 and 40; nine tokens of 4096 would be 39 instead of 21)
 static bool in_lds(int64_t M, int64_t N, int64_t K)
 {
     return M <= (strips_of(N) == 4 ? kLdsTokens / 2 : kLdsTokens) && M * ((K + 127) / 128) * 256 <= kLdsBytes;
 }
 static int64_t packed_bytes(int64_t M, int64_t K) { return (K + 127) / 128 * ((M + 15) / 16) * 4096; }
 
-// K slabs that give the GPU two workgroups for each compute unit, of 16 iterations at least ([40, 25600 -> 5120] 44 us with
-// three of them, 52 with none)
+// K slabs.  The longest that a compute unit works is the iterations of a slab times the workgroups that the busiest one gets, of
+// 256; writing the slabs' sums and joining them costs about what 24 iterations do, and 4 for each slab.  [40, 25600 -> 5120], 160
+// workgroups a slab: none 52 us, two (which leave most units one and some two) 56, three 44.  [40, 12288 -> 8192], 128: none 35,
+// two 30, four 34.  [5, 4096 -> 6144]: none 9.5, two 12.
 static int slabs_of(int64_t M, int64_t N, int64_t K)
 {
     const int64_t groups = (N + 16 * strips_of(N) - 1) / (16 * strips_of(N)) * ((M + 63) / 64), iters = (K + 127) / 128;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({512 / groups, iters / 16, 8}));
+    int best = 1;
+    int64_t least = INT64_MAX;
+    for (int slabs = 1; slabs == 1 || (slabs <= 8 && iters >= 16 * slabs); ++slabs) {
+        const int64_t cost = (groups * slabs + 255) / 256 * iters + (slabs > 1 ? (24 + 4 * slabs) * slabs : 0);  // times slabs
+        if (cost * 840 / slabs < least) least = cost * 840 / slabs, best = slabs;  // (840: a multiple of them all)
+    }
+    return best;
 }
 
 int64_t matvec_workspace(int64_t M, int64_t N, int64_t K)

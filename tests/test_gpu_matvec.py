@@ -133,3 +133,8 @@ def test_empty_and_repeated():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, mq.nvfp4_matvec(xd, *args))
+
+
+def test_k_in_two_slabs():
+    check(5, 20, 4090, 10240)
+    check(6, 5, 40, 6144)
