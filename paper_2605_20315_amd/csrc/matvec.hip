@@ -314,30 +314,39 @@ __global__ __launch_bounds__(64) void matvec_simple_kernel(MatvecArgs a)
     if (lane == 0) store_one(a, blockIdx.y, n, sum * *a.alpha);
 }
 
-// Strips of a workgroup: four share an activation operand ([9, 4096 -> 28672] 22 us, with two 25), two where four would leave
-// compute units without a workgroup ([16, 4096 -> 4096] 11.6 and 13.0 us).  A single strip and eight waves for up to four tokens
-// of a narrow layer ([1, 4096 -> 6144] 7.3 us, four strips 9.4; [1, 14336 -> 4096] 12.5 and 24).
-static int strips_of(int64_t N) { return N >= 8192 ? 4 : 2; }
 // Activations in every workgroup's LDS instead of a launch in front: for so few workgroups that each can afford it
-// ([2, 14336 -> 4096] 14.5 us, packed 20.5; [4, 5120 -> 51200] 46 and 40; nine tokens of 4096 would be 39 instead of 21)
+// ([2, 14336 -> 4096] 14.5 us, packed 20.5; [4, 5120 -> 51200] 46 and 40; nine tokens of 4096 would be 39 instead of 21).  Four
+// strips share a wide layer's; a narrow one has a strip and eight waves a workgroup ([1, 4096 -> 6144] 7.0 us, four strips 9.0;
+// [1, 14336 -> 4096] 12 and 22).
+static bool is_wide(int64_t N) { return N >= 8192; }
 static bool in_lds(int64_t M, int64_t N, int64_t K)
 {
-    return M <= (strips_of(N) == 4 ? kLdsTokens / 2 : kLdsTokens) && M * ((K + 127) / 128) * 256 <= kLdsBytes;
+    return M <= (is_wide(N) ? kLdsTokens / 2 : kLdsTokens) && M * ((K + 127) / 128) * 256 <= kLdsBytes;
 }
 static int64_t packed_bytes(int64_t M, int64_t K) { return (K + 127) / 128 * ((M + 15) / 16) * 4096; }
 
-// K slabs.  The longest that a compute unit works is the iterations of a slab times the workgroups that the busiest one gets, of
-// 256; writing the slabs' sums and joining them costs about what 24 iterations do, and 4 for each slab.  [40, 25600 -> 5120], 160
-// workgroups a slab: none 52 us, two (which leave most units one and some two) 56, three 44.  [40, 12288 -> 8192], 128: none 35,
-// two 30, four 34.  [5, 4096 -> 6144]: none 9.5, two 12.
-static int slabs_of(int64_t M, int64_t N, int64_t K)
+// Strips of a workgroup that share the packed activations, and slabs of K, by the time of the busiest of 256 compute units: the
+// iterations of a slab times the workgroups that it gets.  Writing the slabs' sums and joining them costs about what 24 two-strip
+// iterations do, and 4 for each slab and 64 tokens; an iteration of four strips 1.6 of two.
+//   two strips:   [40, 25600 -> 5120], 160 workgroups a slab: no slabs 52 us, two (most units have one, some two) 56, three 44
+//                 [5, 4096 -> 6144], 192: no slabs 9.5, two 12
+//   four strips:  [40, 25600 -> 5120], 80: three slabs 37; [40, 12288 -> 8192], 128: no slabs 35, two 30, four 34;
+//                 [64, 4096 -> 28672]: 38, two strips 46; [16, 4096 -> 4096] 11 and 9.6
+struct Split {
+    int strips, slabs;
+};
+static Split split_of(int64_t M, int64_t N, int64_t K)
 {
-    const int64_t groups = (N + 16 * strips_of(N) - 1) / (16 * strips_of(N)) * ((M + 63) / 64), iters = (K + 127) / 128;
-    int best = 1;
-    int64_t least = INT64_MAX;
-    for (int slabs = 1; slabs == 1 || (slabs <= 8 && iters >= 16 * slabs); ++slabs) {
-        const int64_t cost = (groups * slabs + 255) / 256 * iters + (slabs > 1 ? (24 + 4 * slabs) * slabs : 0);  // times slabs
-        if (cost * 840 / slabs < least) least = cost * 840 / slabs, best = slabs;  // (840: a multiple of them all)
+    const int64_t iters = (K + 127) / 128, blocks = (M + 63) / 64;
+    Split best{2, 1};
+    double least = 1e300;
+    for (int strips = 2; strips <= 4; strips += 2) {
+        const int64_t groups = (N + 16 * strips - 1) / (16 * strips) * blocks;
+        for (int slabs = 1; slabs == 1 || (slabs <= 8 && iters >= 16 * slabs); ++slabs) {
+            const int64_t rounds = (groups * slabs + 255) / 256;
+            const double cost = (double)(rounds * iters) / slabs * (strips == 4 ? 1.6 : 1.0) + (slabs > 1 ? 24 + 4 * slabs * blocks : 0);
+            if (cost < least) least = cost, best = Split{strips, slabs};
+        }
     }
     return best;
 }
@@ -345,7 +354,7 @@ static int slabs_of(int64_t M, int64_t N, int64_t K)
 int64_t matvec_workspace(int64_t M, int64_t N, int64_t K)
 {
     if (K % 64 || in_lds(M, N, K)) return 0;
-    const int slabs = slabs_of(M, N, K);
+    const int slabs = split_of(M, N, K).slabs;
     return packed_bytes(M, K) + 16 * ((M + 3) / 4) + (slabs > 1 ? 4 * slabs * M * N : 0);
 }
 
@@ -373,16 +382,16 @@ int launch_nvfp4_matvec(const uint16_t *x, int64_t ldx, const uint8_t *codes, co
     MatvecArgs a{x, ldx, codes, scales, alpha, K / 2, 32, K / 16, 4, M, N, K, y, ldy, out, (int)((M + 15) / 16), nullptr, nullptr, nullptr, 1};
     if (layout == MQ_LAYOUT_KTILE) a.c_row = 32, a.c_step = 32 * N, a.s_row = 4, a.s_step = 4 * N;
     if (K % 64) return enqueue(matvec_simple_kernel, dim3((unsigned)N, (unsigned)M), dim3(64), 0, s, a);
-    if (in_lds(M, N, K)) return strips_of(N) == 4 ? launch<true, 1, 4, 4>(a, s) : launch<true, 1, 1, 8>(a, s);
+    if (in_lds(M, N, K)) return is_wide(N) ? launch<true, 1, 4, 4>(a, s) : launch<true, 1, 1, 8>(a, s);
     a.packed = static_cast<const u32x4 *>(ws);
     a.exps = reinterpret_cast<const int *>(static_cast<const char *>(ws) + packed_bytes(M, K));
     if (int rc = enqueue(matvec_pack_kernel, dim3((unsigned)M), dim3(1024), 0, s, a)) return rc;
-    a.slabs = slabs_of(M, N, K);
+    const Split split = split_of(M, N, K);
+    a.slabs = split.slabs;
     a.sums = reinterpret_cast<float *>(static_cast<char *>(ws) + packed_bytes(M, K) + 16 * ((M + 3) / 4));
-    const bool four = strips_of(N) == 4;
     auto go = [&](auto tiles) {
         constexpr int MT = decltype(tiles)::value;
-        return four ? launch<false, MT, 4, 4>(a, s) : launch<false, MT, 2, 4>(a, s);
+        return split.strips == 4 ? launch<false, MT, 4, 4>(a, s) : launch<false, MT, 2, 4>(a, s);
     };
     const int rc = a.tiles == 1 ? go(std::integral_constant<int, 1>()) : a.tiles == 2 ? go(std::integral_constant<int, 2>())
                  : a.tiles == 3 ? go(std::integral_constant<int, 3>()) : go(std::integral_constant<int, 4>());

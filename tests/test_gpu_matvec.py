@@ -138,3 +138,8 @@ def test_empty_and_repeated():
 def test_k_in_two_slabs():
     check(5, 20, 4090, 10240)
     check(6, 5, 40, 6144)
+
+
+def test_four_strips_and_slabs():
+    check(7, 18, 5100, 12800)
+    check(8, 70, 8200, 128)
