@@ -23,6 +23,7 @@ FLAGS = [
     "-Wall", "-Wno-unused-command-line-argument",
 ]
 
+# accumulators in ordinary registers: the softmax works on them, and would copy each from and to the other half of the file
 FILE_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 

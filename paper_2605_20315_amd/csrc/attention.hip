@@ -99,7 +99,7 @@ static __device__ __forceinline__ int64_t sum_of(const Kv8Attend &a, const Cut &
 }
 
 // Tokens per chunk, in tiles, that make the call about c.target items; no more than that where c.fit: one workgroup too many
-// is a second round of all (39 sequences in 530 items for 512 places 325 us, in fewer and longer ones 250).
+// is a second round of all (39 sequences in 530 items for 512 places 30 % longer than in fewer and longer ones, 218 us).
 template <int NT>
 static __device__ int chunk_tiles(const Kv8Attend &a, const Cut &c, PlanLds &lds, int tid)
 {
@@ -236,8 +236,9 @@ constexpr int kFewWaves = 4, kFewThreads = 64 * kFewWaves;
 // One item by four waves, each with every fourth group of 32 tokens.  Lane (c = lane % 16, g = lane / 16) of a wave reads, of
 // the keys, bytes g * D / 4 .. of token c of each half; of the values, bytes c * D / 16 .. of tokens 4g .. 4g + 3 of each half:
 // whole rows of the page in one instruction, operands without any exchange between lanes.
-// Measured, heads of 128, 32 on 8: 64 tokens after 100 to 8000 each, 600 MB, 118 us = 5.1 TB/s (a large copy 4.8), all of it
-// waiting for memory (vector instructions 15 % of the time); two sequences of 105000, 435 MB, 86 us.
+// Measured, heads of 128, 32 on 8: 64 tokens after 100 to 8000 each, 600 MB, 116 us = 5.2 TB/s (a large copy 4.8), all of it
+// waiting for memory (vector instructions 15 % of the time); two sequences of 105000, 435 MB, 83 us.  A branch around the loads
+// ahead would make every wait one for all of them (125 and 92 us with the join, so 120.5 and 89).
 // RT tiles of 16 rows: what a wave has expanded serves all of them (109 sequences of 23000, 52 rows each: 365 us with one, 233 with two).
 template <int D, int RT>
 __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
@@ -524,9 +525,10 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
 // between those and the next ones' maxima; and two workgroups share a compute unit, which their barriers hold up in turn.  So tile i
 // of keys is 32 tokens ahead of tile i of values: tokens t + 32 .. t + 95 and t .. t + 63.  Both of tile i + 1 are loaded when
 // tile i begins and expanded at its end; with two buffers one barrier a tile is enough.
-// Measured, a prompt of 8192 tokens, 32 query and 8 key heads of 128: 635 us = 866 TFLOP/s of 1364 that a library product of
-// 8192^3 reaches here; without the keys ahead 747; one wave a SIMD with 64 rows, which reads LDS half as often, 945 (it has
-// no second wave to fill its waits); eight waves in one workgroup 635, and less even shares of short work.
+// Measured, a prompt of 8192 tokens, 32 query and 8 key heads of 128: 595 us = 924 TFLOP/s of 1364 that a library product of
+// 8192^3 reaches here.  Compared while it took 635 (its page numbers were looked at where they were read): without the keys
+// ahead 747; one wave a SIMD with 64 rows, which reads LDS half as often, 945 (it has no second wave to fill its waits);
+// eight waves in one workgroup 635, and less even shares of short work.
 template <int D>
 __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut c)
 {
@@ -906,8 +908,8 @@ __global__ __launch_bounds__(256) void attend_join(Kv8Attend a, Cut c)
 // ------------------------------------------------------------------------------------------------ launches
 
 constexpr int64_t kWorkspace = (int64_t)64 << 20;
-// Items aimed at: as many workgroups as the GPU holds at a time (attend_few, which is bound by memory, half as many more: a batch
-// of uneven lengths takes 124 us so, 136 with one round; two long sequences 92 and 89), of which those of sequences that are cut
+// Items aimed at: as many workgroups as the GPU holds at a time (attend_few, which is bound by memory, half as many more: when a
+// batch of uneven lengths took 124 us so, it took 136 with one round; two long sequences 92 and 89), of which those of sequences that are cut
 // are less than twice as many, and the workspace has to have slots for them.
 constexpr int kFewTarget = 768;
 // workgroups of attend_many that a compute unit holds, by registers and LDS: three, two and one
