@@ -255,7 +255,8 @@ int bf16_gemm_ws(const void *x_bf16, int64_t ldx, const void *w_bf16, int64_t ld
  * x: [M, K] BF16, row stride ldx.  K % 16 == 0 (K % 64 == 0 for MQ_LAYOUT_KTILE); x, w_codes 16-byte aligned, ldx % 8 == 0,
  * scale arrays 4-byte aligned when K % 64 == 0; any ldy >= N, y aligned to its element.  M <= 65535, N and K < 2^31.
  * workspace: device memory, 16-byte aligned, of mq_nvfp4_matvec_workspace_bytes(M, N, K) bytes (0 for up to four tokens, two
- * where N >= 8192, of at most 32768 elements in all, K rounded up to a multiple of 128, and where K % 64 != 0), or the call is refused with MQ_ERR_SCRATCH; otherwise as in nvfp4_gemm_ws.
+ * where N >= 8192, of at most 32768 elements in all, K rounded up to a multiple of 128, and where K % 64 != 0), or the call is
+ * refused with MQ_ERR_SCRATCH; otherwise as in nvfp4_gemm_ws.
  * Results are bit-identical from run to run.
  */
 int64_t mq_nvfp4_matvec_workspace_bytes(int64_t M, int64_t N, int64_t K);
