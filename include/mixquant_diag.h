@@ -51,6 +51,20 @@ typedef struct {
 int mq_gemm_launches(int64_t M, int64_t N, int64_t K, int layout, int64_t workspace_bytes, int cus, mq_launch out[2]);
 int mq_bf16_gemm_launches(int64_t M, int64_t N, int64_t K, int64_t workspace_bytes, int cus, mq_launch out[2]);
 
+/* kv8_attention for these sizes: the kernel (MQ_KV8_FEW: tiles of 16 or 32 rows, MQ_KV8_MANY: of 128; a row is a query head of a
+ * token), its rows a tile, whether it may cut histories into chunks (a kernel that joins them follows then), its workgroups, and the
+ * places that a sequence has at most.  Two launches share the sequences by their numbers of rows.  Returns as the above. */
+typedef enum {
+    MQ_KV8_FEW = 0,
+    MQ_KV8_MANY = 1
+} mq_kv8_kernel;
+typedef struct {
+    int kernel, rows, cut;
+    int64_t workgroups, places;
+} mq_kv8_launch;
+int mq_kv8_attention_launches(int64_t pages, int P, int Hq, int Hkv, int D, int64_t W, int64_t B, int64_t T, int64_t workspace_bytes,
+                              mq_kv8_launch out[2]);
+
 /* Rows per workgroup of the quantizers with K-step-major output (K % 64 == 0): source 0 nvfp4_quantize,
  * 1 nvfp4_quantize_silu_mul, 2 nvfp4_quantize_rmsnorm.  Minus an mq_status for bad arguments. */
 int mq_quantize_rows(int source, int64_t rows, int64_t K);

@@ -30,6 +30,11 @@ class Launch(ctypes.Structure):
                                                                                        ("cols", ctypes.c_int64)]
 
 
+class Kv8Launch(ctypes.Structure):
+    """mq_kv8_launch of include/mixquant_diag.h."""
+    _fields_ = [(n, ctypes.c_int) for n in ("kernel", "rows", "cut")] + [(n, ctypes.c_int64) for n in ("workgroups", "places")]
+
+
 def load() -> ctypes.CDLL:
     global _lib
     if _lib is not None:
@@ -91,6 +96,8 @@ def load() -> ctypes.CDLL:
     lib.mq_gemm_launches.argtypes = [i64, i64, i64, ci, i64, ci, ctypes.POINTER(Launch)]
     lib.mq_bf16_gemm_launches.restype = ci
     lib.mq_bf16_gemm_launches.argtypes = [i64, i64, i64, i64, ci, ctypes.POINTER(Launch)]
+    lib.mq_kv8_attention_launches.restype = ci
+    lib.mq_kv8_attention_launches.argtypes = [i64, ci, ci, ci, ci, i64, i64, i64, i64, ctypes.POINTER(Kv8Launch)]
     lib.mq_quantize_rows.restype = ci
     lib.mq_quantize_rows.argtypes = [ci, i64, i64]
     lib.mq_status_string.restype = ctypes.c_char_p

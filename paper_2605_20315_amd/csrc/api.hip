@@ -393,10 +393,12 @@ static int check_cache_pointers(const void *kc, const void *ks, const void *vc, 
     return MQ_OK;
 }
 
+// A pool without pages has no place for any token, whatever the tables say: their width is then none, so that no kernel looks for
+// a page (some load from page 0 where a number is no page's).
 static Kv8Seqs sequences(const int32_t *page_table, int64_t pt_ld, int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B,
                          int64_t T, int64_t pages, int P)
 {
-    return Kv8Seqs{page_table, cu_q, kv_lens, pt_ld, pages, (int)W, (int)B, (int)T, P == 16 ? 4 : P == 32 ? 5 : P == 64 ? 6 : 7};
+    return Kv8Seqs{page_table, cu_q, kv_lens, pt_ld, pages, pages > 0 ? (int)W : 0, (int)B, (int)T, P == 16 ? 4 : P == 32 ? 5 : P == 64 ? 6 : 7};
 }
 
 int kv8_append(const void *q_bf16, int64_t ldq, const void *k_bf16, int64_t ldk, const void *v_bf16, int64_t ldv, void *q_out,
@@ -472,6 +474,22 @@ int mq_bf16_gemm_launches(int64_t M, int64_t N, int64_t K, int64_t workspace_byt
     if (!out) return -MQ_ERR_NULL;
     if (M < 0 || N < 0 || K <= 0 || K % 8 != 0 || workspace_bytes < 0 || cus < 1) return -MQ_ERR_SHAPE;
     return M == 0 || N == 0 ? 0 : describe_gemm_bf16(M, N, K, workspace_bytes, cus, out);
+}
+
+int mq_kv8_attention_launches(int64_t pages, int P, int Hq, int Hkv, int D, int64_t W, int64_t B, int64_t T, int64_t workspace_bytes,
+                              mq_kv8_launch out[2])
+{
+    if (!out) return -MQ_ERR_NULL;
+    if (int rc = check_cache(pages, P, Hq, Hkv, D, W, W, B, T)) return -rc;
+    if (workspace_bytes < 0) return -MQ_ERR_SHAPE;
+    if (T == 0 || B == 0) return 0;
+    static float some;  // (only looked at for being there)
+    Kv8Attend a{};
+    a.Hq = Hq, a.Hkv = Hkv, a.D = D;
+    a.ws = workspace_bytes > 0 ? &some : nullptr;
+    a.ws_bytes = workspace_bytes;
+    a.s = sequences(nullptr, W, W, nullptr, nullptr, B, T, pages, P);
+    return describe_kv8_attention(a, out);
 }
 
 int mq_quantize_rows(int source, int64_t rows, int64_t K)

@@ -923,41 +923,74 @@ int64_t kv8_attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D)
     return kWorkspace;
 }
 
-template <int D>
-static int launch_attention(const Kv8Attend &a, hipStream_t s)
+// One launch of a call: which kernel, how it cuts, and its workgroups
+struct Launch {
+    bool many;
+    Cut cut;
+    int64_t items;
+};
+
+static int plan_attention(const Kv8Attend &a, Launch *out)
 {
-    constexpr int kRows = 32 * kManyWaves;
+    constexpr int kManyRows = 32 * kManyWaves;
+    const int D = a.D;
     const int64_t G = a.Hq / a.Hkv, T = a.s.T, B = a.s.B;
     const bool ws = a.ws && a.ws_bytes >= kWorkspace && B <= kPartsMost;
+    int n = 0;
     // If every sequence has a token, none has more than T - B + 1 of them, and where there are few tokens a sequence (a decode
     // batch, drafted tokens among it) a second kernel that finds nothing to do costs more than a longer prompt loses in
     // attend_few.  (Every split of the work is right: it is only slower than it need be.)  Up to kAllMany sequences attend_many takes
     // all if it takes any.
     const bool many = T > 4 * B && (T - B + 1) * G > kFewMost, few = !many || B > kAllMany;
-    auto go = [&](auto kernel, Cut cut, int threads) {
+    auto add = [&](bool is_many, int rows, int most_items, int least, int above, int most) {
+        Cut cut{rows, target_of(most_items, rows, D), least, above, most, true, is_many, a.ws, slots_of(rows, D)};
         // An item for each tile of rows and key head; where sequences are cut, as many more as the target has, or as their
         // longest possible history has chunks
         const int64_t whole = (T * G / cut.rows + B) * a.Hkv, tiles = ((int64_t)a.s.width << a.s.page_shift) / kTile + 1;
-        cut.split = cut.split && ws && whole < 2 * cut.target && tiles >= 2 * cut.least;
-        const int64_t items = cut.split ? std::min(whole + 2 * cut.target, whole * (tiles / cut.least + 1)) : whole;
-        if (items > 0x7fffffff) return (int)MQ_ERR_SHAPE;
-        if (int rc = enqueue(kernel, dim3((unsigned)items), dim3(threads), 0, s, a, cut)) return rc;
-        if (!cut.split) return (int)MQ_OK;
-        constexpr int kPer = 1024 / D;
-        if (T * a.Hq >= 2048) return enqueue(attend_join<D, true>, dim3((unsigned)(T * ((a.Hq + kPer - 1) / kPer))), dim3(256), 0, s, a, cut);
-        return enqueue(attend_join<D, false>, dim3((unsigned)(T * a.Hq)), dim3(256), 0, s, a, cut);
+        cut.split = ws && whole < 2 * cut.target && tiles >= 2 * cut.least;
+        out[n++] = Launch{is_many, cut, cut.split ? std::min(whole + 2 * cut.target, whole * (tiles / cut.least + 1)) : whole};
     };
-    if (few) {
-        auto cut = [&](int rows) { return Cut{rows, target_of(kFewTarget, rows, D), 2, 0, many ? kFewMost : INT32_MAX, true, false, a.ws, slots_of(rows, D)}; };
+    // (heads of 256 have no registers for two tiles)
+    if (few) add(false, D <= 128 && T * G > B * kFewRows ? 2 * kFewRows : kFewRows, kFewTarget, 2, 0, many ? kFewMost : INT32_MAX);
+    if (many) add(true, kManyRows, many_target(D), 4, few ? kFewMost : 0, INT32_MAX);
+    return n;
+}
+
+template <int D>
+static int launch_attention(const Kv8Attend &a, hipStream_t s)
+{
+    Launch plan[2];
+    const int n = plan_attention(a, plan);
+    for (int i = 0; i < n; ++i) {
+        const Launch &p = plan[i];
+        if (p.items > 0x7fffffff) return MQ_ERR_SHAPE;
+        auto go = [&](auto kernel, int threads) { return enqueue(kernel, dim3((unsigned)p.items), dim3(threads), 0, s, a, p.cut); };
         int rc;
-        if constexpr (D <= 128)  // (heads of 256 have no registers for two tiles)
-            rc = T * G > B * kFewRows ? go(attend_few<D, 2>, cut(2 * kFewRows), kFewThreads) : go(attend_few<D, 1>, cut(kFewRows), kFewThreads);
+        if (p.many)
+            rc = go(attend_many<D>, 64 * kManyWaves);
+        else if (p.cut.rows == kFewRows)
+            rc = go(attend_few<D, 1>, kFewThreads);
         else
-            rc = go(attend_few<D, 1>, cut(kFewRows), kFewThreads);
+            rc = go(attend_few<D, D <= 128 ? 2 : 1>, kFewThreads);
+        if (rc) return rc;
+        if (!p.cut.split) continue;
+        constexpr int kPer = 1024 / D;
+        const int64_t T = a.s.T;
+        rc = T * a.Hq >= 2048 ? enqueue(attend_join<D, true>, dim3((unsigned)(T * ((a.Hq + kPer - 1) / kPer))), dim3(256), 0, s, a, p.cut)
+                              : enqueue(attend_join<D, false>, dim3((unsigned)(T * a.Hq)), dim3(256), 0, s, a, p.cut);
         if (rc) return rc;
     }
-    if (!many) return MQ_OK;
-    return go(attend_many<D>, Cut{kRows, target_of(many_target(D), kRows, D), 4, few ? kFewMost : 0, INT32_MAX, true, true, a.ws, slots_of(kRows, D)}, 64 * kManyWaves);
+    return MQ_OK;
+}
+
+int describe_kv8_attention(const Kv8Attend &a, mq_kv8_launch *out)
+{
+    Launch plan[2];
+    const int n = plan_attention(a, plan);
+    for (int i = 0; i < n; ++i)
+        out[i] = mq_kv8_launch{plan[i].many ? MQ_KV8_MANY : MQ_KV8_FEW, plan[i].cut.rows, plan[i].cut.split, plan[i].items,
+                               (int64_t)a.s.width << a.s.page_shift};
+    return n;
 }
 
 int launch_kv8_attention(const Kv8Attend &a, hipStream_t s)

@@ -500,3 +500,14 @@ def mq_bf16_gemm_launches(M: int, N: int, K: int, workspace_bytes: int = 0, comp
     """What the BF16 product launches for this problem (host only)."""
     got = (_lib.Launch * 2)()
     return _launches(_lib.load().mq_bf16_gemm_launches(M, N, K, workspace_bytes, compute_units, got), got)
+
+
+def mq_kv8_attention_launches(pages: int, P: int, Hq: int, Hkv: int, D: int, W: int, B: int, T: int, workspace_bytes: int = 0) -> list:
+    """What kv8_attention launches for these sizes (host only): kernel, rows of a tile, whether histories may be cut, workgroups,
+    and the places that a sequence has at most."""
+    got = (_lib.Kv8Launch * 2)()
+    n = _lib.load().mq_kv8_attention_launches(pages, P, Hq, Hkv, D, W, B, T, workspace_bytes, got)
+    if n < 0:
+        _lib.check(-n, "mq_kv8_attention_launches")
+    return [{"kernel": ("few", "many")[l.kernel], "rows": l.rows, "cut": bool(l.cut), "workgroups": l.workgroups, "places": l.places}
+            for l in got[:n]]

@@ -276,3 +276,28 @@ def test_drafted_tokens_that_see_nothing_and_pages_that_are_none():
 def test_one_long_prompt_among_single_tokens():
     # few tokens a sequence on the whole: the prompt goes the same way as the others
     Problem(21, [1] * 60 + [170] + [1] * 20, [int(n) for n in np.random.default_rng(1).integers(0, 90, 81)], 4, 2, 64, 32).check()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_a_pool_without_pages(D):
+    """Every page number is none: zeros, and nothing to append to.  (An empty tensor has no address: the cache's pointers are those of another.)"""
+    from paper_2605_20315_amd import _lib
+    lib = _lib.load()
+    codes, scales = (torch.full((4 * 128 * 256,), x, dtype=torch.uint8, device="cuda") for x in (0x38, 127))
+    ws = torch.full((64 << 20,), 0xFF, dtype=torch.uint8, device="cuda")
+    for q_lens in ([1], [40], [1] * 12, [300] + [2] * 11):
+        B, T, W = len(q_lens), sum(q_lens), 300
+        q, kv = torch.randn(T, 4, D, device="cuda").to(torch.bfloat16), torch.randn(T, 2, D, device="cuda").to(torch.bfloat16)
+        pt, cu = torch.zeros(B, W, dtype=torch.int32, device="cuda"), dev(np.cumsum([0] + q_lens).astype(np.int32))
+        lens = torch.full((B,), 9000, dtype=torch.int32, device="cuda")
+        out = torch.empty_like(q)
+        cache = [t.data_ptr() for t in (codes, scales, codes, scales)]
+        assert lib.kv8_append(q.data_ptr(), 4 * D, kv.data_ptr(), 2 * D, kv.data_ptr(), 2 * D, out.data_ptr(), *cache, 0, 32, 4, 2, D, pt.data_ptr(), W, W,
+                              cu.data_ptr(), lens.data_ptr(), B, T, None, 0, 0, None, 0, torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(out, q)
+        for bytes_ in (0, ws.numel()):
+            y = torch.full((T, 4, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+            assert lib.kv8_attention(q.data_ptr(), 4 * D, *cache, 0, 32, 4, 2, D, pt.data_ptr(), W, W, cu.data_ptr(), lens.data_ptr(), B, T, 0.125, 0,
+                                     y.data_ptr(), 4 * D, ws.data_ptr() if bytes_ else None, bytes_, torch.cuda.current_stream().cuda_stream) == 0
+            assert (y == 0).all()
+    assert (codes == 0x38).all() and (scales == 127).all()
