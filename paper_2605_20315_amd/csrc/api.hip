@@ -442,8 +442,8 @@ int kv8_attention(const void *q_bf16, int64_t ldq, const uint8_t *k_codes, const
     if (!aligned(q_bf16, 16) || !aligned(y, 16) || ldq % 8 != 0 || ldy % 8 != 0 || (workspace && !aligned(workspace, 16)))
         return MQ_ERR_ALIGN;
     Kv8Attend a{static_cast<const uint16_t *>(q_bf16), ldq, k_codes, k_scales, v_codes, v_scales, static_cast<uint16_t *>(y), ldy, Hq, Hkv, D,
-                // a window that no place lies outside of is none
-                window <= 0 || window >= W * P ? 0 : (int)window, sm_scale * 1.44269504f, nullptr, 0,
+                // a window that no int32 place lies outside of is none (one of W * P can bind: kv_lens may count places beyond the table)
+                window <= 0 || window > 0x7fffffff ? 0 : (int)window, sm_scale * 1.44269504f, nullptr, 0,
                 sequences(page_table, pt_ld, W, cu_q, kv_lens, B, T, pages, P)};
     a.ws = workspace_bytes > 0 ? static_cast<float *>(workspace) : nullptr;
     a.ws_bytes = a.ws ? workspace_bytes : 0;

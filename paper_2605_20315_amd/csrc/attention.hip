@@ -49,13 +49,19 @@ struct Extent {
     int row_tiles, lo, tiles;  // first token (a multiple of kTile) and tiles of tokens that any query sees
 };
 
+// The first place that a token at `pos` sees (at least 0: it may lie before the first place, and its window is any int32)
+static __device__ __forceinline__ int first_seen(const Kv8Attend &a, int pos)
+{
+    return a.window > 0 ? max(pos, a.window - 1) - (a.window - 1) : 0;
+}
+
 static __device__ __forceinline__ Extent extent_of(const Kv8Attend &a, const Cut &c, const Span &sp)
 {
     Extent e{0, 0, 0};
     const int64_t rows = (int64_t)sp.n * (a.Hq / a.Hkv);
     if (rows <= c.above || rows > c.most) return e;
     e.row_tiles = (int)((rows + c.rows - 1) / c.rows);
-    e.lo = a.window > 0 ? max(sp.start - a.window + 1, 0) & ~(kTile - 1) : 0;
+    e.lo = first_seen(a, sp.start) & ~(kTile - 1);
     e.tiles = sp.len > e.lo ? (sp.len - e.lo + kTile - 1) / kTile : 0;
     return e;
 }
@@ -261,7 +267,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
     for (int f = 0; f < RT; ++f) {
         const int row = min(row0 + 16 * f + col, rows - 1), token = row / G, head = it.head * G + row - token * G;
         pos[f] = it.sp.start + token;
-        first[f] = a.window > 0 ? pos[f] - a.window + 1 : 0;
+        first[f] = first_seen(a, pos[f]);
         const uint16_t *const p = a.q + (int64_t)(it.sp.q0 + token) * a.ldq + (int64_t)head * D + g * (D / 4);
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) q[f][s] = *reinterpret_cast<const u32x4 *>(p + 8 * s);
@@ -271,8 +277,8 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
     }
     // what every row of the item, and what any of them sees
     const int pos_lo = it.sp.start + row0 / G, pos_hi = it.sp.start + (min(row0 + kRows, rows) - 1) / G;
-    const int hi = min(it.hi, pos_hi + 1), lo = max(it.lo, a.window > 0 ? pos_lo - a.window + 1 : 0);
-    const int all_lo = a.window > 0 ? pos_hi - a.window + 1 : 0, all_hi = min(it.hi, pos_lo + 1);
+    const int hi = min(it.hi, pos_hi + 1), lo = max(it.lo, first_seen(a, pos_lo));
+    const int all_lo = first_seen(a, pos_hi), all_hi = min(it.hi, pos_lo + 1);
     bool marked = false;  // whether the wave's part of `sums` holds NaN for what rows have seen
 
     const int P = 1 << a.s.page_shift;
@@ -547,14 +553,14 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
     const int G = a.Hq / a.Hkv, rows = it.sp.n * G, tile0 = it.tile * kRows, wave0 = tile0 + 32 * wave;
     // the lane's row (rows beyond the last are computed again and not stored) and the places that it sees
     const int row = min(wave0 + col, rows - 1), token = row / G, head = it.head * G + row - token * G;
-    const int pos = it.sp.start + token, first = a.window > 0 ? pos - a.window + 1 : 0;
+    const int pos = it.sp.start + token, first = first_seen(a, pos);
     // places that any row of the workgroup sees, that any and that every row of the wave sees
     const int group_hi = min(it.hi, it.sp.start + (min(tile0 + kRows, rows) - 1) / G + 1);
-    const int group_lo = max(it.lo, a.window > 0 ? it.sp.start + tile0 / G - a.window + 1 : 0);
+    const int group_lo = max(it.lo, first_seen(a, it.sp.start + tile0 / G));
     const int pos_lo = it.sp.start + min(wave0, rows - 1) / G, pos_hi = it.sp.start + (min(wave0 + 32, rows) - 1) / G;
-    const int all_lo = max(group_lo, a.window > 0 ? pos_hi - a.window + 1 : 0), all_hi = min(group_hi, pos_lo + 1);
+    const int all_lo = max(group_lo, first_seen(a, pos_hi)), all_hi = min(group_hi, pos_lo + 1);
     // places that every row of the workgroup sees
-    const int rows_lo = max(group_lo, a.window > 0 ? it.sp.start + (min(tile0 + kRows, rows) - 1) / G - a.window + 1 : 0);
+    const int rows_lo = max(group_lo, first_seen(a, it.sp.start + (min(tile0 + kRows, rows) - 1) / G));
     const int rows_hi = min(group_hi, it.sp.start + tile0 / G + 1);
 
     bf16x8 q[D / 16];

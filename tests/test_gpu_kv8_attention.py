@@ -301,3 +301,28 @@ def test_a_pool_without_pages(D):
                                      y.data_ptr(), 4 * D, ws.data_ptr() if bytes_ else None, bytes_, torch.cuda.current_stream().cuda_stream) == 0
             assert (y == 0).all()
     assert (codes == 0x38).all() and (scales == 127).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_windows_of_lengths_beyond_the_table(D):
+    """The places of the tokens count on past the table's W * P, so that a window of that many still leaves some out."""
+    for q_lens, past, lens in (([1, 3], [60, 61], [100, 64]), ([1] * 9 + [90], [63] * 10, [64 + 8 * b for b in range(9)] + [2 ** 20]),
+                               ([70], [0], [120]), ([2], [3000], [3500])):
+        places = (max(a + b for a, b in zip(q_lens, past)) + 15) // 16 * 16
+        for window in (1, places // 2, places - 1, places, places + 1, 2 * places):
+            p = Problem(D + window, q_lens, past, 4, 2, D, 16, window)
+            assert p.pt.shape[1] * 16 == places
+            p.pt[:] = p.r.permutation(len(p.kc))[: p.pt.size].reshape(p.pt.shape) if p.pt.size <= len(p.kc) else p.r.integers(0, len(p.kc), p.pt.shape)
+            p.kc[:], p.vc[:] = (ref.e4m3_code(p.r.normal(size=p.kc.shape) * 100) for _ in "kv")
+            p.lens[:] = lens
+            p.check()
+
+
+def test_windows_larger_than_any_place():
+    import paper_2605_20315_amd as mq
+    p = Problem(30, [1, 40, 5, 90], [30, 0, 200, 70], 4, 2, 64, 16)
+    p.lens[1] = 11  # rows before the first place
+    args = p.device()
+    want = mq.kv8_attention(*args, p.scale)
+    for window in (2 ** 31 - 2, 2 ** 31 - 1, 2 ** 31, 2 ** 40, -1, -(2 ** 40)):
+        assert torch.equal(mq.kv8_attention(*args, p.scale, window).view(torch.int16), want.view(torch.int16)), window
