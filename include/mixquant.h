@@ -299,7 +299,7 @@ int nvfp4_matvec(const void *x_bf16, int64_t ldx, const uint8_t *w_codes, const 
  *
  * kv8_attention: y[t, h, :] = sum_j p_j v_j, p = softmax_j(sm_scale * (q[t, h, :] . k_j)) over the places j that token t sees:
  * 0 <= j <= pos, its own place, and j > pos - window where window > 0.  Query head h reads key head h / (Hq / Hkv).  A token that
- * sees nothing gets zeros.  Products of BF16 numbers, sums and the softmax's maxima and sums in FP32, probabilities rounded to
+ * sees nothing gets zeros (one that sees scores of -infinity alone NaN, as the formula).  Products of BF16 numbers, sums and the softmax's maxima and sums in FP32, probabilities rounded to
  * BF16 for the product with the values, y BF16 (nearest even), [T, Hq, D] with token stride ldy.  Hq % Hkv == 0, sm_scale
  * finite and > 0.  Places that no query of the call sees may hold anything.
  * workspace: as in nvfp4_gemm_ws; with mq_kv8_attention_workspace_bytes(...) bytes (at most 64 MiB; less counts as none) long

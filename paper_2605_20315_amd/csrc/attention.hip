@@ -201,6 +201,18 @@ static __device__ __forceinline__ float weight_of(float m, float l, float top)
     return m == kNone ? l : __builtin_amdgcn_exp2f(m - top);
 }
 
+// What a row's sums are multiplied by.  A sum of exponentials of zero: the row sees no place, and gives zeros, or no score above
+// -infinity, and gives NaN as the definition does.
+static __device__ __forceinline__ float inverse_of(const Kv8Attend &a, int b, const Span &sp, int pos, float total)
+{
+    if (total != 0.0f) return 1.0f / total;
+    const int32_t *const table = a.s.page_table + b * a.s.pt_ld;
+#pragma unroll 1
+    for (int place = first_seen(a, pos); place <= min(pos, sp.len - 1); place = ((place >> a.s.page_shift) + 1) << a.s.page_shift)
+        if ((unsigned)table[place >> a.s.page_shift] < (uint64_t)a.s.pages) return __builtin_nanf("");
+    return 0.0f;
+}
+
 // 0x01 in the bytes that are NaN codes
 static __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u; }
 
@@ -510,8 +522,8 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
             if ((tid & 15) == 0) p[kRows * D + r] = best, p[kRows * D + kRows + r] = total;
             continue;
         }
-        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
         const int token = row / G;
+        const float inv = inverse_of(a, it.b, it.sp, it.sp.start + token, total);
         uint32_t *const y = reinterpret_cast<uint32_t *>(a.y + (int64_t)(it.sp.q0 + token) * a.ldy + (int64_t)(it.head * G + row - token * G) * D + e0);
 #pragma unroll
         for (int e = 0; e < D / 16; e += 2) y[e / 2] = pack2(o[e] * inv, o[e + 1] * inv);
@@ -798,7 +810,7 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
     const bool split = it.chunks > 1;
     float *const part = slot_at(c, D, it.slot);
     if (split && h == 0) part[c.rows * D + local] = mb, part[c.rows * D + c.rows + local] = l;
-    const float inv = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv = split ? 1.0f : inverse_of(a, it.b, it.sp, pos, l);
     uint16_t *const y = a.y + (int64_t)(it.sp.q0 + token) * a.ldy + (int64_t)head * D;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -907,7 +919,7 @@ __global__ __launch_bounds__(256) void attend_join(Kv8Attend a, Cut c)
     } else if (h0 + part >= a.Hq) {
         return;
     }
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const float inv = inverse_of(a, b, sp, sp.start + t - sp.q0, total);
     *reinterpret_cast<u32x2 *>(a.y + (int64_t)t * a.ldy + (int64_t)h * D + 4 * col) = u32x2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
 }
 

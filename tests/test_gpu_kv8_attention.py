@@ -326,3 +326,17 @@ def test_windows_larger_than_any_place():
     want = mq.kv8_attention(*args, p.scale)
     for window in (2 ** 31 - 2, 2 ** 31 - 1, 2 ** 31, 2 ** 40, -1, -(2 ** 40)):
         assert torch.equal(mq.kv8_attention(*args, p.scale, window).view(torch.int16), want.view(torch.int16)), window
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_rows_whose_scores_are_all_minus_infinity_are_nan(D):
+    """As their softmax is; rows that see no place stay zero, and all others are what they are."""
+    for q_lens, past, window in (([1, 1, 4], [0, 200, 40], 0), ([1, 2, 1], [5000, 3, 300], 0), ([40, 90, 5], [2600, 10, 0], 0), ([3, 70], [90, 100], 20),
+                                 ([1] * 9 + [130], list(range(0, 900, 100)) + [2600], 0)):
+        p = Problem(D + len(q_lens), q_lens, past, 4, 2, D, 16, window)
+        p.kc[..., 5] = np.where((p.kc[..., 5] & 127) == 127, p.kc[..., 5], p.kc[..., 5] & 127 | 8)  # positive, and zero nowhere
+        p.q[::2, 1, 5] = p.q[1::3, 2, 5] = -np.inf
+        p.lens[1] = min(p.lens[1], q_lens[1] - 1) if q_lens[1] > 1 else p.lens[1]  # its first row sees nothing
+        with np.errstate(invalid="ignore"):
+            assert np.isnan(p.reference()[0]).any()
+            p.check()
