@@ -303,7 +303,7 @@ int nvfp4_matvec(const void *x_bf16, int64_t ldx, const uint8_t *w_codes, const 
  * BF16 for the product with the values, y BF16 (nearest even), [T, Hq, D] with token stride ldy.  Hq % Hkv == 0, sm_scale
  * finite and > 0.  Places that no query of the call sees may hold anything.
  * workspace: as in nvfp4_gemm_ws; with mq_kv8_attention_workspace_bytes(...) bytes (at most 64 MiB; less counts as none) long
- * histories are cut across workgroups, and a second kernel adds the parts in ascending order: bit-identical from run to run.
+ * histories are cut across workgroups where the call has too few of them to fill the GPU twice, and a second kernel adds the parts in ascending order: bit-identical from run to run.
  */
 typedef enum {
     MQ_ROPE_PLAIN = 0,

@@ -948,28 +948,49 @@ struct Launch {
     int64_t items;
 };
 
+constexpr int kManyRows = 32 * kManyWaves;
+
+// Tiles of rows at most, over sequences of more than cut.above and at most cut.most rows with T tokens in all: the host knows no
+// sequence's own length.  A tile begun by every sequence; none that a token has not; where sequences of more rows are another kernel's,
+// what their own rows fill; and where those of fewer are, the most that a row can count for, two tiles of kManyRows + 1 rows.
+static int64_t row_tiles_most(const Cut &cut, int64_t T, int64_t B, int64_t G)
+{
+    static_assert(2 * (kFewMost + 1) >= kManyRows + 1, "one tile of kFewMost + 1 rows counts for less");
+    int64_t most = std::min(T * G / cut.rows + B, T * ((G + cut.rows - 1) / cut.rows));
+    if (cut.most < INT32_MAX) most = std::min(most, B * ((cut.most + cut.rows - 1) / cut.rows));
+    if (cut.above > 0) most = std::min(most, 2 * T * G / (kManyRows + 1));
+    return most;
+}
+
 static int plan_attention(const Kv8Attend &a, Launch *out)
 {
-    constexpr int kManyRows = 32 * kManyWaves;
     const int D = a.D;
     const int64_t G = a.Hq / a.Hkv, T = a.s.T, B = a.s.B;
     const bool ws = a.ws && a.ws_bytes >= kWorkspace && B <= kPartsMost;
     int n = 0;
     // If every sequence has a token, none has more than T - B + 1 of them, and where there are few tokens a sequence (a decode
     // batch, drafted tokens among it) a second kernel that finds nothing to do costs more than a longer prompt loses in
-    // attend_few.  (Every split of the work is right: it is only slower than it need be.)  Up to kAllMany sequences attend_many takes
-    // all if it takes any.
+    // attend_few.  (Every split of the work is right: it is only slower than it need be.  A batch on that side of the line with one
+    // chunk of 512 after 100000 among 200 single tokens takes 2.1 ms.)  Up to kAllMany sequences attend_many takes all if it takes any: with
+    // short histories that saves two launches (300 tokens beside 7 single ones after 500 to 2000: 32 us, 50 by two kernels; two
+    // prompts of 100 beside 6 after 500 to 1000: 22 and 36; 512 beside one after 20000: 43 and 67), deep ones pay for tiles of 128 rows with few
+    // in them (1024 beside 7 after 100000: 630 us, 325 by two kernels; 512 beside 3 after 50000: 141 and 101).  All with heads of 128, 32 on 8.
     const bool many = T > 4 * B && (T - B + 1) * G > kFewMost, few = !many || B > kAllMany;
     auto add = [&](bool is_many, int rows, int most_items, int least, int above, int most) {
         Cut cut{rows, target_of(most_items, rows, D), least, above, most, true, is_many, a.ws, slots_of(rows, D)};
         // An item for each tile of rows and key head; where sequences are cut, as many more as the target has, or as their
-        // longest possible history has chunks
-        const int64_t whole = (T * G / cut.rows + B) * a.Hkv, tiles = ((int64_t)a.s.width << a.s.page_shift) / kTile + 1;
+        // longest possible history has chunks.  (2048 tokens beside 8 single ones after 100000 take 1056 us if those are not cut, 387 so;
+        // 190 single tokens, one of them after 131000, 803 and 197.)
+        const int64_t whole = row_tiles_most(cut, T, B, G) * a.Hkv, tiles = ((int64_t)a.s.width << a.s.page_shift) / kTile + 1;
         cut.split = ws && whole < 2 * cut.target && tiles >= 2 * cut.least;
         out[n++] = Launch{is_many, cut, cut.split ? std::min(whole + 2 * cut.target, whole * (tiles / cut.least + 1)) : whole};
     };
-    // (heads of 256 have no registers for two tiles)
-    if (few) add(false, D <= 128 && T * G > B * kFewRows ? 2 * kFewRows : kFewRows, kFewTarget, 2, 0, many ? kFewMost : INT32_MAX);
+    // Two tiles of rows from one expansion where the average sequence has more than one; beside attend_many, whose tokens are most
+    // of T, by the rows of a single token (2048 beside 8 single tokens after 100000: 387 us with one tile, 418 with two; 600 beside 30
+    // after 1000 to 5000, heads of 64: 67 and 75; but 512 beside 40 times 13 drafted ones after 10000: 326 and 297).  Heads of 256 have no
+    // registers for two.
+    const bool two = D <= 128 && (many ? G > kFewRows : T * G > B * kFewRows);
+    if (few) add(false, two ? 2 * kFewRows : kFewRows, kFewTarget, 2, 0, many ? kFewMost : INT32_MAX);
     if (many) add(true, kManyRows, many_target(D), 4, few ? kFewMost : 0, INT32_MAX);
     return n;
 }

@@ -340,3 +340,14 @@ def test_rows_whose_scores_are_all_minus_infinity_are_nan(D):
         with np.errstate(invalid="ignore"):
             assert np.isnan(p.reference()[0]).any()
             p.check()
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 2, 64), (8, 2, 128), (2, 1, 256), (20, 1, 128)])
+def test_deep_histories_beside_a_prompt(Hq, Hkv, D):
+    """More than eight sequences: two kernels, both of which cut histories."""
+    import paper_2605_20315_amd as mq
+    q_lens, past = [150] + [1, 2, 1, 3, 1, 1, 1, 1, 1, 0, 1], [2000, 3000, 1700, 0, 2600, 1, 90, 64, 2048, 31, 5, 1000]
+    p = Problem(D, q_lens, past, Hq, Hkv, D, 16)
+    plan = mq.mq_kv8_attention_launches(len(p.kc), 16, Hq, Hkv, D, p.pt.shape[1], len(q_lens), sum(q_lens), 64 << 20)
+    assert [x["kernel"] for x in plan] == ["few", "many"] and all(x["cut"] for x in plan)
+    p.check()
