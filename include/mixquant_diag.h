@@ -42,7 +42,9 @@ typedef enum {
     MQ_KERNEL_BF16_RING = 3,
     MQ_KERNEL_BF16_STAGE = 4,
     MQ_KERNEL_BF16_D2L = 5,
-    MQ_KERNEL_BF16_SHORT = 6
+    MQ_KERNEL_BF16_SHORT = 6,
+    MQ_KERNEL_MATVEC = 7,     /* activations packed by a kernel in front */
+    MQ_KERNEL_MATVEC_LDS = 8  /* by every workgroup for itself */
 } mq_kernel;
 typedef struct {
     int kernel, bm, bn, waves, slabs;
@@ -50,6 +52,9 @@ typedef struct {
 } mq_launch;
 int mq_gemm_launches(int64_t M, int64_t N, int64_t K, int layout, int64_t workspace_bytes, int cus, mq_launch out[2]);
 int mq_bf16_gemm_launches(int64_t M, int64_t N, int64_t K, int64_t workspace_bytes, int cus, mq_launch out[2]);
+
+/* nvfp4_matvec: one launch (beside its packing and joining kernels), bm tokens x bn rows of W a workgroup. */
+int mq_nvfp4_matvec_launches(int64_t M, int64_t N, int64_t K, mq_launch out[1]);
 
 /* kv8_attention for these sizes: the kernel (MQ_KV8_FEW: tiles of 16 or 32 rows, MQ_KV8_MANY: of 128; a row is a query head of a
  * token), its rows a tile, whether it may cut histories into chunks (a kernel that joins them follows then), its workgroups, and the

@@ -96,6 +96,8 @@ def load() -> ctypes.CDLL:
     lib.mq_gemm_launches.argtypes = [i64, i64, i64, ci, i64, ci, ctypes.POINTER(Launch)]
     lib.mq_bf16_gemm_launches.restype = ci
     lib.mq_bf16_gemm_launches.argtypes = [i64, i64, i64, i64, ci, ctypes.POINTER(Launch)]
+    lib.mq_nvfp4_matvec_launches.restype = ci
+    lib.mq_nvfp4_matvec_launches.argtypes = [i64, i64, i64, ctypes.POINTER(Launch)]
     lib.mq_kv8_attention_launches.restype = ci
     lib.mq_kv8_attention_launches.argtypes = [i64, ci, ci, ci, ci, i64, i64, i64, i64, ctypes.POINTER(Kv8Launch)]
     lib.mq_quantize_rows.restype = ci

@@ -476,6 +476,13 @@ int mq_bf16_gemm_launches(int64_t M, int64_t N, int64_t K, int64_t workspace_byt
     return M == 0 || N == 0 ? 0 : describe_gemm_bf16(M, N, K, workspace_bytes, cus, out);
 }
 
+int mq_nvfp4_matvec_launches(int64_t M, int64_t N, int64_t K, mq_launch out[1])
+{
+    if (!out) return -MQ_ERR_NULL;
+    if (M < 0 || M > 65535 || N < 0 || N > 0x7fffffff || K <= 0 || K > 0x7fffffff || K % kBlock != 0) return -MQ_ERR_SHAPE;
+    return M == 0 || N == 0 ? 0 : describe_nvfp4_matvec(M, N, K, out);
+}
+
 int mq_kv8_attention_launches(int64_t pages, int P, int Hq, int Hkv, int D, int64_t W, int64_t B, int64_t T, int64_t workspace_bytes,
                               mq_kv8_launch out[2])
 {

@@ -61,6 +61,7 @@ int describe_kv8_attention(const Kv8Attend &a, mq_kv8_launch *out);  // what the
 int64_t kv8_attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D);
 int launch_nvfp4_matvec(const uint16_t *x, int64_t ldx, const uint8_t *codes, const uint8_t *scales, const float *alpha, int64_t M,
                         int64_t N, int64_t K, void *y, int64_t ldy, int out, int layout, void *ws, hipStream_t s);
+int describe_nvfp4_matvec(int64_t M, int64_t N, int64_t K, mq_launch *out);
 int64_t matvec_workspace(int64_t M, int64_t N, int64_t K);
 int configure_matvec_kernels();
 

@@ -358,6 +358,19 @@ int64_t matvec_workspace(int64_t M, int64_t N, int64_t K)
     return packed_bytes(M, K) + 16 * ((M + 3) / 4) + (slabs > 1 ? 4 * slabs * M * N : 0);
 }
 
+int describe_nvfp4_matvec(int64_t M, int64_t N, int64_t K, mq_launch *out)
+{
+    if (K % 64) {
+        *out = mq_launch{MQ_KERNEL_SIMPLE, 1, 1, 1, 1, M, N};
+    } else if (in_lds(M, N, K)) {
+        *out = mq_launch{MQ_KERNEL_MATVEC_LDS, 16, is_wide(N) ? 64 : 16, is_wide(N) ? 4 : 8, 1, M, N};
+    } else {
+        const Split split = split_of(M, N, K);
+        *out = mq_launch{MQ_KERNEL_MATVEC, 16 * (int)std::min<int64_t>((M + 15) / 16, 4), 16 * split.strips, 4, split.slabs, M, N};
+    }
+    return 1;
+}
+
 template <bool LDS, int MT, int S, int NW>
 static int launch(const MatvecArgs &a, hipStream_t s)
 {
@@ -365,7 +378,6 @@ static int launch(const MatvecArgs &a, hipStream_t s)
     const int64_t lds = LDS ? a.M * ((a.K + 127) / 128) * 256 : 0;
     return enqueue(matvec_kernel<LDS, MT, S, NW>, dim3((unsigned)strips, (unsigned)tokens, (unsigned)a.slabs), dim3(64 * NW), (size_t)lds, s, a);
 }
-
 
 int configure_matvec_kernels()
 {

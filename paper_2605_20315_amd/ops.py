@@ -479,7 +479,7 @@ def mfma_probe(iters: int = 4000) -> float:
     return flop.value
 
 
-KERNEL_NAMES = ("simple", "fp4_direct", "fp4_small", "bf16_ring", "bf16_stage", "bf16_d2l", "bf16_short")
+KERNEL_NAMES = ("simple", "fp4_direct", "fp4_small", "bf16_ring", "bf16_stage", "bf16_d2l", "bf16_short", "matvec", "matvec_lds")
 
 
 def _launches(n: int, out) -> list:
@@ -500,6 +500,12 @@ def mq_bf16_gemm_launches(M: int, N: int, K: int, workspace_bytes: int = 0, comp
     """What the BF16 product launches for this problem (host only)."""
     got = (_lib.Launch * 2)()
     return _launches(_lib.load().mq_bf16_gemm_launches(M, N, K, workspace_bytes, compute_units, got), got)
+
+
+def mq_nvfp4_matvec_launches(M: int, N: int, K: int) -> list:
+    """What nvfp4_matvec launches for this problem beside its packing and joining kernels (host only)."""
+    got = (_lib.Launch * 1)()
+    return _launches(_lib.load().mq_nvfp4_matvec_launches(M, N, K, got), got)
 
 
 def mq_kv8_attention_launches(pages: int, P: int, Hq: int, Hkv: int, D: int, W: int, B: int, T: int, workspace_bytes: int = 0) -> list:
