@@ -810,7 +810,8 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
     const bool split = it.chunks > 1;
     float *const part = slot_at(c, D, it.slot);
     if (split && h == 0) part[c.rows * D + local] = mb, part[c.rows * D + c.rows + local] = l;
-    const float inv = split ? 1.0f : inverse_of(a, it.b, it.sp, pos, l);
+    // (the item is read from LDS again: kept through the loop it spills 16 more scalar registers, 595 us for the long prompt's 591)
+    const float inv = split ? 1.0f : inverse_of(a, plan.found.b, plan.found.sp, pos, l);
     uint16_t *const y = a.y + (int64_t)(it.sp.q0 + token) * a.ldy + (int64_t)head * D;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
