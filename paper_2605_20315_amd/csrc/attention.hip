@@ -28,7 +28,8 @@ struct Cut {
     int rows, target, least, above, most;
     bool split, fit;
     float *ws;
-    int slots;  // that the workspace holds
+    int slots;   // that the workspace holds
+    int tokens;  // attend_join goes by sequences of at most so many tokens; 0: by the call's tokens
 };
 
 struct Item {
@@ -868,22 +869,28 @@ __global__ __launch_bounds__(256) void attend_join(Kv8Attend a, Cut c)
     __shared__ float tops[4], totals[kParts];
     __shared__ f32x4 sums[kParts][kCols];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = tid % kCols, part = tid / kCols;
-    const int per = ROWS ? kParts : 1, groups = (a.Hq + per - 1) / per, t = blockIdx.x / groups, h0 = (blockIdx.x - t * groups) * per;
-    int b = 0;  // sequences that end at or before t
-    for (int base = 0; base < a.s.B; base += 256) {
-        int done = 0;
+    const int per = ROWS ? kParts : 1, groups = (a.Hq + per - 1) / per, unit = blockIdx.x / groups, h0 = (blockIdx.x - unit * groups) * per;
+    int b = 0, t = unit;
+    if (c.tokens > 0) {
+        b = unit / c.tokens;
+    } else {
+        // sequences that end at or before t
+        for (int base = 0; base < a.s.B; base += 256) {
+            int done = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int i = base + 64 * k + lane;
-            done += __popcll(__ballot(i < a.s.B && a.s.cu_q[min(i, a.s.B - 1) + 1] <= t));
+            for (int k = 0; k < 4; ++k) {
+                const int i = base + 64 * k + lane;
+                done += __popcll(__ballot(i < a.s.B && a.s.cu_q[min(i, a.s.B - 1) + 1] <= t));
+            }
+            b += done;
+            if (done < 256) break;
         }
-        b += done;
-        if (done < 256) break;
+        if (b >= a.s.B) return;
     }
-    if (b >= a.s.B) return;
     const Parts parts = reinterpret_cast<const Parts *>(c.ws)[b];
     if (parts.chunks < 2 || parts.slot < 0 || (int64_t)parts.slot + (int64_t)parts.chunks * parts.row_tiles * a.Hkv > c.slots) return;
     const Span sp = span_of(a.s, b);
+    if (c.tokens > 0) t = sp.q0 + unit - b * c.tokens;
     if (t < sp.q0 || t >= sp.q0 + sp.n) return;
     const int G = a.Hq / a.Hkv, h = ROWS ? min(h0 + part, a.Hq - 1) : h0;
     const int kv = h / G, row = (t - sp.q0) * G + h - kv * G, tile = row / c.rows, r = row - tile * c.rows;
@@ -952,12 +959,13 @@ struct Launch {
 constexpr int kManyRows = 32 * kManyWaves;
 
 // Tiles of rows at most, over sequences of more than cut.above and at most cut.most rows with T tokens in all: the host knows no
-// sequence's own length.  A tile begun by every sequence; none that a token has not; where sequences of more rows are another kernel's,
-// what their own rows fill; and where those of fewer are, the most that a row can count for, two tiles of kManyRows + 1 rows.
+// sequence's own length.  A tile begun by every sequence; where sequences of more rows are another kernel's, what their own rows fill; and
+// where those of fewer are, the most that a row can count for, two tiles of kManyRows + 1 rows.  (2048 tokens beside 8
+// single ones after 100000: 1056 us when the prompt's rows counted for attend_few and kept it from cutting, 405 so.)
 static int64_t row_tiles_most(const Cut &cut, int64_t T, int64_t B, int64_t G)
 {
     static_assert(2 * (kFewMost + 1) >= kManyRows + 1, "one tile of kFewMost + 1 rows counts for less");
-    int64_t most = std::min(T * G / cut.rows + B, T * ((G + cut.rows - 1) / cut.rows));
+    int64_t most = T * G / cut.rows + B;
     if (cut.most < INT32_MAX) most = std::min(most, B * ((cut.most + cut.rows - 1) / cut.rows));
     if (cut.above > 0) most = std::min(most, 2 * T * G / (kManyRows + 1));
     return most;
@@ -975,23 +983,30 @@ static int plan_attention(const Kv8Attend &a, Launch *out)
     // chunk of 512 after 100000 among 200 single tokens takes 2.1 ms.)  Up to kAllMany sequences attend_many takes all if it takes any: with
     // short histories that saves two launches (300 tokens beside 7 single ones after 500 to 2000: 32 us, 50 by two kernels; two
     // prompts of 100 beside 6 after 500 to 1000: 22 and 36; 512 beside one after 20000: 43 and 67), deep ones pay for tiles of 128 rows with few
-    // in them (1024 beside 7 after 100000: 630 us, 325 by two kernels; 512 beside 3 after 50000: 141 and 101).  All with heads of 128, 32 on 8.
+    // in them (1024 beside 7 after 100000: 630 us, 330 by two kernels; 512 beside 3 after 50000: 140 and 110).  All with heads of 128, 32 on 8.
     const bool many = T > 4 * B && (T - B + 1) * G > kFewMost, few = !many || B > kAllMany;
     auto add = [&](bool is_many, int rows, int most_items, int least, int above, int most) {
-        Cut cut{rows, target_of(most_items, rows, D), least, above, most, true, is_many, a.ws, slots_of(rows, D)};
+        Cut cut{rows, target_of(most_items, rows, D), least, above, most, true, is_many, a.ws, slots_of(rows, D), 0};
+        // Beside attend_many the sequences of attend_few have few tokens each, and most of the call's are not theirs (2048 beside 20
+        // single ones after 300: 106 us, 108 with a join over all tokens)
+        const int64_t tokens = std::max<int64_t>(kFewMost / G, 1);
+        if (most < INT32_MAX && B * tokens < T) cut.tokens = (int)tokens;
         // An item for each tile of rows and key head; where sequences are cut, as many more as the target has, or as their
-        // longest possible history has chunks.  (2048 tokens beside 8 single ones after 100000 take 1056 us if those are not cut, 387 so;
-        // 190 single tokens, one of them after 131000, 803 and 197.)
+        // longest possible history has chunks.  None are cut where there are twice as many items as the GPU has places: looking for
+        // them and the join cost more than they give in a batch without very uneven lengths (170 single tokens after 200 to 300, 8 key
+        // heads: 27 us, 37 if they may be cut; after 2000 126 and 130; but 190 with one after 131000 803 and 197).
         const int64_t whole = row_tiles_most(cut, T, B, G) * a.Hkv, tiles = ((int64_t)a.s.width << a.s.page_shift) / kTile + 1;
         cut.split = ws && whole < 2 * cut.target && tiles >= 2 * cut.least;
         out[n++] = Launch{is_many, cut, cut.split ? std::min(whole + 2 * cut.target, whole * (tiles / cut.least + 1)) : whole};
     };
-    // Two tiles of rows from one expansion where the average sequence has more than one; beside attend_many, whose tokens are most
-    // of T, by the rows of a single token (2048 beside 8 single tokens after 100000: 387 us with one tile, 418 with two; 600 beside 30
-    // after 1000 to 5000, heads of 64: 67 and 75; but 512 beside 40 times 13 drafted ones after 10000: 326 and 297).  Heads of 256 have no
-    // registers for two.
-    const bool two = D <= 128 && (many ? G > kFewRows : T * G > B * kFewRows);
-    if (few) add(false, two ? 2 * kFewRows : kFewRows, kFewTarget, 2, 0, many ? kFewMost : INT32_MAX);
+    // Two tiles of rows from one expansion where the average sequence has more than one: 64 times 5 drafted tokens after 100 to 8000
+    // 150 us, 178 with one tile; 40 times 13 after 10000 255 and 312; but 64 times 4 129 and 121.  A prompt in the batch raises the average
+    // for the single tokens beside it, which then lose by it what drafted ones would gain: 2048 beside 8 after 100000 412 and 381, 512
+    // beside 40 times 13 296 and 324.  Heads of 256 have no registers for two.
+    const bool two = D <= 128 && T * G > B * kFewRows;
+    // Chunks of 8 tiles at least beside attend_many, whose own time hides longer ones (600 beside 40 after 200: 47 us, 62 with 2 tiles; 1000
+    // beside 12 after 1000: 60 and 68; the same with deep histories; uncut these two take 66 and 74)
+    if (few) add(false, two ? 2 * kFewRows : kFewRows, kFewTarget, many ? 8 : 2, 0, many ? kFewMost : INT32_MAX);
     if (many) add(true, kManyRows, many_target(D), 4, few ? kFewMost : 0, INT32_MAX);
     return n;
 }
@@ -1015,7 +1030,7 @@ static int launch_attention(const Kv8Attend &a, hipStream_t s)
         if (rc) return rc;
         if (!p.cut.split) continue;
         constexpr int kPer = 1024 / D;
-        const int64_t T = a.s.T;
+        const int64_t T = p.cut.tokens ? (int64_t)a.s.B * p.cut.tokens : a.s.T;
         rc = T * a.Hq >= 2048 ? enqueue(attend_join<D, true>, dim3((unsigned)(T * ((a.Hq + kPer - 1) / kPer))), dim3(256), 0, s, a, p.cut)
                               : enqueue(attend_join<D, false>, dim3((unsigned)(T * a.Hq)), dim3(256), 0, s, a, p.cut);
         if (rc) return rc;

@@ -34,17 +34,24 @@ def test_deep_histories_beside_a_prompt_are_cut(D):
     """A prompt's tokens count for the kernel that takes them, not for the one that takes the single tokens beside it."""
     for T, B in ((2048 + 8, 9), (2048 + 30, 31), (8192 + 20, 21), (300 + 9, 10)):
         p = _by_kernel(10 ** 6, 64, 32, 8, D, 2048, B, T, FULL)
-        assert p["few"]["cut"] and p["few"]["rows"] == 16, (T, B)
+        assert p["few"]["cut"], (T, B)
         assert p["few"]["workgroups"] <= B * 4 * 8 + 2 * 768
     # and the single tokens do not count for the prompt's
     assert _by_kernel(10 ** 6, 64, 32, 8, D, 2048, 200, 1000, FULL)["many"]["cut"]
 
 
-def test_a_batch_of_single_tokens_counts_one_item_for_each_and_key_head():
-    for B in (1, 64, 150, 191):
-        few = _by_kernel(10 ** 6, 64, 32, 8, 128, 2048, B, B, FULL)["few"]
-        assert few["cut"] and _by_kernel(10 ** 6, 64, 32, 8, 128, 2048, B, B, 0)["few"]["workgroups"] == B * 8
-    assert not _by_kernel(10 ** 6, 64, 32, 8, 128, 2048, 192, 192, FULL)["few"]["cut"]
+def test_large_batches_of_single_tokens_are_not_cut():
+    for B in (1, 64, 150, 153):
+        assert _by_kernel(10 ** 6, 64, 32, 8, 128, 2048, B, B, FULL)["few"]["cut"]
+    for B in (154, 170, 191, 300):  # timed: 3 to 10 us more with the join, which finds nothing to do where lengths are alike
+        assert not _by_kernel(10 ** 6, 64, 32, 8, 128, 2048, B, B, FULL)["few"]["cut"]
+
+
+def test_two_tiles_of_rows_where_the_average_sequence_has_more_than_one():
+    # timed: 64 sequences of 4 tokens with four query heads a key head 121 us with one tile, of 5 tokens 150 with two
+    for tokens, rows in ((1, 16), (4, 16), (5, 32), (13, 32)):
+        assert _by_kernel(10 ** 5, 64, 32, 8, 128, 200, 64, 64 * tokens, FULL)["few"]["rows"] == rows
+        assert _by_kernel(10 ** 5, 64, 32, 8, 256, 200, 64, 64 * tokens, FULL)["few"]["rows"] == 16
 
 
 def test_every_tile_of_rows_has_a_workgroup():
