@@ -35,8 +35,8 @@
  *    alpha  : one float           the tensor-level scale
  * with value x_hat[r, k] = alpha * E4M3(scales[r, k/16]) * E2M1(code[r, k])   (Eq. 1, right).
  * Scale bytes are what Eq. 2 produces: non-negative and finite, 0x00 .. 0x7E.  The quantizers
- * emit nothing else; nvfp4_gemm given a byte with the sign bit set or the NaN pattern 0x7F
- * returns unspecified values for the outputs that the block touches (never a fault).
+ * emit nothing else; the products (nvfp4_gemm, nvfp4_matvec) given a byte with the sign bit set or the NaN
+ * pattern 0x7F return unspecified values for the outputs that the block touches (never a fault).
  */
 #ifndef MIXQUANT_H
 #define MIXQUANT_H
@@ -301,7 +301,9 @@ int nvfp4_matvec(const void *x_bf16, int64_t ldx, const uint8_t *w_codes, const 
  * 0 <= j <= pos, its own place, and j > pos - window where window > 0.  Query head h reads key head h / (Hq / Hkv).  A token that
  * sees nothing gets zeros (one that sees scores of -infinity alone NaN, as the formula).  Products of BF16 numbers, sums and the softmax's maxima and sums in FP32, probabilities rounded to
  * BF16 for the product with the values, y BF16 (nearest even), [T, Hq, D] with token stride ldy.  Hq % Hkv == 0, sm_scale
- * finite and > 0.  Places that no query of the call sees may hold anything.
+ * finite and > 0.  Places that no query of the call sees may hold anything.  The sums of p_j v_j are divided by the sum of
+ * exponentials at the end: where the magnitudes of a row's values add up to 2^119 or more they may overflow, and scores are to stay
+ * below 2^30 in magnitude.
  * workspace: as in nvfp4_gemm_ws; with mq_kv8_attention_workspace_bytes(...) bytes (at most 64 MiB; less counts as none) long
  * histories are cut across workgroups where the call has too few of them to fill the GPU twice, and a second kernel adds the parts in ascending order: bit-identical from run to run.
  */

@@ -12,6 +12,14 @@
 // chunk lengths chosen on the device from the sequences' own lengths so that the items are about `target` (a batch of uneven
 // lengths is cut evenly, and the host needs to know no lengths).  A sequence with several chunks leaves its partial sums in
 // the workspace, and attend_join adds them in ascending order.
+//
+// Roundings.  Codes times page scales are BF16 numbers exactly, and scores, maxima, sums and the output's sums are binary32.  The
+// probabilities are rounded to BF16 for the product with the values, 2^-8 of each at most, since a value with its page's
+// exponent (-112 .. 119) fits no 16-bit operand but BF16, and both operands of a product are of one type: a prompt of 8192 is
+// 0.0020 from 64 bits so, where a result whose only rounding is its own is 0.0016 (single tokens: 0.0017 and 0.0017).  The sum they are divided
+// by is of the unrounded ones.
+// Ranges.  The output's sums are not divided before the end: with values of 2^119 over the number of places seen and more they may
+// overflow.  Scores beyond 2^30 leave less of the exponential of a row's own maximum than 32 bits hold.
 #include "kv8.h"
 
 namespace mq {
@@ -935,8 +943,9 @@ __global__ __launch_bounds__(256) void attend_join(Kv8Attend a, Cut c)
 
 constexpr int64_t kWorkspace = (int64_t)64 << 20;
 // Items aimed at: as many workgroups as the GPU holds at a time (attend_few, which is bound by memory, half as many more: when a
-// batch of uneven lengths took 124 us so, it took 136 with one round; two long sequences 92 and 89), of which those of sequences that are cut
-// are less than twice as many, and the workspace has to have slots for them.
+// batch of uneven lengths took 124 us so, it took 136 with one round; two long sequences 92 and 89), but no more than half of the slots that
+// the workspace holds, since the items of the sequences that are cut are less than twice as many.  For attend_many that is less than the
+// GPU's places: 496 of 512 with heads of 128, 250 of 256 with heads of 256 (with heads of 64 the places, 768).
 constexpr int kFewTarget = 768;
 // workgroups of attend_many that a compute unit holds, by registers and LDS: three, two and one
 static int many_target(int D) { return 256 * (D == 64 ? 3 : D == 128 ? 2 : 1); }

@@ -446,7 +446,9 @@ def kv8_attention(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tensor
                   page_table: torch.Tensor, cu_q: torch.Tensor, kv_lens: torch.Tensor, sm_scale: float, window: int = 0,
                   y: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Causal attention of q [T, Hq, D], the last tokens of their sequences, over the paged FP8 cache; BF16 [T, Hq, D].
-    window > 0: a token sees itself and the window - 1 places before it.  workspace: any contiguous GPU tensor, or None."""
+    window > 0: a token sees itself and the window - 1 places before it.  workspace: any contiguous GPU tensor of
+    mq_kv8_attention_workspace_bytes; without one (None, or a smaller one) no history is cut across workgroups, and one long sequence
+    is read by as many workgroups as it has key heads."""
     done = _fast.attention(q, k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, sm_scale, window, y, workspace)
     if done is not None:
         return done
