@@ -299,13 +299,14 @@ int nvfp4_matvec(const void *x_bf16, int64_t ldx, const uint8_t *w_codes, const 
  *
  * kv8_attention: y[t, h, :] = sum_j p_j v_j, p = softmax_j(sm_scale * (q[t, h, :] . k_j)) over the places j that token t sees:
  * 0 <= j <= pos, its own place, and j > pos - window where window > 0.  Query head h reads key head h / (Hq / Hkv).  A token that
- * sees nothing gets zeros (one that sees scores of -infinity alone NaN, as the formula).  Products of BF16 numbers, sums and the softmax's maxima and sums in FP32, probabilities rounded to
- * BF16 for the product with the values, y BF16 (nearest even), [T, Hq, D] with token stride ldy.  Hq % Hkv == 0, sm_scale
- * finite and > 0.  Places that no query of the call sees may hold anything.  The sums of p_j v_j are divided by the sum of
- * exponentials at the end: where the magnitudes of a row's values add up to 2^119 or more they may overflow, and scores are to stay
- * below 2^30 in magnitude.
+ * sees nothing gets zeros (one that sees scores of -infinity alone NaN, as the formula).  Products of BF16 numbers, sums and the
+ * softmax's maxima and sums in FP32, probabilities rounded to BF16 for the product with the values, y BF16 (nearest even),
+ * [T, Hq, D] with token stride ldy.  Hq % Hkv == 0, sm_scale finite and > 0.  Places that no query of the call sees may hold
+ * anything.  The sums of p_j v_j are divided by the sum of exponentials at the end: where the magnitudes of a row's values add up
+ * to 2^119 or more they may overflow, and scores are to stay below 2^30 in magnitude.
  * workspace: as in nvfp4_gemm_ws; with mq_kv8_attention_workspace_bytes(...) bytes (at most 64 MiB; less counts as none) long
- * histories are cut across workgroups where the call has too few of them to fill the GPU twice, and a second kernel adds the parts in ascending order: bit-identical from run to run.
+ * histories are cut across workgroups where the call has too few of them to fill the GPU twice, and a second kernel adds the
+ * parts in ascending order: bit-identical from run to run.
  */
 typedef enum {
     MQ_ROPE_PLAIN = 0,
