@@ -56,7 +56,7 @@ typedef enum {
     MQ_ERR_ARG = 4,    /* unknown enum value */
     MQ_ERR_HIP = 5,    /* kernel launch failed; see mq_last_hip_error() */
     MQ_ERR_SCRATCH = 6 /* nvfp4_gemm_noalloc: the problem wants more scratch than its static array holds;
-                          nvfp4_matvec: than the workspace holds */
+                          nvfp4_matvec, mq_sample: than the workspace holds */
 } mq_status;
 
 typedef enum {
@@ -324,6 +324,64 @@ int kv8_attention(const void *q_bf16, int64_t ldq, const uint8_t *k_codes, const
                   const uint8_t *v_scales, int64_t pages, int P, int Hq, int Hkv, int D, const int32_t *page_table, int64_t pt_ld,
                   int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T, float sm_scale, int64_t window,
                   void *y, int64_t ldy, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Decoding with drafted tokens over the same cache.  A drafter proposes a tree of tokens for each sequence; the model takes all of
+ * them in one step, as the sequence's new tokens, and the path that its own choices confirm is kept.  One round, all of it on
+ * the device:
+ *    mq_draft_tree, then in every layer kv8_append (with the positions) and kv8_tree_attention, the logits of every
+ *    token, mq_sample, mq_draft_accept, and in every layer kv8_compact.
+ * cu_q and kv_lens as above: the new tokens are counted in kv_lens, and `start` is the first one's place, kv_lens[b] - n.  A token's
+ * number is its place among its sequence's new ones.  parents: int32 [T], each the number of an earlier token of the sequence;
+ * anything else (-1) makes a root.  Usually token 0 is the last one that was kept, and the root of all others.  int32 arrays 4-byte aligned.
+ *
+ * mq_draft_tree: tree [T, words] (dense): bit j % 32 of word j / 32 of a token is set where token number j is the token itself or above it,
+ * and, where window > 0, fewer than `window` levels above.  positions [T]: start + the number of tokens above it.  1 <= words <= 32.  A
+ * token whose own number is 32 * words or more gets no bits and its place as position.
+ *
+ * kv8_tree_attention: kv8_attention, but that of the new tokens a token sees those whose bits in its row of `tree` are set (none from
+ * number 32 * words on), itself among them only if its bit is; and of the places before `start` all or, where window > 0, those
+ * j > position - window.  positions: int32 [T], or NULL for the tokens' places; one below `start` counts as `start`.  Rows that see nothing,
+ * precision, requirements and workspace as there.
+ *
+ * mq_sample: tokens[r] from row r of the logits [rows, V], BF16 or FP32 (type: MQ_OUT_BF16 or MQ_OUT_FP32), row stride ld >= V elements,
+ * aligned to their elements.  The tokens of a row are ordered by falling logit, the lower index first among equals; w = exp((logit -
+ * largest) / temperature).  Kept are the first top_k (all where top_k <= 0), of those the ones with less than top_p times their mass in
+ * front of them (all where top_p >= 1), and of those the ones with w >= min_p (all where min_p <= 0); the first of the order always.  The
+ * result is the lowest index up to which (and with it) the kept tokens' mass is more than uniform[r] times that of all kept ones; a draw of 1 or more counts
+ * as one just below, one below 0 or NaN as 0.  A temperature that is not above 0 gives the first of the order, as a top_p or min_p of NaN does.  NaN
+ * and -infinity are never chosen (-1 where a row has nothing else), +infinity has all the mass.  temperature, top_p, min_p: float
+ * [rows], top_k: int32 [rows], each or NULL (1, none); uniform: float [rows].  Weights and sums in 64 bits, weights to 2^-34 of
+ * their value and those below 2^-43 as none.  rows, V <= 2^20.  Bit-identical from run to run.
+ * workspace: as in nvfp4_matvec, of mq_sample_workspace_bytes(rows, V) bytes.
+ *
+ * mq_draft_accept: sampled [T]: the token that the model chose behind each new token; tokens [T]: the drafted ones.  From token 0 on the path
+ * goes to the lowest-numbered child whose token is the one sampled at its parent, while there is one.  path [T]: at cu_q[b] the numbers
+ * of sequence b's path, then -1; counts [B]: its length (0 where the sequence has no new tokens); next [B]: the token
+ * sampled at its end (-1 there); lens_out [B]: kv_lens - n + count, at least 0.
+ *
+ * kv8_compact: the places start + path[i] to start + i, i < counts[b], path strictly rising, 0 <= path[i] < n.  A page's exponent becomes the smallest
+ * with which the finite magnitudes that come from other pages are at most 448 * 2^e, and at least what it was; codes that come, and
+ * those in front of the first that moves, are brought to it with one rounding each as in kv8_append.  All other places
+ * are left as they are.  A place that has no page is neither read nor written.  Pages that hold places
+ * behind `start` of one sequence must not be another's.
+ */
+int mq_draft_tree(const int32_t *parents, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T, int words, int64_t window,
+                  uint32_t *tree, int32_t *positions, void *stream);
+int kv8_tree_attention(const void *q_bf16, int64_t ldq, const uint8_t *k_codes, const uint8_t *k_scales, const uint8_t *v_codes,
+                       const uint8_t *v_scales, int64_t pages, int P, int Hq, int Hkv, int D, const int32_t *page_table, int64_t pt_ld,
+                       int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T, const uint32_t *tree, int words,
+                       const int32_t *positions, float sm_scale, int64_t window, void *y, int64_t ldy, void *workspace,
+                       int64_t workspace_bytes, void *stream);
+int64_t mq_sample_workspace_bytes(int64_t rows, int64_t V);
+int mq_sample(const void *logits, int64_t rows, int64_t V, int64_t ld, int type, const float *uniform, const float *temperature,
+              const int32_t *top_k, const float *top_p, const float *min_p, int32_t *tokens, void *workspace, int64_t workspace_bytes,
+              void *stream);
+int mq_draft_accept(const int32_t *parents, const int32_t *tokens, const int32_t *sampled, const int32_t *cu_q, const int32_t *kv_lens,
+                    int64_t B, int64_t T, int32_t *path, int32_t *counts, int32_t *next, int32_t *lens_out, void *stream);
+int kv8_compact(uint8_t *k_codes, uint8_t *k_scales, uint8_t *v_codes, uint8_t *v_scales, int64_t pages, int P, int Hkv, int D,
+                const int32_t *page_table, int64_t pt_ld, int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T,
+                const int32_t *path, const int32_t *counts, void *stream);
 
 /* Human-readable name of an mq_status value (static storage). */
 const char *mq_status_string(int status);

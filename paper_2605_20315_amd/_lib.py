@@ -90,6 +90,19 @@ def load() -> ctypes.CDLL:
     lib.kv8_attention.restype = ci
     lib.kv8_attention.argtypes = [vp, i64, vp, vp, vp, vp, i64, ci, ci, ci, ci, vp, i64, i64, vp, vp, i64, i64, ctypes.c_float, i64,
                                   vp, i64, vp, i64, vp]
+    lib.kv8_tree_attention.restype = ci
+    lib.kv8_tree_attention.argtypes = [vp, i64, vp, vp, vp, vp, i64, ci, ci, ci, ci, vp, i64, i64, vp, vp, i64, i64, vp, ci, vp,
+                                       ctypes.c_float, i64, vp, i64, vp, i64, vp]
+    lib.mq_draft_tree.restype = ci
+    lib.mq_draft_tree.argtypes = [vp, vp, vp, i64, i64, ci, i64, vp, vp, vp]
+    lib.mq_draft_accept.restype = ci
+    lib.mq_draft_accept.argtypes = [vp, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp]
+    lib.kv8_compact.restype = ci
+    lib.kv8_compact.argtypes = [vp, vp, vp, vp, i64, ci, ci, ci, vp, i64, i64, vp, vp, i64, i64, vp, vp, vp]
+    lib.mq_sample_workspace_bytes.restype = i64
+    lib.mq_sample_workspace_bytes.argtypes = [i64, i64]
+    lib.mq_sample.restype = ci
+    lib.mq_sample.argtypes = [vp, i64, i64, i64, ci, vp, vp, vp, vp, vp, vp, vp, i64, vp]
     lib.mq_mfma_probe.restype = ci
     lib.mq_mfma_probe.argtypes = [vp, ci, vp, ctypes.POINTER(ctypes.c_double)]
     lib.mq_gemm_launches.restype = ci

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmixquant.so")
 BINDING = os.path.join(HERE, "_binding.so")
-SOURCES = ["api.hip", "quantize.hip", "gemm.hip", "kvcache.hip", "attention.hip", "matvec.hip"]
+SOURCES = ["api.hip", "quantize.hip", "gemm.hip", "kvcache.hip", "attention.hip", "matvec.hip", "draft.hip", "sample.hip"]
 CXX = os.environ.get("CXX", "g++")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -428,11 +428,13 @@ int64_t mq_kv8_attention_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, 
     return kv8_attention_workspace(T, B, Hq, Hkv, D);
 }
 
-int kv8_attention(const void *q_bf16, int64_t ldq, const uint8_t *k_codes, const uint8_t *k_scales, const uint8_t *v_codes,
-                  const uint8_t *v_scales, int64_t pages, int P, int Hq, int Hkv, int D, const int32_t *page_table, int64_t pt_ld,
-                  int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T, float sm_scale, int64_t window,
-                  void *y, int64_t ldy, void *workspace, int64_t workspace_bytes, void *stream)
+// Checks of an attention call, and its arguments for the launch; `any`: whether it has anything to do
+static int attend_args(Kv8Attend &a, bool &any, const void *q_bf16, int64_t ldq, const uint8_t *k_codes, const uint8_t *k_scales,
+                       const uint8_t *v_codes, const uint8_t *v_scales, int64_t pages, int P, int Hq, int Hkv, int D, const int32_t *page_table,
+                       int64_t pt_ld, int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T, float sm_scale, int64_t window,
+                       void *y, int64_t ldy, void *workspace, int64_t workspace_bytes)
 {
+    any = false;
     if (int rc = check_cache(pages, P, Hq, Hkv, D, pt_ld, W, B, T)) return rc;
     if (ldq < (int64_t)Hq * D || ldy < (int64_t)Hq * D || workspace_bytes < 0) return MQ_ERR_SHAPE;
     if (!(sm_scale > 0.0f) || !std::isfinite(sm_scale)) return MQ_ERR_ARG;
@@ -441,14 +443,116 @@ int kv8_attention(const void *q_bf16, int64_t ldq, const uint8_t *k_codes, const
     if (!q_bf16 || !y) return MQ_ERR_NULL;
     if (!aligned(q_bf16, 16) || !aligned(y, 16) || ldq % 8 != 0 || ldy % 8 != 0 || (workspace && !aligned(workspace, 16)))
         return MQ_ERR_ALIGN;
-    Kv8Attend a{static_cast<const uint16_t *>(q_bf16), ldq, k_codes, k_scales, v_codes, v_scales, static_cast<uint16_t *>(y), ldy, Hq, Hkv, D,
-                // a window that no int32 place lies outside of is none (one of W * P can bind: kv_lens may count places beyond the table)
-                window <= 0 || window > 0x7fffffff ? 0 : (int)window, sm_scale * 1.44269504f, nullptr, 0,
-                sequences(page_table, pt_ld, W, cu_q, kv_lens, B, T, pages, P)};
+    a.q = static_cast<const uint16_t *>(q_bf16), a.ldq = ldq;
+    a.k_codes = k_codes, a.k_scales = k_scales, a.v_codes = v_codes, a.v_scales = v_scales;
+    a.y = static_cast<uint16_t *>(y), a.ldy = ldy;
+    a.Hq = Hq, a.Hkv = Hkv, a.D = D;
+    // a window that no int32 place lies outside of is none (one of W * P can bind: kv_lens may count places beyond the table)
+    a.window = window <= 0 || window > 0x7fffffff ? 0 : (int)window;
+    a.scale = sm_scale * 1.44269504f;
     a.ws = workspace_bytes > 0 ? static_cast<float *>(workspace) : nullptr;
     a.ws_bytes = a.ws ? workspace_bytes : 0;
+    a.s = sequences(page_table, pt_ld, W, cu_q, kv_lens, B, T, pages, P);
+    any = true;
+    return MQ_OK;
+}
+
+int kv8_attention(const void *q_bf16, int64_t ldq, const uint8_t *k_codes, const uint8_t *k_scales, const uint8_t *v_codes,
+                  const uint8_t *v_scales, int64_t pages, int P, int Hq, int Hkv, int D, const int32_t *page_table, int64_t pt_ld,
+                  int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T, float sm_scale, int64_t window,
+                  void *y, int64_t ldy, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    Kv8Attend a{};
+    bool any;
+    if (int rc = attend_args(a, any, q_bf16, ldq, k_codes, k_scales, v_codes, v_scales, pages, P, Hq, Hkv, D, page_table, pt_ld, W, cu_q, kv_lens, B,
+                             T, sm_scale, window, y, ldy, workspace, workspace_bytes))
+        return rc;
+    if (!any) return MQ_OK;
     if (int rc = ensure_device(nullptr)) return rc;
     return launch_kv8_attention(a, static_cast<hipStream_t>(stream));
+}
+
+int kv8_tree_attention(const void *q_bf16, int64_t ldq, const uint8_t *k_codes, const uint8_t *k_scales, const uint8_t *v_codes,
+                       const uint8_t *v_scales, int64_t pages, int P, int Hq, int Hkv, int D, const int32_t *page_table, int64_t pt_ld,
+                       int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T, const uint32_t *tree, int words,
+                       const int32_t *positions, float sm_scale, int64_t window, void *y, int64_t ldy, void *workspace,
+                       int64_t workspace_bytes, void *stream)
+{
+    Kv8TreeAttend a{};
+    bool any;
+    if (words < 1 || words > kDraftMost / 32) return MQ_ERR_SHAPE;
+    if (int rc = attend_args(a, any, q_bf16, ldq, k_codes, k_scales, v_codes, v_scales, pages, P, Hq, Hkv, D, page_table, pt_ld, W, cu_q, kv_lens, B,
+                             T, sm_scale, window, y, ldy, workspace, workspace_bytes))
+        return rc;
+    if (!any) return MQ_OK;
+    if (!tree) return MQ_ERR_NULL;
+    if (!aligned(tree, 4) || !aligned(positions, 4)) return MQ_ERR_ALIGN;
+    a.tree = tree, a.words = words, a.positions = positions;
+    if (int rc = ensure_device(nullptr)) return rc;
+    return launch_kv8_tree_attention(a, static_cast<hipStream_t>(stream));
+}
+
+// The sequences of a call without a cache
+static int check_sequences(int64_t B, int64_t T) { return B < 0 || T < 0 || B > 0x7fffffff - 4 || T > 0x7fffffff ? MQ_ERR_SHAPE : MQ_OK; }
+
+int mq_draft_tree(const int32_t *parents, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T, int words, int64_t window,
+                  uint32_t *tree, int32_t *positions, void *stream)
+{
+    if (int rc = check_sequences(B, T)) return rc;
+    if (words < 1 || words > kDraftMost / 32) return MQ_ERR_SHAPE;
+    if (T == 0 || B == 0) return MQ_OK;
+    if (!parents || !cu_q || !kv_lens || !tree || !positions) return MQ_ERR_NULL;
+    if (!aligned(parents, 4) || !aligned(cu_q, 4) || !aligned(kv_lens, 4) || !aligned(tree, 4) || !aligned(positions, 4)) return MQ_ERR_ALIGN;
+    const DraftTree a{parents, tree, positions, words, window <= 0 || window > kDraftMost ? 0 : (int)window,
+                      sequences(nullptr, 0, 0, cu_q, kv_lens, B, T, 0, 16)};
+    return launch_draft_tree(a, static_cast<hipStream_t>(stream));
+}
+
+int mq_draft_accept(const int32_t *parents, const int32_t *tokens, const int32_t *sampled, const int32_t *cu_q, const int32_t *kv_lens,
+                    int64_t B, int64_t T, int32_t *path, int32_t *counts, int32_t *next, int32_t *lens_out, void *stream)
+{
+    if (int rc = check_sequences(B, T)) return rc;
+    if (B == 0) return MQ_OK;
+    if (!cu_q || !kv_lens || !counts || !next || !lens_out || (T > 0 && (!parents || !tokens || !sampled || !path))) return MQ_ERR_NULL;
+    for (const void *p : {(const void *)parents, (const void *)tokens, (const void *)sampled, (const void *)cu_q, (const void *)kv_lens,
+                          (const void *)path, (const void *)counts, (const void *)next, (const void *)lens_out})
+        if (!aligned(p, 4)) return MQ_ERR_ALIGN;
+    const DraftAccept a{parents, tokens, sampled, path, counts, next, lens_out, sequences(nullptr, 0, 0, cu_q, kv_lens, B, T, 0, 16)};
+    return launch_draft_accept(a, static_cast<hipStream_t>(stream));
+}
+
+int kv8_compact(uint8_t *k_codes, uint8_t *k_scales, uint8_t *v_codes, uint8_t *v_scales, int64_t pages, int P, int Hkv, int D,
+                const int32_t *page_table, int64_t pt_ld, int64_t W, const int32_t *cu_q, const int32_t *kv_lens, int64_t B, int64_t T,
+                const int32_t *path, const int32_t *counts, void *stream)
+{
+    if (int rc = check_cache(pages, P, Hkv, Hkv, D, pt_ld, W, B, T)) return rc;
+    if (T == 0 || B == 0) return MQ_OK;
+    if (int rc = check_cache_pointers(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens)) return rc;
+    if (!path || !counts) return MQ_ERR_NULL;
+    if (!aligned(path, 4) || !aligned(counts, 4)) return MQ_ERR_ALIGN;
+    const Kv8Compact a{k_codes, k_scales, v_codes, v_scales, path, counts, Hkv, D, sequences(page_table, pt_ld, W, cu_q, kv_lens, B, T, pages, P)};
+    return launch_kv8_compact(a, static_cast<hipStream_t>(stream));
+}
+
+int64_t mq_sample_workspace_bytes(int64_t rows, int64_t V)
+{
+    return rows <= 0 || rows > kSampleRows || V <= 0 || V > kSampleTokens ? 0 : sample_workspace(rows, V);
+}
+
+int mq_sample(const void *logits, int64_t rows, int64_t V, int64_t ld, int type, const float *uniform, const float *temperature,
+              const int32_t *top_k, const float *top_p, const float *min_p, int32_t *tokens, void *workspace, int64_t workspace_bytes,
+              void *stream)
+{
+    if (rows < 0 || rows > kSampleRows || V <= 0 || V > kSampleTokens || ld < V || workspace_bytes < 0) return MQ_ERR_SHAPE;
+    if (type != MQ_OUT_BF16 && type != MQ_OUT_FP32) return MQ_ERR_ARG;
+    if (rows == 0) return MQ_OK;
+    if (!logits || !uniform || !tokens) return MQ_ERR_NULL;
+    if (!aligned(logits, type == MQ_OUT_BF16 ? 2 : 4) || !aligned(workspace, 16)) return MQ_ERR_ALIGN;
+    for (const void *p : {(const void *)uniform, (const void *)temperature, (const void *)top_k, (const void *)top_p, (const void *)min_p, (const void *)tokens})
+        if (!aligned(p, 4)) return MQ_ERR_ALIGN;
+    if (sample_workspace(rows, V) > (workspace ? workspace_bytes : 0)) return MQ_ERR_SCRATCH;
+    const Sample a{logits, rows, V, ld, uniform, temperature, top_p, min_p, top_k, tokens, workspace};
+    return launch_sample(a, type == MQ_OUT_FP32, static_cast<hipStream_t>(stream));
 }
 
 int mq_mfma_probe(float *scratch_dev, int iters, void *stream, double *flop_out)
@@ -517,7 +621,7 @@ const char *mq_status_string(int status)
     case MQ_ERR_HIP: return "MQ_ERR_HIP: kernel launch failed (see mq_last_hip_error)";
     case MQ_ERR_SCRATCH:
         return "MQ_ERR_SCRATCH: the problem wants more scratch memory than the static array of "
-               "nvfp4_gemm_noalloc holds (use nvfp4_gemm_ws with a workspace), or than the workspace given to nvfp4_matvec";
+               "nvfp4_gemm_noalloc holds (use nvfp4_gemm_ws with a workspace), or than the workspace given to nvfp4_matvec or mq_sample";
     default: return "unknown mq_status";
     }
 }

@@ -222,6 +222,51 @@ static __device__ __forceinline__ float inverse_of(const Kv8Attend &a, int b, co
     return 0.0f;
 }
 
+// Drafted tokens.  A token sees the places before the sequence's new tokens, and of those its own mask's: the new ones are in the
+// last places, so only the last tiles differ from those of a chain, and there a row's 32 places are one word of bits.
+template <bool TREE>
+using Attend = std::conditional_t<TREE, Kv8TreeAttend, Kv8Attend>;
+
+// The position that a window is measured from; it is no less than that of the sequence's first new token
+static __device__ __forceinline__ int position_of(const Kv8TreeAttend &a, const Span &sp, int token)
+{
+    return a.positions ? max(a.positions[sp.q0 + token], sp.start) : sp.start + token;
+}
+
+static __device__ __forceinline__ uint32_t bits_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
+
+// Which of the places t .. t + 31 a token sees, as bits; `first` is the first that its window leaves.
+static __device__ __forceinline__ uint32_t seen_word(const Kv8TreeAttend &a, const Span &sp, const uint32_t *mask, int first, int t)
+{
+    const int64_t at = (int64_t)t - sp.start;  // the number of place t among the new tokens
+    uint32_t seen = 0;
+    if (at < 0) seen = bits_below((int)min(-at, (int64_t)32)) & ~bits_below((int)max(min((int64_t)first - t, (int64_t)32), (int64_t)0));
+    if (at > -32 && at < 32 * a.words) {
+        const int w = (int)(at >> 5), s = (int)(at & 31);
+        const uint32_t lo = w >= 0 ? mask[w] : 0u, hi = s > 0 && w + 1 < a.words ? mask[w + 1] : 0u;
+        seen |= (uint32_t)((((uint64_t)hi << 32) | lo) >> s);
+    }
+    return seen;
+}
+
+// As inverse_of, for the sequence's new token `token`
+static __device__ __forceinline__ float tree_inverse_of(const Kv8TreeAttend &a, int b, const Span &sp, int token, float total)
+{
+    if (total != 0.0f) return 1.0f / total;
+    const int32_t *const table = a.s.page_table + b * a.s.pt_ld;
+    auto has_page = [&](int place) { return (unsigned)table[place >> a.s.page_shift] < (uint64_t)a.s.pages; };
+#pragma unroll 1
+    for (int place = first_seen(a, position_of(a, sp, token)); place < min(sp.start, sp.len); place = ((place >> a.s.page_shift) + 1) << a.s.page_shift)
+        if (has_page(place)) return __builtin_nanf("");
+    const uint32_t *const mask = a.tree + (int64_t)(sp.q0 + token) * a.words;
+#pragma unroll 1
+    for (int i = 0; i < min(sp.n, 32 * a.words); ++i) {
+        const int place = sp.start + i;
+        if ((mask[i >> 5] >> (i & 31) & 1) && place >= 0 && place < sp.len && has_page(place)) return __builtin_nanf("");
+    }
+    return 0.0f;
+}
+
 // 0x01 in the bytes that are NaN codes
 static __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u; }
 
@@ -267,8 +312,8 @@ constexpr int kFewWaves = 4, kFewThreads = 64 * kFewWaves;
 // waiting for memory (vector instructions 15 % of the time); two sequences of 105000, 435 MB, 83 us.  A branch around the loads
 // ahead would make every wait one for all of them (125 and 92 us with the join, so 120.5 and 89).
 // RT tiles of 16 rows: what a wave has expanded serves all of them (109 sequences of 23000, 52 rows each: 365 us with one, 233 with two).
-template <int D, int RT>
-__global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
+template <int D, int RT, bool TREE>
+__global__ __launch_bounds__(kFewThreads) void attend_few(Attend<TREE> a, Cut c)
 {
     constexpr int KW = D / 16;  // dwords of a key row's quarter, and MFMA steps over the head elements per 2 of them
     constexpr int VW = D / 64;  // dwords of a value row's sixteenth
@@ -281,13 +326,19 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
     if (!it.found) return;
     const int G = a.Hq / a.Hkv, rows = it.sp.n * G, row0 = it.tile * kRows;
     int pos[RT], first[RT];  // the places that the lane's row of each tile sees: from first to pos
+    [[maybe_unused]] const uint32_t *mask[RT];
     u32x4 q[RT][D / 32];
     f32x4 acc[RT][D / 16];
     float mb[RT], l[RT];  // the running maximum times the scale, and the lane's share of the sum
 #pragma unroll
     for (int f = 0; f < RT; ++f) {
         const int row = min(row0 + 16 * f + col, rows - 1), token = row / G, head = it.head * G + row - token * G;
-        pos[f] = it.sp.start + token;
+        if constexpr (TREE) {
+            pos[f] = position_of(a, it.sp, token);
+            mask[f] = a.tree + (int64_t)(it.sp.q0 + token) * a.words;
+        } else {
+            pos[f] = it.sp.start + token;
+        }
         first[f] = first_seen(a, pos[f]);
         const uint16_t *const p = a.q + (int64_t)(it.sp.q0 + token) * a.ldq + (int64_t)head * D + g * (D / 4);
 #pragma unroll
@@ -297,9 +348,20 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
         mb[f] = kNone, l[f] = 0.0f;
     }
     // what every row of the item, and what any of them sees
-    const int pos_lo = it.sp.start + row0 / G, pos_hi = it.sp.start + (min(row0 + kRows, rows) - 1) / G;
-    const int hi = min(it.hi, pos_hi + 1), lo = max(it.lo, first_seen(a, pos_lo));
-    const int all_lo = first_seen(a, pos_hi), all_hi = min(it.hi, pos_lo + 1);
+    int lo, hi, all_lo, all_hi;
+    if constexpr (TREE) {
+        hi = min(it.hi, it.sp.start + it.sp.n), lo = max(it.lo, first_seen(a, it.sp.start));
+        all_lo = first[0], all_hi = min(it.hi, it.sp.start);
+#pragma unroll
+        for (int f = 1; f < RT; ++f) all_lo = max(all_lo, first[f]);
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) all_lo = max(all_lo, __shfl_xor(all_lo, d));
+        all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    } else {
+        const int pos_lo = it.sp.start + row0 / G, pos_hi = it.sp.start + (min(row0 + kRows, rows) - 1) / G;
+        hi = min(it.hi, pos_hi + 1), lo = max(it.lo, first_seen(a, pos_lo));
+        all_lo = first_seen(a, pos_hi), all_hi = min(it.hi, pos_lo + 1);
+    }
     bool marked = false;  // whether the wave's part of `sums` holds NaN for what rows have seen
 
     const int P = 1 << a.s.page_shift;
@@ -372,6 +434,10 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
             bool odd = false;
 #pragma unroll
             for (int f = 0; f < RT; ++f) seen[f] = 0;
+            [[maybe_unused]] uint32_t word[RT];  // of the lane's row, from its places on
+            if constexpr (TREE)
+#pragma unroll
+                for (int f = 0; f < RT; ++f) word[f] = seen_word(a, it.sp, mask[f], first[f], t) >> (4 * g);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -380,7 +446,12 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
                     const bool there = at >= lo && at < hi && (h ? id1 : id0) >= 0;
 #pragma unroll
                     for (int f = 0; f < RT; ++f) {
-                        if (there && at >= first[f] && at <= pos[f])
+                        bool sees;
+                        if constexpr (TREE)
+                            sees = word[f] >> (16 * h + j) & 1;
+                        else
+                            sees = at >= first[f] && at <= pos[f];
+                        if (there && sees)
                             seen[f] |= 1u << (4 * h + j);
                         else
                             s[f][h][j] = kNone;
@@ -532,7 +603,11 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
             continue;
         }
         const int token = row / G;
-        const float inv = inverse_of(a, it.b, it.sp, it.sp.start + token, total);
+        float inv;
+        if constexpr (TREE)
+            inv = tree_inverse_of(a, it.b, it.sp, token, total);
+        else
+            inv = inverse_of(a, it.b, it.sp, it.sp.start + token, total);
         uint32_t *const y = reinterpret_cast<uint32_t *>(a.y + (int64_t)(it.sp.q0 + token) * a.ldy + (int64_t)(it.head * G + row - token * G) * D + e0);
 #pragma unroll
         for (int e = 0; e < D / 16; e += 2) y[e / 2] = pack2(o[e] * inv, o[e + 1] * inv);
@@ -556,8 +631,8 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
 // 8192^3 reaches here.  Compared while it took 635 (its page numbers were looked at where they were read): without the keys
 // ahead 747; one wave a SIMD with 64 rows, which reads LDS half as often, 945 (it has no second wave to fill its waits);
 // eight waves in one workgroup 635, and less even shares of short work.
-template <int D>
-__global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut c)
+template <int D, bool TREE>
+__global__ __launch_bounds__(64 * kManyWaves) void attend_many(Attend<TREE> a, Cut c)
 {
     constexpr int NW = kManyWaves, NT = 64 * NW, TN = 4 * D / NT;  // tasks of a thread: 32 bytes of codes each
     static_assert(TN * NT == 4 * D && (TN > 1 || NT == 2 * 2 * D), "every thread has the same tasks, or half of the waves those of keys");
@@ -574,15 +649,29 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
     const int G = a.Hq / a.Hkv, rows = it.sp.n * G, tile0 = it.tile * kRows, wave0 = tile0 + 32 * wave;
     // the lane's row (rows beyond the last are computed again and not stored) and the places that it sees
     const int row = min(wave0 + col, rows - 1), token = row / G, head = it.head * G + row - token * G;
-    const int pos = it.sp.start + token, first = first_seen(a, pos);
-    // places that any row of the workgroup sees, that any and that every row of the wave sees
-    const int group_hi = min(it.hi, it.sp.start + (min(tile0 + kRows, rows) - 1) / G + 1);
-    const int group_lo = max(it.lo, first_seen(a, it.sp.start + tile0 / G));
-    const int pos_lo = it.sp.start + min(wave0, rows - 1) / G, pos_hi = it.sp.start + (min(wave0 + 32, rows) - 1) / G;
-    const int all_lo = max(group_lo, first_seen(a, pos_hi)), all_hi = min(group_hi, pos_lo + 1);
-    // places that every row of the workgroup sees
-    const int rows_lo = max(group_lo, first_seen(a, it.sp.start + (min(tile0 + kRows, rows) - 1) / G));
-    const int rows_hi = min(group_hi, it.sp.start + tile0 / G + 1);
+    int pos, first;
+    // places that any row of the workgroup sees, that every row of the wave sees, and that every row of the workgroup sees
+    int group_lo, group_hi, all_lo, all_hi, rows_lo, rows_hi;
+    [[maybe_unused]] const uint32_t *mask = nullptr;
+    if constexpr (TREE) {
+        pos = position_of(a, it.sp, token), first = first_seen(a, pos);
+        mask = a.tree + (int64_t)(it.sp.q0 + token) * a.words;
+        group_hi = min(it.hi, it.sp.start + it.sp.n), group_lo = max(it.lo, first_seen(a, it.sp.start));
+        all_lo = first;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) all_lo = max(all_lo, __shfl_xor(all_lo, d));
+        all_lo = max(group_lo, __builtin_amdgcn_readfirstlane(all_lo)), all_hi = min(group_hi, it.sp.start);
+        // (the rows' positions are in no order: with a window none are taken for seen by all, which costs a look for NaN codes)
+        rows_lo = a.window > 0 ? group_hi : group_lo, rows_hi = all_hi;
+    } else {
+        pos = it.sp.start + token, first = first_seen(a, pos);
+        group_hi = min(it.hi, it.sp.start + (min(tile0 + kRows, rows) - 1) / G + 1);
+        group_lo = max(it.lo, first_seen(a, it.sp.start + tile0 / G));
+        const int pos_lo = it.sp.start + min(wave0, rows - 1) / G, pos_hi = it.sp.start + (min(wave0 + 32, rows) - 1) / G;
+        all_lo = max(group_lo, first_seen(a, pos_hi)), all_hi = min(group_hi, pos_lo + 1);
+        rows_lo = max(group_lo, first_seen(a, it.sp.start + (min(tile0 + kRows, rows) - 1) / G));
+        rows_hi = min(group_hi, it.sp.start + tile0 / G + 1);
+    }
 
     bf16x8 q[D / 16];
     {
@@ -713,6 +802,15 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
         top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale;
     };
     auto sees = [&](int at, int no_page) { return at >= max(first, group_lo) && at <= pos && at < group_hi && !no_page; };
+    // TREE: the places t .. t + 31 that the lane's row sees, without those that have no page (bad: of the first and second 16)
+    [[maybe_unused]] auto seen_of = [&](int t, int bad) {
+        uint32_t w = 0;
+        if constexpr (TREE) {
+            w = seen_word(a, it.sp, mask, first, t) & bits_below(group_hi - t) & ~bits_below(group_lo - t);
+            w &= (bad & 1 ? 0xffff0000u : ~0u) & (bad & 2 ? 0xffffu : ~0u);
+        }
+        return w;
+    };
     const unsigned char *key_at, *value_at;
     auto half_step = [&](int i, int half, int flag) {
         const unsigned char *const next = key_at + half * (D / 16) * kBlock16, *const from = value_at + 2 * half * (D / 32) * kBlock16;
@@ -720,6 +818,11 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
         const int t = begin + i * kTile + 32 * half, bad = flag >> (2 * half) & 3;
         const bool edge = t < all_lo || t + 32 > all_hi || bad;
         if (edge) {
+            [[maybe_unused]] const uint32_t word = seen_of(t, bad) >> (4 * h);
+            if constexpr (TREE) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[half][j] = word >> (8 * (j / 4) + j % 4) & 1 ? s[half][j] : kNone;
+            } else
 #pragma unroll
             for (int j = 0; j < 16; ++j) s[half][j] = sees(t + 8 * (j / 4) + 4 * h + j % 4, bad >> (j / 8) & 1) ? s[half][j] : kNone;
             maxima(half);
@@ -778,8 +881,9 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
                 }
         }
         __syncthreads();
+        [[maybe_unused]] const uint32_t words[2] = {seen_of(begin + i * kTile, flag & 3), seen_of(begin + i * kTile + 32, flag >> 2 & 3)};
         for (int j = 0; j < kTile; ++j)
-            if (sees(begin + i * kTile + j, flag >> (j / 16) & 1))
+            if (TREE ? (words[j >> 5] >> (j & 31) & 1) != 0 : sees(begin + i * kTile + j, flag >> (j / 16) & 1))
                 for (int d = 0; d < D / 32; ++d) marks[d][tid] |= nans[j][d];
         __syncthreads();
     };
@@ -820,7 +924,11 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
     float *const part = slot_at(c, D, it.slot);
     if (split && h == 0) part[c.rows * D + local] = mb, part[c.rows * D + c.rows + local] = l;
     // (the item is read from LDS again: kept through the loop it spills 16 more scalar registers, 595 us for the long prompt's 591)
-    const float inv = split ? 1.0f : inverse_of(a, plan.found.b, plan.found.sp, pos, l);
+    float inv = 1.0f;
+    if constexpr (TREE)
+        inv = split ? 1.0f : tree_inverse_of(a, plan.found.b, plan.found.sp, token, l);
+    else
+        inv = split ? 1.0f : inverse_of(a, plan.found.b, plan.found.sp, pos, l);
     uint16_t *const y = a.y + (int64_t)(it.sp.q0 + token) * a.ldy + (int64_t)head * D;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -870,8 +978,8 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut 
 
 // Rows (token, head) of the sequences with several chunks.  D / 4 threads cover a row's elements; a workgroup's 1024 / D such
 // groups take a row each (ROWS: many rows), or every so-many-th chunk of one row.
-template <int D, bool ROWS>
-__global__ __launch_bounds__(256) void attend_join(Kv8Attend a, Cut c)
+template <int D, bool ROWS, bool TREE>
+__global__ __launch_bounds__(256) void attend_join(Attend<TREE> a, Cut c)
 {
     constexpr int kCols = D / 4, kParts = 256 / kCols;
     __shared__ float tops[4], totals[kParts];
@@ -935,7 +1043,11 @@ __global__ __launch_bounds__(256) void attend_join(Kv8Attend a, Cut c)
     } else if (h0 + part >= a.Hq) {
         return;
     }
-    const float inv = inverse_of(a, b, sp, sp.start + t - sp.q0, total);
+    float inv;
+    if constexpr (TREE)
+        inv = tree_inverse_of(a, b, sp, t - sp.q0, total);
+    else
+        inv = inverse_of(a, b, sp, sp.start + t - sp.q0, total);
     *reinterpret_cast<u32x2 *>(a.y + (int64_t)t * a.ldy + (int64_t)h * D + 4 * col) = u32x2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
 }
 
@@ -1020,8 +1132,8 @@ static int plan_attention(const Kv8Attend &a, Launch *out)
     return n;
 }
 
-template <int D>
-static int launch_attention(const Kv8Attend &a, hipStream_t s)
+template <int D, bool TREE>
+static int launch_attention(const Attend<TREE> &a, hipStream_t s)
 {
     Launch plan[2];
     const int n = plan_attention(a, plan);
@@ -1031,17 +1143,17 @@ static int launch_attention(const Kv8Attend &a, hipStream_t s)
         auto go = [&](auto kernel, int threads) { return enqueue(kernel, dim3((unsigned)p.items), dim3(threads), 0, s, a, p.cut); };
         int rc;
         if (p.many)
-            rc = go(attend_many<D>, 64 * kManyWaves);
+            rc = go(attend_many<D, TREE>, 64 * kManyWaves);
         else if (p.cut.rows == kFewRows)
-            rc = go(attend_few<D, 1>, kFewThreads);
+            rc = go(attend_few<D, 1, TREE>, kFewThreads);
         else
-            rc = go(attend_few<D, D <= 128 ? 2 : 1>, kFewThreads);
+            rc = go(attend_few<D, D <= 128 ? 2 : 1, TREE>, kFewThreads);
         if (rc) return rc;
         if (!p.cut.split) continue;
         constexpr int kPer = 1024 / D;
         const int64_t T = p.cut.tokens ? (int64_t)a.s.B * p.cut.tokens : a.s.T;
-        rc = T * a.Hq >= 2048 ? enqueue(attend_join<D, true>, dim3((unsigned)(T * ((a.Hq + kPer - 1) / kPer))), dim3(256), 0, s, a, p.cut)
-                              : enqueue(attend_join<D, false>, dim3((unsigned)(T * a.Hq)), dim3(256), 0, s, a, p.cut);
+        rc = T * a.Hq >= 2048 ? enqueue(attend_join<D, true, TREE>, dim3((unsigned)(T * ((a.Hq + kPer - 1) / kPer))), dim3(256), 0, s, a, p.cut)
+                              : enqueue(attend_join<D, false, TREE>, dim3((unsigned)(T * a.Hq)), dim3(256), 0, s, a, p.cut);
         if (rc) return rc;
     }
     return MQ_OK;
@@ -1060,7 +1172,13 @@ int describe_kv8_attention(const Kv8Attend &a, mq_kv8_launch *out)
 int launch_kv8_attention(const Kv8Attend &a, hipStream_t s)
 {
     if (a.s.T == 0 || a.s.B == 0) return MQ_OK;
-    return a.D == 64 ? launch_attention<64>(a, s) : a.D == 128 ? launch_attention<128>(a, s) : launch_attention<256>(a, s);
+    return a.D == 64 ? launch_attention<64, false>(a, s) : a.D == 128 ? launch_attention<128, false>(a, s) : launch_attention<256, false>(a, s);
+}
+
+int launch_kv8_tree_attention(const Kv8TreeAttend &a, hipStream_t s)
+{
+    if (a.s.T == 0 || a.s.B == 0) return MQ_OK;
+    return a.D == 64 ? launch_attention<64, true>(a, s) : a.D == 128 ? launch_attention<128, true>(a, s) : launch_attention<256, true>(a, s);
 }
 
 }  // namespace mq

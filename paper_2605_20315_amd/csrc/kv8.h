@@ -46,6 +46,47 @@ struct Kv8Attend {
     Kv8Seqs s;
 };
 
+// The same for drafted tokens: [T, words] masks over a sequence's new tokens, and their positions or NULL (their places)
+struct Kv8TreeAttend : Kv8Attend {
+    const uint32_t *tree;
+    const int32_t *positions;
+    int words;
+};
+
+constexpr int kDraftMost = 1024;  // new tokens of a sequence that a mask can name: 32 words
+
+struct DraftTree {
+    const int32_t *parents;
+    uint32_t *tree;  // [T, words]
+    int32_t *positions;
+    int words, window;
+    Kv8Seqs s;  // (without a table)
+};
+
+struct DraftAccept {
+    const int32_t *parents, *tokens, *sampled;
+    int32_t *path, *counts, *next, *lens;
+    Kv8Seqs s;  // (without a table)
+};
+
+struct Kv8Compact {
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    const int32_t *path, *counts;
+    int Hkv, D;
+    Kv8Seqs s;
+};
+
+constexpr int64_t kSampleRows = 1 << 20, kSampleTokens = 1 << 20;
+
+struct Sample {
+    const void *logits;
+    int64_t rows, V, ld;
+    const float *uniform, *temperature, *top_p, *min_p;  // each but the first may be NULL
+    const int32_t *top_k;
+    int32_t *tokens;
+    void *ws;
+};
+
 struct RopeTable {
     double freq[128];
     float *table;
@@ -57,6 +98,12 @@ struct RopeTable {
 int launch_rope_table(const RopeTable &r, hipStream_t s);
 int launch_kv8_append(const Kv8Append &a, hipStream_t s);
 int launch_kv8_attention(const Kv8Attend &a, hipStream_t s);
+int launch_kv8_tree_attention(const Kv8TreeAttend &a, hipStream_t s);
+int launch_draft_tree(const DraftTree &a, hipStream_t s);
+int launch_draft_accept(const DraftAccept &a, hipStream_t s);
+int launch_kv8_compact(const Kv8Compact &a, hipStream_t s);
+int launch_sample(const Sample &a, bool fp32, hipStream_t s);
+int64_t sample_workspace(int64_t rows, int64_t V);
 int describe_kv8_attention(const Kv8Attend &a, mq_kv8_launch *out);  // what the above launches (mixquant_diag.h)
 int64_t kv8_attention_workspace(int64_t T, int64_t B, int Hq, int Hkv, int D);
 int launch_nvfp4_matvec(const uint16_t *x, int64_t ldx, const uint8_t *codes, const uint8_t *scales, const float *alpha, int64_t M,

@@ -471,6 +471,173 @@ def kv8_attention(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tensor
     return y
 
 
+def _here(*tensors) -> None:
+    """The kernels run on the current device's stream."""
+    _need_gpu(*tensors)
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t.device.index != device:
+            raise MixQuantError(f"a tensor lives on {t.device}, the current device is cuda:{device}")
+
+
+def _vector(what: str, t: torch.Tensor, n: int, dtype=torch.int32) -> torch.Tensor:
+    if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
+        raise MixQuantError(f"expected {what} as a contiguous {dtype} [{n}]")
+    return t
+
+
+def _ptr(t: torch.Tensor | None):
+    return t.data_ptr() if t is not None else None
+
+
+def _new_tokens(parents: torch.Tensor, cu_q: torch.Tensor, kv_lens: torch.Tensor):
+    """Checks of the sequences' new tokens; (T, B)."""
+    _here(parents, cu_q, kv_lens)
+    T, B = parents.numel(), kv_lens.numel()
+    _vector("parents", parents, T)
+    _vector("kv_lens", kv_lens, B)
+    _vector("cu_q", cu_q, B + 1)
+    return T, B
+
+
+def mq_draft_tree(parents: torch.Tensor, cu_q: torch.Tensor, kv_lens: torch.Tensor, words: int, window: int = 0,
+                  tree: torch.Tensor | None = None, positions: torch.Tensor | None = None):
+    """(tree, positions) of drafted tokens: int32 [T, words], whose bit j says that a token has the j-th new token of its sequence above it
+    or is it, and int32 [T], for kv8_tree_attention and kv8_append.  parents int32 [T]: the number of each token's parent among its
+    sequence's new tokens, -1 for none.  words: 32 tokens each, for the longest of the sequences.  window > 0: only the window - 1
+    tokens next above."""
+    T, B = _new_tokens(parents, cu_q, kv_lens)
+    words = int(words)
+    if tree is None:
+        tree = torch.empty((T, max(words, 0)), dtype=torch.int32, device=parents.device)
+    if positions is None:
+        positions = torch.empty(T, dtype=torch.int32, device=parents.device)
+    _here(tree, positions)
+    if tree.dtype != torch.int32 or tree.shape != (T, words) or not tree.is_contiguous():
+        raise MixQuantError(f"expected tree as a contiguous int32 [tokens, words] of [{T}, {words}]")
+    _vector("positions", positions, T)
+    rc = _lib.load().mq_draft_tree(parents.data_ptr(), cu_q.data_ptr(), kv_lens.data_ptr(), B, T, words, window, tree.data_ptr(),
+                                   positions.data_ptr(), _stream())
+    _lib.check(rc, "mq_draft_tree")
+    return tree, positions
+
+
+def kv8_tree_attention(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor, v_scales: torch.Tensor,
+                       page_table: torch.Tensor, cu_q: torch.Tensor, kv_lens: torch.Tensor, tree: torch.Tensor, sm_scale: float,
+                       window: int = 0, positions: torch.Tensor | None = None, y: torch.Tensor | None = None,
+                       workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Attention of drafted tokens' queries q [T, Hq, D] over the paged FP8 cache, which holds them as the last tokens of their
+    sequences: each sees the places before its sequence's new tokens, and of those its mask's; BF16 [T, Hq, D].  tree: int32 [T, words], what
+    mq_draft_tree gives.  window > 0: of the places before them only those behind position - window; positions int32 [T], else
+    the tokens' places.  workspace: as in kv8_attention."""
+    _here(q, k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, tree)
+    T, Hq, D, ldq = _heads_ld(q)
+    pages, P, Hkv, pt_ld, W, B = _cache(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, T, D)
+    if tree.dtype != torch.int32 or tree.dim() != 2 or tree.shape[0] != T or not tree.is_contiguous():
+        raise MixQuantError(f"expected tree as a contiguous int32 [{T}, words]")
+    if positions is not None:
+        _here(positions)
+        _vector("positions", positions, T)
+    if y is None:
+        y = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=q.device)
+    _here(y)
+    if y.shape != (T, Hq, D):
+        raise MixQuantError("y has another shape than q")
+    ldy = _heads_ld(y)[3]
+    ws_ptr, ws_bytes = 0, 0
+    if workspace is not None:
+        _here(workspace)
+        assert workspace.is_contiguous()
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    rc = _lib.load().kv8_tree_attention(q.data_ptr(), ldq, k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(),
+                                        v_scales.data_ptr(), pages, P, Hq, Hkv, D, page_table.data_ptr(), pt_ld, W, cu_q.data_ptr(),
+                                        kv_lens.data_ptr(), B, T, tree.data_ptr(), tree.shape[1], _ptr(positions), sm_scale, window,
+                                        y.data_ptr(), ldy, ws_ptr, ws_bytes, _stream())
+    _lib.check(rc, "kv8_tree_attention")
+    return y
+
+
+def mq_sample_workspace_bytes(rows: int, V: int) -> int:
+    """Workspace size that mq_sample needs."""
+    return int(_lib.load().mq_sample_workspace_bytes(rows, V))
+
+
+def mq_sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: torch.Tensor | None = None, top_k: torch.Tensor | None = None,
+              top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None, tokens: torch.Tensor | None = None,
+              workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """One token from each row of BF16 or FP32 logits [rows, V], as int32 [rows]: the first top_k of the order of falling logits, of
+    those the ones with less than top_p of their mass in front of them, of those the ones with at least min_p of the largest
+    weight; then the lowest index up to which the kept ones have more than `uniform` of their mass.  The settings are float32 (top_k
+    int32) [rows], or None for 1, none, none and none; a temperature of 0 gives the largest logit's index.  workspace: any contiguous GPU
+    tensor of mq_sample_workspace_bytes; without one it is taken from torch's allocator for the call."""
+    _here(logits, uniform)
+    if logits.dtype not in (torch.bfloat16, torch.float32):
+        raise MixQuantError("expected BF16 or FP32 logits")
+    rows, V, ld = _rows_k_ld(logits)
+    _vector("uniform", uniform, rows, torch.float32)
+    for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                           ("min_p", min_p, torch.float32)):
+        if t is not None:
+            _here(t)
+            _vector(name, t, rows, dtype)
+    if tokens is None:
+        tokens = torch.empty(rows, dtype=torch.int32, device=logits.device)
+    _here(tokens)
+    _vector("tokens", tokens, rows)
+    ws_bytes = mq_sample_workspace_bytes(rows, V)
+    if workspace is None and ws_bytes:
+        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=logits.device)
+    ws_ptr = 0
+    if workspace is not None:
+        _here(workspace)
+        assert workspace.is_contiguous()
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    rc = _lib.load().mq_sample(logits.data_ptr(), rows, V, ld, MQ_OUT_BF16 if logits.dtype == torch.bfloat16 else MQ_OUT_FP32,
+                               uniform.data_ptr(), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), tokens.data_ptr(), ws_ptr,
+                               ws_bytes, _stream())
+    _lib.check(rc, "mq_sample")
+    return tokens
+
+
+def mq_draft_accept(parents: torch.Tensor, tokens: torch.Tensor, sampled: torch.Tensor, cu_q: torch.Tensor, kv_lens: torch.Tensor,
+                    path: torch.Tensor | None = None, counts: torch.Tensor | None = None, next: torch.Tensor | None = None,
+                    lens: torch.Tensor | None = None):
+    """The drafted tokens that the sampled ones confirm: (path, counts, next, lens).  From token 0 of a sequence's new ones on, the lowest
+    child whose token is the one sampled at its parent.  path int32 [T]: at cu_q[b] the numbers of b's path, then -1; counts int32 [B]: its
+    length; next int32 [B]: the token sampled at its end; lens int32 [B]: the sequence's length with the path alone."""
+    T, B = _new_tokens(parents, cu_q, kv_lens)
+    _here(tokens, sampled)
+    _vector("tokens", tokens, T)
+    _vector("sampled", sampled, T)
+    made = []
+    for name, t, n in (("path", path, T), ("counts", counts, B), ("next", next, B), ("lens", lens, B)):
+        t = torch.empty(n, dtype=torch.int32, device=parents.device) if t is None else t
+        _here(t)
+        made.append(_vector(name, t, n))
+    path, counts, next, lens = made
+    rc = _lib.load().mq_draft_accept(parents.data_ptr(), tokens.data_ptr(), sampled.data_ptr(), cu_q.data_ptr(), kv_lens.data_ptr(), B, T,
+                                     path.data_ptr(), counts.data_ptr(), next.data_ptr(), lens.data_ptr(), _stream())
+    _lib.check(rc, "mq_draft_accept")
+    return path, counts, next, lens
+
+
+def kv8_compact(k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor, v_scales: torch.Tensor, page_table: torch.Tensor,
+                cu_q: torch.Tensor, kv_lens: torch.Tensor, path: torch.Tensor, counts: torch.Tensor) -> None:
+    """Brings the tokens of the paths together in the paged FP8 cache, in place: path and counts as mq_draft_accept gives them, cu_q and
+    kv_lens those of the step that appended the drafted tokens."""
+    _here(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, path, counts)
+    if k_codes.dim() != 4:
+        raise MixQuantError("expected a cache of codes [pages, heads, tokens, D]")
+    T, D = path.numel(), k_codes.shape[3]
+    pages, P, Hkv, pt_ld, W, B = _cache(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, T, D)
+    _vector("path", path, T)
+    _vector("counts", counts, B)
+    rc = _lib.load().kv8_compact(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), pages, P, Hkv, D,
+                                 page_table.data_ptr(), pt_ld, W, cu_q.data_ptr(), kv_lens.data_ptr(), B, T, path.data_ptr(),
+                                 counts.data_ptr(), _stream())
+    _lib.check(rc, "kv8_compact")
+
+
 def mfma_probe(iters: int = 4000) -> float:
     """Enqueue the matrix-pipe rate probe on the current stream; returns the flop count of the launch."""
     import ctypes
