@@ -1,186 +1,786 @@
 // One token from each row of logits: temperature, top-k, top-p and min-p, from given uniform numbers.
 //
 // The tokens of a row are ordered by falling logit, the lower index first among equals; each of the filters keeps a first part of
-// that order, so all of them together are one border: a logit, and how many of the tokens that have just it.  Weights are
-// exp((logit - largest) / temperature) as whole multiples of 2^-43, computed in 64 bits: their sums are exact and in no order, and
-// a token is decided by which side of a border a sum of up to a million of them lies on.
+// that order, so all of them together are one border in it.  Nothing is sorted: the logits are counted into bins, and only
+// the tokens of the border's own bin are looked at one by one.
+//
+// With pos = 8 log2(e) logit / temperature, in binary64, a token's weight is 2^(pos / 8) over a common factor, and its bin is
+// floor(pos): the same for every part of a row, whatever the largest logit there, so that parts are counted by themselves and put
+// together by shifting.  Weights in a bin lie between 2^-1/8 and 1 of its top, and a bin's mass is its count less
+// what its weights fall short of one: 64 bits hold both, 2^-34 of a weight fine, and one addition in LDS counts a token.
+//
+// Two kernels.  sample_chunks reads the logits once, a chunk of a row by a workgroup: the largest, the mass, and where the row has
+// filters the count and mass up to each of the 512 bins below the chunk's largest (weights down to 2^-64).  sample_rows, a
+// workgroup a row: the border's bin from the sums of the chunks', the border in it, the chunk that the draw falls into, the token.
+// Bound by reading the logits, and for few rows by the trips to memory that one kernel and the other take one after another.
 #include "kv8.h"
 
 namespace mq {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr double kUnit = (double)(1ll << 43);
+typedef unsigned long long u64;
+constexpr int kBins = 512;
+constexpr int kCountBit = 47;  // a bin of a chunk: count << 47 | shortfall in 2^-34, at most 2^14 * 2^30.4
+constexpr double kFine = (double)(1ll << 34);
+constexpr int kChunkThreads = 512, kRowThreads = 1024;
+constexpr int kChunk = 8192;  // logits
+constexpr int kChunksMost = (int)(kSampleTokens / kChunk);  // of a row
 
-// Logits as unsigned numbers of the same order: NaN as -infinity, the two zeros as one
+struct Chunk {
+    float top;    // the largest logit
+    int first;    // its lowest index (of a row that takes the largest)
+    double mass;  // over that of the top of the largest logit's bin
+};
+
+struct alignas(16) Upto {
+    double mass;
+    int count;
+};
+
+// What is known of a row with filters: the masses and counts up to each bin below its largest logit's, and the tokens, as numbers, of the
+// bins that a border may be in (listed may be more than there is room for)
+constexpr int kList = 4096;
+struct Row {
+    double masses[kBins];
+    int counts[kBins];
+    int listed, pad;
+    u64 list[kList];
+};
+
+// The workspace: a Chunk for each chunk of a launch's rows, and for rows with filters the masses and counts up to each bin, and a Row
+struct Tables {
+    Chunk *chunks;
+    Upto *upto;
+    Row *rows;
+};
+constexpr int64_t kChunkBytes = sizeof(Chunk) + kBins * sizeof(Upto);
+
+struct Setting {
+    double scale, inverse;  // pos over logit, and logit over pos
+    int k;
+    float p, min_p;
+    bool largest, filters;
+};
+
+static __device__ __forceinline__ Setting setting_of(const Sample &a, int64_t r)
+{
+    const float t = a.temperature ? a.temperature[r] : 1.0f;
+    Setting s;
+    s.k = a.top_k ? a.top_k[r] : 0;
+    s.p = a.top_p ? a.top_p[r] : 1.0f;
+    s.min_p = a.min_p ? a.min_p[r] : 0.0f;
+    s.largest = !(t > 0.0f) || s.k == 1 || !(s.p > 0.0f) || s.min_p != s.min_p || s.min_p > 1.0f;
+    if (s.k <= 0 || s.k >= a.V) s.k = 0;
+    s.filters = s.k > 0 || s.p < 1.0f || s.min_p > 0.0f;
+    s.scale = 8.0 * 1.4426950408889634074 / (double)t;
+    s.inverse = (double)t * (0.69314718055994530942 / 8.0);
+    return s;
+}
+
+// Where a logit lies, given the largest: +infinity leaves weight to nothing else, and nothing is above it
+static __device__ __forceinline__ double pos_of(float x, float top, double scale) { return top == __builtin_inff() ? 0.0 : (double)x * scale; }
+static __device__ __forceinline__ bool weighs(float x, float top) { return top == __builtin_inff() ? x == top : x != -__builtin_inff(); }
+
+// 2^((f - 1) / 8) for f in 0 .. 1: the sixth-order Taylor polynomial about 1/2, within 6e-14
+static __device__ __forceinline__ double in_bin(double f)
+{
+    constexpr double h = 0.086643397569993163677, s = 0.95760328069857364694;  // ln(2) / 8, 2^(-1/16)
+    const double z = f - 0.5;
+    double w = s * h * h * h * h * h * h / 720;
+    w = __builtin_fma(w, z, s * h * h * h * h * h / 120);
+    w = __builtin_fma(w, z, s * h * h * h * h / 24);
+    w = __builtin_fma(w, z, s * h * h * h / 6);
+    w = __builtin_fma(w, z, s * h * h / 2);
+    w = __builtin_fma(w, z, s * h);
+    return __builtin_fma(w, z, s);
+}
+
+// 2^y for y <= 0: the Taylor polynomial of order 11 about the nearest whole number, within 7e-15; nothing below 2^-1000
+static __device__ __forceinline__ double power(double y)
+{
+    constexpr double h = 0.69314718055994530942;
+    constexpr double c[12] = {1, h, h * h / 2, h * h * h / 6, h * h * h * h / 24, h * h * h * h * h / 120, h * h * h * h * h * h / 720,
+                              h * h * h * h * h * h * h / 5040, h * h * h * h * h * h * h * h / 40320, h * h * h * h * h * h * h * h * h / 362880,
+                              h * h * h * h * h * h * h * h * h * h / 3628800, h * h * h * h * h * h * h * h * h * h * h / 39916800};
+    y = fmax(y, -1000.0);
+    const double shifted = y + 0x1.8p52, z = y - (shifted - 0x1.8p52);
+    double w = c[11];
+#pragma unroll
+    for (int i = 10; i >= 0; --i) w = __builtin_fma(w, z, c[i]);
+    return __builtin_bit_cast(double, __builtin_bit_cast(u64, w) + (__builtin_bit_cast(u64, shifted) << 52));
+}
+
+// Logits as unsigned numbers of the same order, the two zeros as one
 static __device__ __forceinline__ uint32_t key_of(float x)
 {
-    x = x != x ? -__builtin_inff() : x + 0.0f;
-    const uint32_t u = __float_as_uint(x);
+    const uint32_t u = __float_as_uint(x + 0.0f);
     return u >> 31 ? ~u : u | 0x80000000u;
 }
 static __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
 
+typedef uint32_t words2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// 16 bytes of a row from element i on (aligned to an element); what lies behind the row as -infinity
 template <class T>
-static __device__ __forceinline__ float load_logit(const T *p, int64_t i)
+static __device__ __forceinline__ u32x4 load16(const T *row, int i, int V)
+{
+    constexpr int N = 16 / sizeof(T);
+    if (i + N <= V) return *reinterpret_cast<const std::conditional_t<sizeof(T) == 2, words2, words4> *>(row + i);
+    uint32_t e[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if constexpr (sizeof(T) == 2)
+            e[j] = i + j < V ? row[i + j] : 0xff80u;
+        else
+            e[j] = i + j < V ? __float_as_uint(row[i + j]) : 0xff800000u;
+    }
+    if constexpr (sizeof(T) == 2)
+        return u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+    else
+        return u32x4{e[0], e[1], e[2], e[3]};
+}
+
+// the j-th of them
+template <class T>
+static __device__ __forceinline__ float bits_of(u32x4 w, int j)
 {
     if constexpr (sizeof(T) == 2)
-        return __uint_as_float((uint32_t)p[i] << 16);
+        return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
     else
-        return p[i];
+        return __uint_as_float(w[j]);
 }
 
+// NaN as -infinity
 template <class T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(Sample a)
+static __device__ __forceinline__ float logit_of(u32x4 w, int j)
 {
-    __shared__ unsigned long long mass[256];
-    __shared__ uint32_t count[256];
-    __shared__ unsigned long long parts[kWaves];
-    __shared__ int counts[kWaves];
-    __shared__ unsigned long long found_mass;
-    __shared__ int found_digit, found_at;
-    __shared__ uint32_t found_count;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = (int)a.V;
-    const int64_t r = blockIdx.x;
-    const T *const row = reinterpret_cast<const T *>(a.logits) + r * a.ld;
+    const float x = bits_of<T>(w, j);
+    return x == x ? x : -__builtin_inff();
+}
 
-    // the first of the order: the largest key, the lowest index
-    unsigned long long best = 0;
-    for (int i = tid; i < V; i += kThreads) best = max(best, ((unsigned long long)key_of(load_logit(row, i)) << 32) | (uint32_t)~i);
+// bits_of for a j that is not known to the compiler
+template <class T>
+static __device__ __forceinline__ float pick(u32x4 w, int j)
+{
+    const int k = sizeof(T) == 2 ? j >> 1 : j;
+    uint32_t v = w[0];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) best = max(best, (unsigned long long)__shfl_xor((long long)best, d));
-    if (lane == 0) parts[wave] = best;
+    for (int i = 1; i < 4; ++i) v = k == i ? w[i] : v;
+    if constexpr (sizeof(T) == 2) v = j & 1 ? v & 0xffff0000u : v << 16;
+    return __uint_as_float(v);
+}
+
+template <class T, class F>
+static __device__ __forceinline__ T wave_fold(T v, F &&f)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v = f(v, __shfl_xor(v, d));
+    return v;
+}
+
+// One chunk of kChunk logits.  They stay in LDS, so that the loop over them is no longer than its body: unrolled, the
+// code alone (12 KB read once by each compute unit) takes longer than the logits.
+template <class T>
+__global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables t, int64_t row0, int chunks)
+{
+    constexpr int N = 16 / sizeof(T), NV = kChunk / kChunkThreads / N, NW = kChunkThreads / 64;
+    __shared__ u32x4 stage[NV][kChunkThreads];
+    __shared__ u64 bins[kBins];
+    __shared__ float tops[NW];
+    __shared__ int firsts[NW];
+    __shared__ double sums[NW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = (int)a.V;
+    const int local = blockIdx.x / chunks, c = blockIdx.x - local * chunks, base = c * kChunk;
+    const int64_t r = row0 + local;
+    const T *const row = reinterpret_cast<const T *>(a.logits) + r * a.ld;
+    const Setting s = setting_of(a, r);
+    float top = -__builtin_inff();
+    {
+        u32x4 x[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) x[j] = load16(row, base + (j * kChunkThreads + tid) * N, V);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            stage[j][tid] = x[j];
+#pragma unroll
+            for (int i = 0; i < N; ++i) top = fmaxf(top, logit_of<T>(x[j], i));
+        }
+    }
+    top = wave_fold(top, [](float u, float v) { return fmaxf(u, v); });
+    if (lane == 0) tops[wave] = top;
+    bins[tid] = 0;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) best = max(best, parts[w]);
-    __syncthreads();
-    const uint32_t top_key = (uint32_t)(best >> 32);
-    const float top = value_of(top_key);
-    const float t = a.temperature ? a.temperature[r] : 1.0f, p = a.top_p ? a.top_p[r] : 1.0f, mp = a.min_p ? a.min_p[r] : 0.0f;
-    const int k = a.top_k ? a.top_k[r] : 0;
-    if (top == -__builtin_inff() || !(t > 0.0f) || k == 1 || !(p > 0.0f) || mp != mp || mp > 1.0f) {
-        if (tid == 0) a.tokens[r] = top == -__builtin_inff() ? -1 : (int)~(uint32_t)best;
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, tops[w]);
+    Chunk *const out = t.chunks + blockIdx.x;
+    if (s.largest) {
+        int first = 0x7fffffff;
+#pragma unroll 1
+        for (int j = NV - 1; j >= 0; --j) {
+            const u32x4 x = stage[j][tid];
+#pragma unroll
+            for (int i = N - 1; i >= 0; --i)
+                if (logit_of<T>(x, i) == top) first = base + (j * kChunkThreads + tid) * N + i;
+        }
+        first = wave_fold(first, [](int u, int v) { return min(u, v); });
+        if (lane == 0) firsts[wave] = first;
+        __syncthreads();
+        if (tid == 0) {
+#pragma unroll
+            for (int w = 0; w < NW; ++w) first = min(first, firsts[w]);
+            *out = Chunk{top, first, 0.0};
+        }
         return;
     }
-    auto weight = [&](uint32_t key) -> double {
-        const float x = value_of(key);
-        if (x == top) return 1.0;
-        return x == -__builtin_inff() || top == __builtin_inff() ? 0.0 : exp(((double)x - (double)top) / (double)t);
-    };
-    auto whole = [&](double w) { return (unsigned long long)(w * kUnit + 0.5); };
-
-    // The border: the first element of the order with which the count, or the mass, reaches the limit.  `ties` of the elements with
-    // border_key are kept, `before` is the mass in front of them.
-    uint32_t border_key = 0;
-    long long ties = V;
-    auto find = [&](bool by_mass, double limit, unsigned long long &before) {
-        uint32_t prefix = 0, n_before = 0;
-        before = 0;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) mass[tid] = 0, count[tid] = 0;
-            __syncthreads();
-            for (int i = tid; i < V; i += kThreads) {
-                const uint32_t key = key_of(load_logit(row, i));
-                if (shift < 24 && (key >> (shift + 8)) != prefix) continue;
-                atomicAdd(&count[key >> shift & 255], 1u);
-                atomicAdd(&mass[key >> shift & 255], whole(weight(key)));
+    const double edge = floor(pos_of(top, top, s.scale));  // the largest logit's bin
+    if (!s.filters || top == -__builtin_inff()) {
+        if (s.filters && tid == 0 && c == 0) t.rows[local].listed = 0;
+        double sum = 0.0;
+        const double by = s.scale / 8, from = (edge + 1.0) / 8;
+        const bool finite = top != __builtin_inff();
+#pragma unroll 1
+        for (int j = 0; j < NV; ++j) {
+            const u32x4 x = stage[j][tid];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float y = logit_of<T>(x, i);
+                const bool some = weighs(y, top);
+                const double w = power((double)(finite && some ? y : 0.0f) * by - from);
+                sum += some ? w : 0.0;
             }
-            __syncthreads();
-            if (tid == 0) {
-                int d = 255, last = 0;
-                for (; d >= 0; --d) {
-                    if (!count[d]) continue;
-                    last = d;
-                    if (by_mass ? (double)(before + mass[d]) >= limit : (double)(n_before + count[d]) >= limit) break;
-                    before += mass[d], n_before += count[d];
-                }
-                if (d < 0) before -= mass[last], n_before -= count[last], d = last;  // (the limit is beyond all of them)
-                found_digit = d, found_mass = before, found_count = n_before;
-            }
-            __syncthreads();
-            prefix = prefix << 8 | (uint32_t)found_digit, before = found_mass, n_before = found_count;
-            __syncthreads();
         }
-        border_key = prefix;
-        const unsigned long long w = whole(weight(prefix));
-        if (!by_mass)
-            ties = (long long)(limit - n_before);
-        else
-            ties = w == 0 ? 1 : max((long long)ceil((limit - (double)before) / (double)w), 1ll);
-    };
-    unsigned long long before = 0, all = 0;
-    auto sum_of = [&](auto &&of) {
-        unsigned long long s = 0;
-        for (int i = tid; i < V; i += kThreads) s += of(key_of(load_logit(row, i)));
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) s += (unsigned long long)__shfl_xor((long long)s, d);
-        if (lane == 0) parts[wave] = s;
+        sum = wave_fold(sum, [](double u, double v) { return u + v; });
+        if (lane == 0) sums[wave] = sum;
         __syncthreads();
-        s = 0;
+        if (tid == 0) {
+            sum = 0.0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) s += parts[w];
-        __syncthreads();
-        return s;
-    };
-    if (k > 0 && k < V) find(false, k, before);
-    if (p < 1.0f) {
-        const unsigned long long w = whole(weight(border_key));
-        all = border_key ? before + (unsigned long long)ties * w : sum_of([&](uint32_t key) { return whole(weight(key)); });
-        find(true, (double)p * (double)all, before);
-    }
-    auto kept = [&](uint32_t key) { return key >= border_key && (key == top_key || weight(key) >= (double)mp); };
-
-    // the kept tokens in the order of their indices, a thousand at a time, twice: their mass, then where it passes the draw
-    unsigned long long total = 0, aim = 0;
-    for (int pass = 0; pass < 2; ++pass) {
-        unsigned long long sum = 0;
-        long long seen = 0;
-        if (tid == 0) found_at = -1;
-        for (int base = 0; base < V; base += kThreads) {
-            const int i = base + tid;
-            const uint32_t key = i < V ? key_of(load_logit(row, i)) : 0;
-            const bool tie = i < V && key == border_key;
-            const unsigned long long tied = __ballot(tie);
-            if (lane == 0) counts[wave] = __popcll(tied);
-            __syncthreads();
-            long long rank = seen + __popcll(tied & ((1ull << lane) - 1));
-            for (int w = 0; w < kWaves; ++w) {
-                if (w < wave) rank += counts[w];
-                seen += counts[w];
-            }
-            unsigned long long m = i < V && kept(key) && (!tie || rank < ties) ? whole(weight(key)) : 0, upto = m;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const unsigned long long u = (unsigned long long)__shfl_up((long long)upto, d);
-                if (lane >= d) upto += u;
-            }
-            if (lane == 63) parts[wave] = upto;
-            __syncthreads();
-            unsigned long long front = sum;
-            for (int w = 0; w < kWaves; ++w) {
-                if (w < wave) front += parts[w];
-                sum += parts[w];
-            }
-            if (pass && m && front <= aim && front + upto > aim && front + upto - m <= aim) found_at = i;
-            __syncthreads();
+            for (int w = 0; w < NW; ++w) sum += sums[w];
+            *out = Chunk{top, 0, sum};
         }
-        total = sum;
-        const double u = (double)a.uniform[r] * (double)total;
-        aim = u > 0.0 ? (u < (double)total ? (unsigned long long)u : total - 1) : 0;
-        aim = min(aim, total - 1);
+        return;
     }
-    if (tid == 0) a.tokens[r] = found_at;
+#pragma unroll 1
+    for (int j = 0; j < NV; ++j) {
+        const u32x4 x = stage[j][tid];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float y = logit_of<T>(x, i);
+            const double pos = pos_of(y, top, s.scale), q = floor(pos), below = edge - q;
+            // 2^52 more than the shortfall, whose bits are then the low ones
+            const double d = __builtin_fma(in_bin(pos - q), -kFine, kFine + 0x1p52);
+            if (weighs(y, top) && below < kBins) atomicAdd(&bins[(int)below], (1ull << kCountBit) + (__builtin_bit_cast(u64, d) - 0x4330000000000000ull));
+        }
+    }
+    __syncthreads();
+    // counts and masses up to each bin
+    const u64 bin = bins[tid];
+    int count = (int)(bin >> kCountBit);
+    double mass = ((double)((u64)count << 34) - (double)(bin & ((1ull << kCountBit) - 1))) * (1.0 / kFine) * power(-0.125 * tid);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int n = __shfl_up(count, d);
+        const double m = __shfl_up(mass, d);
+        if (lane >= d) count += n, mass += m;
+    }
+    if (lane == 63) firsts[wave] = count, sums[wave] = mass;
+    __syncthreads();
+    int n = 0;
+    double m = 0.0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+        if (w < wave) n += firsts[w], m += sums[w];
+    count += n, mass = m + mass;
+    t.upto[(int64_t)blockIdx.x * kBins + tid] = Upto{mass, count};
+    if (tid == kBins - 1) *out = Chunk{top, 0, mass};
+    if (tid == 0 && c == 0) t.rows[local].listed = 0;
 }
+static_assert(kChunkThreads == kBins, "a thread for each bin");
+
+constexpr int kFew = 128;  // tokens that are compared each with each
+
+struct Token {
+    u64 number, weight;  // its place in the order (the first the largest), its weight in 2^-40 of its bin's top
+};
+
+// Tokens as numbers in their order: 36 bits, or 52
+static_assert(kSampleTokens == 1 << 20, "the bits of an index");
+template <class T>
+static __device__ __forceinline__ u64 number_of(uint32_t key, int i)
+{
+    return (u64)(sizeof(T) == 2 ? key >> 16 : key) << 20 | (0xfffff - i);
+}
+
+// What of a row's borders goes by the bins alone: the bins of the three borders, those of the mass's between what it is at least
+// and at most (what the first k have is only known to a bin)
+struct Borders {
+    int k, m, p0, p1;
+    bool part_k;  // whether the first k end inside their bin
+};
+template <class F>
+static __device__ __forceinline__ Borders borders_of(const Setting &s, double peak, double edge, const double *masses, const int *counts, int tid, double &limit_m, F &&sync_count)
+{
+    Borders b{kBins, kBins, kBins, kBins, false};
+    limit_m = -__builtin_inf();
+    if (s.min_p > 0.0f) {
+        limit_m = peak + 8.0 * log2((double)s.min_p);
+        b.m = (int)fmin(edge - floor(limit_m), (double)kBins);
+    }
+    if (s.k > 0) b.k = sync_count(tid < kBins && counts[tid] < s.k);
+    double most = masses[kBins - 1], least = most;
+    if (b.k < kBins) {
+        most = least = masses[b.k];
+        b.part_k = counts[b.k] > s.k;
+        if (b.part_k) least = b.k > 0 ? masses[b.k - 1] : 0.0;
+    }
+    if (s.p < 1.0f) {
+        b.p0 = min(sync_count(tid < kBins && masses[tid] < (double)s.p * least), b.k);
+        b.p1 = min(sync_count(tid < kBins && masses[tid] < (double)s.p * most), b.k);
+    }
+    return b;
+}
+
+// A row's counts and masses up to each bin, and the tokens of the bins that a border is in, a part of the row's chunks by each
+// workgroup.
+template <class T>
+__global__ __launch_bounds__(kRowThreads) void sample_border(Sample a, Tables t, int64_t row0, int chunks, int parts)
+{
+    constexpr int NT = kRowThreads, N = 16 / sizeof(T);
+    constexpr float kInf = __builtin_inff();
+    __shared__ float tops[kChunksMost];
+    __shared__ int shifts[kChunksMost];
+    __shared__ double scales[kChunksMost], masses[kBins];
+    __shared__ int counts[kBins];
+    __shared__ bool need[kBins + 1];
+    __shared__ u64 list[kList];
+    __shared__ int listed, at;
+    const int tid = threadIdx.x, lane = tid & 63, V = (int)a.V, local = blockIdx.x / parts, part = blockIdx.x - local * parts;
+    const int64_t r = row0 + local;
+    const Setting s = setting_of(a, r);
+    if (!s.filters || s.largest) return;
+    const Chunk *const heads = t.chunks + (int64_t)local * chunks;
+    const Upto *const upto = t.upto + (int64_t)local * chunks * kBins;
+    Row &out = t.rows[local];
+    float own = -kInf;
+    if (tid < chunks) tops[tid] = own = heads[tid].top;
+    __syncthreads();
+    float top = -kInf;
+    for (int c = lane; c < chunks; c += 64) top = fmaxf(top, tops[c]);
+    top = wave_fold(top, [](float u, float v) { return fmaxf(u, v); });
+    if (top == -kInf) return;
+    const double peak = pos_of(top, top, s.scale), edge = floor(peak);
+    if (tid < chunks) {
+        const double below = own == top ? 0.0 : !weighs(own, top) ? kBins : fmin(edge - floor(own * s.scale), (double)kBins);
+        shifts[tid] = (int)below;
+        scales[tid] = power(-0.125 * below);
+    }
+    if (tid <= kBins) need[tid] = false;
+    if (tid == 0) listed = 0;
+    __syncthreads();
+    {  // half of the chunks by each half of the threads
+        const int b = tid & (kBins - 1), half = tid / kBins;
+        double m = 0.0;
+        int n = 0;
+#pragma unroll 8
+        for (int c = half; c < chunks; c += NT / kBins) {
+            const int i = b - shifts[c];
+            const Upto u = upto[c * kBins + max(i, 0)];
+            if (i >= 0) m += u.mass * scales[c], n += u.count;
+        }
+        if (half) masses[b] = m, counts[b] = n;
+        __syncthreads();
+        if (!half) masses[b] += m, counts[b] += n;
+        __syncthreads();
+        if (part == 0 && !half) out.masses[b] = masses[b], out.counts[b] = counts[b];
+    }
+    static_assert(NT == 2 * kBins, "two halves");
+    double limit_m;
+    const Borders b = borders_of(s, peak, edge, masses, counts, tid, limit_m, [](bool x) { return __syncthreads_count(x); });
+    if (tid < kBins)
+        need[tid] = (tid == b.k && b.part_k && (s.p < 1.0f || b.k <= b.m)) || (tid >= b.p0 && tid <= b.p1 && tid <= b.m) || (tid == b.m && b.m <= b.k && b.m <= b.p1);
+    __syncthreads();
+    const T *const row = reinterpret_cast<const T *>(a.logits) + r * a.ld;
+    const int first = (int)((int64_t)chunks * part / parts) * kChunk, end = min(V, (int)((int64_t)chunks * (part + 1) / parts) * kChunk);
+    // the bins' numbers, a token's in 64 bits
+#pragma unroll 1
+    for (int i0 = first + tid * N; i0 < end; i0 += NT * N) {
+        const u32x4 x = load16(row, i0, V);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float y = logit_of<T>(x, i);
+            const double below = edge - floor(pos_of(y, top, s.scale));
+            if (weighs(y, top) && below < kBins && need[(int)below]) {
+                const int slot = atomicAdd(&listed, 1);
+                if (slot < kList) list[slot] = number_of<T>(key_of(y), i0 + i);
+            }
+        }
+    }
+    __syncthreads();
+    if (tid == 0) at = listed > 0 ? atomicAdd(&out.listed, listed) : 0;
+    __syncthreads();
+    for (int i = tid; i < min(listed, kList - at); i += NT) out.list[at + i] = list[i];
+}
+
+struct RowLds {
+    float tops[kChunksMost];
+    int shift[kChunksMost];  // bins between the row's largest logit and the chunk's; kBins: its weights are none
+    double scale[kChunksMost], kept[kChunksMost];
+    u64 part[kChunksMost];  // what the border's bin adds to a chunk
+    double masses[kBins];   // of the bins up to each
+    int counts[kBins];
+    u64 list[kList];
+    Token few[kFew];
+    int listed;
+    int digit_counts[256];
+    u64 digit_masses[256];
+    u64 found_mass;
+    int found, found_n;
+    u64 cut;
+    u64 fronts[kRowThreads / 64];
+    int chosen;
+    double rest;
+};
+
+// One row by one workgroup.  What takes it is one trip to memory after another, and its own code, which each compute unit reads
+// once, from memory: so everything that looks at tokens stands here once, in loops.
+template <class T>
+__global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, int64_t row0, int chunks)
+{
+    constexpr int NT = kRowThreads, N = 16 / sizeof(T);
+    constexpr float kInf = __builtin_inff();
+    __shared__ RowLds l;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = (int)a.V;
+    const int64_t r = row0 + blockIdx.x;
+    const T *const row = reinterpret_cast<const T *>(a.logits) + r * a.ld;
+    const Chunk *const parts = t.chunks + (int64_t)blockIdx.x * chunks;
+    const Upto *const upto = t.upto + (int64_t)blockIdx.x * chunks * kBins;
+    const Row &known = t.rows[blockIdx.x];
+    const Setting s = setting_of(a, r);
+    Chunk own{-kInf, 0, 0.0};
+    if (tid < chunks) own = parts[tid], l.tops[tid] = own.top;
+    const bool filters = s.filters && !s.largest;
+    const int listed = filters ? known.listed : 0;
+    if (filters) {
+        if (tid < kBins) l.masses[tid] = known.masses[tid], l.counts[tid] = known.counts[tid];
+#pragma unroll
+        for (int i = 0; i < kList / NT; ++i)
+            if (i * NT + tid < listed) l.list[i * NT + tid] = known.list[i * NT + tid];
+    }
+    __syncthreads();
+    float top = -kInf;
+    for (int c = lane; c < chunks; c += 64) top = fmaxf(top, l.tops[c]);
+    top = wave_fold(top, [](float u, float v) { return fmaxf(u, v); });
+    if (s.largest || top == -kInf) {
+        if (wave == 0) {
+            int first = 0x7fffffff;
+            for (int c = lane; c < chunks; c += 64)
+                if (l.tops[c] == top) first = min(first, parts[c].first);
+            first = wave_fold(first, [](int u, int v) { return min(u, v); });
+            if (lane == 0) a.tokens[r] = top == -kInf ? -1 : first;
+        }
+        return;
+    }
+    const double peak = pos_of(top, top, s.scale), edge = floor(peak);
+    if (tid < chunks) {
+        const double below = own.top == top ? 0.0 : !weighs(own.top, top) ? kBins : fmin(edge - floor(own.top * s.scale), (double)kBins);
+        l.shift[tid] = (int)below;
+        l.scale[tid] = below < kBins ? power(-0.125 * below) : 0.0;
+        l.kept[tid] = own.mass * l.scale[tid];
+        l.part[tid] = 0;
+    }
+    __syncthreads();
+
+    auto value_of_number = [](u64 number) {
+        const uint32_t key = (uint32_t)(number >> 20);
+        return value_of(sizeof(T) == 4 ? key : key << 16 | (key >> 15 ? 0u : 0xffffu));
+    };
+    // The lowest logit (as a key) with a pos of at least `limit` that has weight: pos is monotonous in it, and the quotient less than a step off
+    auto lowest = [&](double limit) -> uint32_t {
+        if (top == kInf) return 0xff800000u;
+        if (s.scale == 0.0) return 0x00800000u;
+        const float y = (float)fmin(fmax(limit * s.inverse, -3.4028234663852886e38), 3.4028234663852886e38);
+        uint32_t key = key_of(y) - 2;
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) key += (double)value_of(key) * s.scale < limit;
+        return max(key, 0x00800000u);
+    };
+    // the lowest number of a logit from `key` on (16 bits of a key stand for the first of 65536 above zero, below for the last)
+    auto number_from = [&](uint32_t key) { return number_of<T>(sizeof(T) == 2 && key >> 31 ? key + 0xffffu : key, 0xfffff); };
+    auto first_of = [&](int b) { return lowest(edge - b); };                       // of bin b's logits
+
+    // The least number that is kept, and its bin: the filters' borders are such numbers, and the highest of them counts
+    u64 cut = number_of<T>(top == kInf ? 0xff800000u : 0x00800000u, 0xfffff);
+    if (filters) {
+        auto mass_to = [&](int b) { return b > 0 ? l.masses[b - 1] : 0.0; };  // of the bins in front of b
+        auto count_in = [&](int b) { return l.counts[b] - (b > 0 ? l.counts[b - 1] : 0); };
+        auto reaching = [&](double limit) { return __syncthreads_count(tid < kBins && l.masses[tid] < limit); };
+        double limit_m;
+        const Borders known_to = borders_of(s, peak, edge, l.masses, l.counts, tid, limit_m, [](bool x) { return __syncthreads_count(x); });
+        const int bin_m = known_to.m, bin_k = known_to.k;
+        int bin_p = kBins;
+        if (s.min_p > 0.0f) cut = max(cut, number_from(lowest(limit_m)));
+        double all = l.masses[min(bin_k, kBins - 1)], limit_p = 0.0;
+
+        // The border of the first k in its bin, that of the mass in its, and what is kept of the last bin, each where it is needed.
+        // A pass reads the tokens of a bin, from the list or, where that is not whole, from the row: into 256 classes by eight bits of
+        // their numbers, the few left ones into a list of their own, or what is kept of them into the chunks' masses.
+        enum { kNew = 8, kCount = 0, kMass, kRest };
+        enum { kToDigits, kToFew, kToParts };
+        int count = 0, n = 0;          // tokens between lo and hi, and above hi
+        u64 lo = 0, hi = 0, mass = 0;  // and the mass above hi
+        bool whole = false;            // whether all of the last bin is kept
+        double limit = 0.0;
+        auto look_at = [&](int b) {
+            n = 0, mass = 0, count = count_in(b);
+            lo = number_from(first_of(b)), hi = b > 0 ? number_from(first_of(b - 1)) - 1 : number_of<T>(~0u, 0);
+        };
+#pragma unroll 1
+        for (int task = kNew + kCount;;) {
+            if (task == kNew + kCount) {
+                task = kNew + kMass;
+                if (bin_k < kBins) {
+                    if (!known_to.part_k) {
+                        cut = max(cut, number_from(first_of(bin_k)));
+                    } else if (s.p < 1.0f || bin_k <= bin_m) {
+                        task = kCount;
+                        look_at(bin_k);
+                        limit = (double)(s.k - l.counts[bin_k] + count);
+                    }
+                }
+            }
+            if (task == kNew + kMass) {
+                task = kNew + kRest;
+                if (s.p < 1.0f) {
+                    limit_p = (double)s.p * all;
+                    bin_p = min(reaching(limit_p), bin_k);
+                    if (bin_p < kBins && bin_p <= bin_m) {
+                        task = kMass;
+                        look_at(bin_p);
+                        limit = (limit_p - mass_to(bin_p)) * (0x1p40 / power(-0.125 * bin_p));
+                    }
+                }
+            }
+            if (task == kNew + kRest) {
+                task = kRest;
+                const int b = min(min(bin_k, bin_p), bin_m);
+                if (b == kBins) break;
+                look_at(b);
+                if (cut <= lo) {
+                    whole = true;
+                    break;
+                }
+            }
+            // one pass
+            const int what = task == kRest ? kToParts : count > kFew ? kToDigits : kToFew;
+            const int shift = max(64 - __clzll((long long)(lo ^ hi)) - 8, 0);
+            const u64 from = what == kToParts ? max(lo, cut) : lo;
+            if (tid < 256) l.digit_counts[tid] = 0, l.digit_masses[tid] = 0;
+            if (tid == 0) l.listed = 0;
+            __syncthreads();
+            auto take = [&](u64 number) {
+                if (number < from || number > hi) return;
+                const double pos = pos_of(value_of_number(number), top, s.scale);
+                const u64 weight = (u64)(in_bin(pos - floor(pos)) * 0x1p40 + 0.5);
+                if (what == kToParts) {
+                    atomicAdd(&l.part[(0xfffff - (int)(number & 0xfffff)) / kChunk], weight);
+                } else if (what == kToDigits) {
+                    const int d = (int)(number >> shift) & 255;
+                    atomicAdd(&l.digit_counts[d], 1);
+                    atomicAdd(&l.digit_masses[d], weight);
+                } else {
+                    const int slot = atomicAdd(&l.listed, 1);
+                    if (slot < kFew) l.few[slot] = Token{number, weight};
+                }
+            };
+            if (listed <= kList) {
+#pragma unroll 1
+                for (int i = tid; i < listed; i += NT) take(l.list[i]);
+            } else {
+#pragma unroll 1
+                for (int i0 = tid * N; i0 < V; i0 += NT * N) {
+                    const u32x4 x = load16(row, i0, V);
+#pragma unroll 1
+                    for (int i = 0; i < N; ++i) {
+                        const float y = pick<T>(x, i);
+                        if (y == y) take(number_of<T>(key_of(y), i0 + i));
+                    }
+                }
+            }
+            __syncthreads();
+            if (what == kToParts) break;
+            if (what == kToDigits) {
+                if (wave == 0) {  // a lane takes four classes, the highest first
+                    int dn[4], sn = 0;
+                    u64 dm[4], sm = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dn[i] = l.digit_counts[255 - 4 * lane - i], dm[i] = l.digit_masses[255 - 4 * lane - i], sn += dn[i], sm += dm[i];
+                    int fn = sn;
+                    u64 fm = sm;
+#pragma unroll
+                    for (int d = 1; d < 64; d <<= 1) {
+                        const int un = __shfl_up(fn, d);
+                        const u64 um = (u64)__shfl_up((long long)fm, d);
+                        if (lane >= d) fn += un, fm += um;
+                    }
+                    auto reaches = [&](int number, u64 sum) { return (task == kMass ? (double)sum : (double)number) >= limit; };
+                    const u64 hits = __ballot(reaches(n + fn, mass + fm));
+                    if (lane == (hits ? __ffsll(hits) - 1 : 63)) {  // (rounding may leave the limit behind all of them)
+                        fn = n + fn - sn, fm = mass + fm - sm;
+                        bool done = false;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (done) continue;
+                            done = i == 3 || reaches(fn + dn[i], fm + dm[i]);
+                            if (done)
+                                l.found = 255 - 4 * lane - i;
+                            else
+                                fn += dn[i], fm += dm[i];
+                        }
+                        l.found_n = fn, l.found_mass = fm;
+                    }
+                }
+                __syncthreads();
+                n = l.found_n, mass = l.found_mass, count = l.digit_counts[l.found];
+                const u64 above = shift + 8 >= 64 ? 0 : hi >> (shift + 8) << (shift + 8), least = above | (u64)l.found << shift;
+                lo = max(lo, least), hi = min(hi, least | ((1ull << shift) - 1));  // (the first and last class may begin and end outside)
+                __syncthreads();
+                if (count > 0) continue;  // (none: the limit is behind all, so all are kept)
+            }
+            // the few left: how many are in front of each, and their mass; the one with which the limit is reached
+            if (tid == 0) l.cut = lo, l.found_mass = mass;
+            __syncthreads();
+            if (tid < count) {
+                const Token x = l.few[tid];
+                int fn = n;
+                u64 fm = mass;
+#pragma unroll 4
+                for (int i = 0; i < count; ++i) {
+                    const Token y = l.few[i];
+                    const bool front = y.number > x.number;
+                    fn += front, fm += front ? y.weight : 0;
+                }
+                const bool reached = task == kCount ? (double)(fn + 1) == limit : (double)fm < limit && (double)(fm + x.weight) >= limit;
+                if (reached) l.cut = x.number, l.found_mass = fm + x.weight;
+            }
+            __syncthreads();
+            cut = max(cut, l.cut);
+            if (task == kCount) all = mass_to(bin_k) + (double)l.found_mass * 0x1p-40 * power(-0.125 * bin_k);
+            task = kNew + task + 1;
+        }
+        const int border = min(min(bin_k, bin_p), bin_m);
+        if (border < kBins && tid < chunks) {
+            const int b = border - l.shift[tid] + whole;
+            const double m = b > 0 && l.shift[tid] < kBins ? upto[tid * kBins + b - 1].mass : 0.0;
+            l.kept[tid] = m * l.scale[tid] + (double)l.part[tid] * 0x1p-40 * power(-0.125 * border);
+        }
+        __syncthreads();
+    }
+
+    // the chunk that the draw falls into: sums over two chunks a lane
+    if (wave == 0) {
+        static_assert(kChunksMost == 128, "two a lane");
+        const double m0 = 2 * lane < chunks ? l.kept[2 * lane] : 0.0, m1 = 2 * lane + 1 < chunks ? l.kept[2 * lane + 1] : 0.0, sum = m0 + m1;
+        double front = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const double u = __shfl_up(front, d);
+            if (lane >= d) front += u;
+        }
+        const double total = __shfl(front, 63), u = (double)a.uniform[r];
+        const double aim = u > 0.0 ? fmin(u, 1.0 - 0x1p-40) * total : 0.0;
+        const u64 hits = __ballot(front > aim && sum > 0.0), some = __ballot(sum > 0.0);
+        if (lane == (hits ? __ffsll(hits) - 1 : 63 - __clzll((long long)some))) {  // (rounding may leave the draw behind the last)
+            const double before = front - sum;
+            const bool second = !(m0 > 0.0) || (m1 > 0.0 && before + m0 <= aim);
+            l.chosen = 2 * lane + second;
+            l.rest = aim - (second ? before + m0 : before);
+        }
+    }
+    __syncthreads();
+
+    // The token in it, eight side by side to a thread: weights in whole 2^-43 of the top of the chunk's first bin, so that all sums
+    // agree (what is kept of a chunk has its largest logit in it).
+    constexpr int kEach = kChunk / NT, kVectors = kEach / N;
+    const int chosen = l.chosen, first = chosen * kChunk + tid * kEach;
+    u32x4 x[kVectors];
+#pragma unroll
+    for (int j = 0; j < kVectors; ++j) x[j] = load16(row, min(first + j * N, V), V);
+    const double from = (floor(pos_of(l.tops[chosen], top, s.scale)) + 1.0) * 0.125;
+    u64 before = 0, aim = 0;
+    bool mine = false;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        u64 sum = 0;
+        int token = -1;
+#pragma unroll 1
+        for (int i = 0; i < kEach; ++i) {
+            u32x4 w = x[0];
+            if constexpr (kVectors == 2) w = i >= N ? x[1] : w;
+            const float y = pick<T>(w, i % N);
+            if (y == y && number_of<T>(key_of(y), first + i) >= cut && first + i < V) sum += (u64)(power(pos_of(y, top, s.scale) * 0.125 - from) * 0x1p43 + 0.5);
+            if (token < 0 && before + sum > aim) token = first + i;
+        }
+        if (pass) {
+            if (mine) a.tokens[r] = token;
+            break;
+        }
+        u64 front = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const u64 u = (u64)__shfl_up((long long)front, d);
+            if (lane >= d) front += u;
+        }
+        if (lane == 63) l.fronts[wave] = front;
+        __syncthreads();
+        u64 total = 0;
+        before = front - sum;
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) {
+            const u64 f = l.fronts[w];
+            if (w < wave) before += f;
+            total += f;
+        }
+        const double rest = l.rest / l.scale[chosen] * 0x1p43;
+        aim = min(rest > 0.0 ? (u64)fmin(rest, 0x1p62) : 0ull, total - 1);
+        mine = sum > 0 && before <= aim && aim < before + sum;
+        if (!__any(mine)) break;
+    }
+}
+
+// Rows of a launch: those of 64 MiB of workspace
+constexpr int64_t kSampleSpace = (int64_t)64 << 20;
+static int64_t chunks_of(int64_t V) { return (V + kChunk - 1) / kChunk; }
+static int64_t row_bytes(int64_t chunks) { return chunks * kChunkBytes + sizeof(Row); }
+static int64_t rows_of(int64_t rows, int64_t chunks) { return std::min(rows, std::max<int64_t>(kSampleSpace / row_bytes(chunks), 1)); }
 
 int64_t sample_workspace(int64_t rows, int64_t V)
 {
-    (void)rows, (void)V;
-    return 0;
+    const int64_t chunks = chunks_of(V);
+    return rows_of(rows, chunks) * row_bytes(chunks);
 }
 
-int launch_sample(const Sample &a, bool fp32, hipStream_t s)
+template <class T>
+static int sample_typed(const Sample &a, hipStream_t s)
 {
-    return fp32 ? enqueue(sample_kernel<float>, dim3((unsigned)a.rows), dim3(kThreads), 0, s, a)
-                : enqueue(sample_kernel<uint16_t>, dim3((unsigned)a.rows), dim3(kThreads), 0, s, a);
+    const int64_t chunks = chunks_of(a.V), most = rows_of(a.rows, chunks);
+    Chunk *const first = static_cast<Chunk *>(a.ws);
+    Upto *const upto = reinterpret_cast<Upto *>(first + most * chunks);
+    const Tables t{first, upto, reinterpret_cast<Row *>(upto + most * chunks * kBins)};
+    for (int64_t r = 0; r < a.rows; r += most) {
+        const int64_t n = std::min(most, a.rows - r);
+        auto go = [&](auto kernel, int64_t groups, int threads, auto... more) {
+            return enqueue(kernel, dim3((unsigned)groups), dim3(threads), 0, s, a, t, r, (int)chunks, more...);
+        };
+        if (int rc = go(sample_chunks<T>, n * chunks, kChunkThreads)) return rc;
+        if (a.top_k || a.top_p || a.min_p) {
+            const int64_t parts = std::min(chunks, std::max<int64_t>(512 / n, 1));
+            if (int rc = go(sample_border<T>, n * parts, kRowThreads, (int)parts)) return rc;
+        }
+        if (int rc = go(sample_rows<T>, n, kRowThreads)) return rc;
+    }
+    return MQ_OK;
 }
+
+int launch_sample(const Sample &a, bool fp32, hipStream_t s) { return fp32 ? sample_typed<float>(a, s) : sample_typed<uint16_t>(a, s); }
 
 }  // namespace mq

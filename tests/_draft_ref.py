@@ -76,7 +76,6 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         return int(order[0])
     with np.errstate(invalid="ignore", over="ignore"):
         w = np.where(x == top, 1.0, np.where((x == -np.inf) | (top == np.inf), 0.0, np.exp((x - top) / np.float64(temperature))))
-    w[w < 2.0 ** -44] = 0.0
     kept = order[:top_k] if top_k > 0 else order
     if top_p < 1:
         mass = np.cumsum(w[kept])
