@@ -21,7 +21,7 @@ typedef unsigned long long u64;
 constexpr int kBins = 512;
 constexpr int kCountBit = 47;  // a bin of a chunk: count << 47 | shortfall in 2^-34, at most 2^14 * 2^30.4
 constexpr double kFine = (double)(1ll << 34);
-constexpr int kChunkThreads = 512, kRowThreads = 1024;
+constexpr int kChunkThreads = 256, kRowThreads = 1024;
 constexpr int kChunk = 8192;  // logits
 constexpr int kChunksMost = (int)(kSampleTokens / kChunk);  // of a row
 
@@ -31,10 +31,14 @@ struct Chunk {
     double mass;  // over that of the top of the largest logit's bin
 };
 
-struct alignas(16) Upto {
-    double mass;
-    int count;
+// Count and mass of a chunk up to a bin in one word: count << 50 | mass in 2^-36 of the top of its largest logit's bin
+struct Upto {
+    u64 word;
 };
+constexpr int kUptoCount = 50;
+constexpr double kUptoUnit = 0x1p36;
+static __device__ __forceinline__ double mass_of(Upto u) { return (double)(u.word & ((1ull << kUptoCount) - 1)) * (1.0 / kUptoUnit); }
+static __device__ __forceinline__ int count_of(Upto u) { return (int)(u.word >> kUptoCount); }
 
 // What is known of a row with filters: the masses and counts up to each bin below its largest logit's, and the tokens, as numbers, of the
 // bins that a border may be in (listed may be more than there is room for)
@@ -107,6 +111,21 @@ static __device__ __forceinline__ double power(double y)
 #pragma unroll
     for (int i = 10; i >= 0; --i) w = __builtin_fma(w, z, c[i]);
     return __builtin_bit_cast(double, __builtin_bit_cast(u64, w) + (__builtin_bit_cast(u64, shifted) << 52));
+}
+
+// 2^(v / 32) from 2^(i / 32), i < 32, and a polynomial of order 4 about the nearest whole v, within 2e-12; nothing below 2^-1000
+static __device__ __forceinline__ double power32(double v, const double *powers)
+{
+    constexpr double h = 0.021660849392498290919;  // ln(2) / 32
+    v = fmax(v, -32000.0);
+    const double shifted = v + 0x1.8p52, z = v - (shifted - 0x1.8p52);
+    double w = h * h * h * h / 24;
+    w = __builtin_fma(w, z, h * h * h / 6);
+    w = __builtin_fma(w, z, h * h / 2);
+    w = __builtin_fma(w, z, h);
+    w = __builtin_fma(w, z, 1.0);
+    const int n = (int)(uint32_t)__builtin_bit_cast(u64, shifted);
+    return __builtin_ldexp(w * powers[n & 31], n >> 5);
 }
 
 // Logits as unsigned numbers of the same order, the two zeros as one
@@ -186,9 +205,10 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
     constexpr int N = 16 / sizeof(T), NV = kChunk / kChunkThreads / N, NW = kChunkThreads / 64;
     __shared__ u32x4 stage[NV][kChunkThreads];
     __shared__ u64 bins[kBins];
+    __shared__ int largest[kBins];
     __shared__ float tops[NW];
     __shared__ int firsts[NW];
-    __shared__ double sums[NW];
+    __shared__ double sums[NW], powers[32];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = (int)a.V;
     const int local = blockIdx.x / chunks, c = blockIdx.x - local * chunks, base = c * kChunk;
     const int64_t r = row0 + local;
@@ -206,9 +226,10 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
             for (int i = 0; i < N; ++i) top = fmaxf(top, logit_of<T>(x[j], i));
         }
     }
+    const float mine = top;
     top = wave_fold(top, [](float u, float v) { return fmaxf(u, v); });
     if (lane == 0) tops[wave] = top;
-    bins[tid] = 0;
+    bins[2 * tid] = bins[2 * tid + 1] = 0, largest[2 * tid] = largest[2 * tid + 1] = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < NW; ++w) top = fmaxf(top, tops[w]);
@@ -235,18 +256,24 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
     const double edge = floor(pos_of(top, top, s.scale));  // the largest logit's bin
     if (!s.filters || top == -__builtin_inff()) {
         if (s.filters && tid == 0 && c == 0) t.rows[local].listed = 0;
+        // (in 64 bits these few instructions take as long as the loads; NaN and -infinity come out as 2^-1000)
+        if (tid < 32) powers[tid] = power(0.03125 * tid);
+        __syncthreads();
         double sum = 0.0;
-        const double by = s.scale / 8, from = (edge + 1.0) / 8;
-        const bool finite = top != __builtin_inff();
+        const double from = -(edge + 1.0) * 4;
+        if (top == __builtin_inff()) {
 #pragma unroll 1
-        for (int j = 0; j < NV; ++j) {
-            const u32x4 x = stage[j][tid];
+            for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float y = logit_of<T>(x, i);
-                const bool some = weighs(y, top);
-                const double w = power((double)(finite && some ? y : 0.0f) * by - from);
-                sum += some ? w : 0.0;
+                for (int i = 0; i < N; ++i) sum += bits_of<T>(stage[j][tid], i) == top ? powers[28] * 0.5 : 0.0;  // (2^(-1/8), the bottom of its bin)
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < NV; ++j) {
+                const u32x4 x = stage[j][tid];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    sum += power32(__builtin_fma((double)bits_of<T>(x, i) * s.scale, 4.0, from), powers);
+                }
             }
         }
         sum = wave_fold(sum, [](double u, double v) { return u + v; });
@@ -260,42 +287,81 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
         }
         return;
     }
+    // Bins behind which nothing counts: behind those of the largest k of the threads' largest, and behind what min_p leaves where the
+    // mass of the others is not asked for.  An addition in LDS to a bin that lanes share waits for them (all filters on 64 rows of 151673: 22.4 us, 14.9 so).
+    double last = kBins - 1;
+    if (s.k > 0 && s.k <= kChunkThreads) {
+        const double below = edge - floor(pos_of(mine, top, s.scale));
+        if (weighs(mine, top) && below < kBins) atomicAdd(&largest[(int)below], 1);
+        __syncthreads();
+        const int n0 = largest[2 * tid], n1 = n0 + largest[2 * tid + 1];
+        int n = n1;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int u = __shfl_up(n, d);
+            if (lane >= d) n += u;
+        }
+        if (lane == 63) firsts[wave] = n;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            if (w < wave) n += firsts[w];
+        const int before = n - n1;
+        last = fmin(last, (double)(__syncthreads_count(n < s.k) + __syncthreads_count(before + n0 < s.k)));
+    }
+    if (s.min_p > 0.0f && s.p >= 1.0f) last = fmin(last, 1.0 - floor(8.0 * log2((double)s.min_p)));
+    const bool finite = top != __builtin_inff();
 #pragma unroll 1
     for (int j = 0; j < NV; ++j) {
         const u32x4 x = stage[j][tid];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float y = logit_of<T>(x, i);
-            const double pos = pos_of(y, top, s.scale), q = floor(pos), below = edge - q;
-            // 2^52 more than the shortfall, whose bits are then the low ones
-            const double d = __builtin_fma(in_bin(pos - q), -kFine, kFine + 0x1p52);
-            if (weighs(y, top) && below < kBins) atomicAdd(&bins[(int)below], (1ull << kCountBit) + (__builtin_bit_cast(u64, d) - 0x4330000000000000ull));
+            const float y = bits_of<T>(x, i);
+            const double pos = finite ? (double)y * s.scale : y == top ? 0.0 : -0x1p1000, q = floor(pos), below = edge - q;
+            if (below <= last) {  // (not for NaN and -infinity)
+                // 2^52 more than the shortfall, whose bits are then the low ones
+                const double d = __builtin_fma(in_bin(pos - q), -kFine, kFine + 0x1p52);
+                atomicAdd(&bins[(int)below], (1ull << kCountBit) + (__builtin_bit_cast(u64, d) - 0x4330000000000000ull));
+            }
         }
     }
     __syncthreads();
-    // counts and masses up to each bin
-    const u64 bin = bins[tid];
-    int count = (int)(bin >> kCountBit);
-    double mass = ((double)((u64)count << 34) - (double)(bin & ((1ull << kCountBit) - 1))) * (1.0 / kFine) * power(-0.125 * tid);
+    // counts and masses up to each bin, two to a thread
+    int count[2];
+    double mass[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const u64 bin = bins[2 * tid + i];
+        count[i] = (int)(bin >> kCountBit);
+        mass[i] = ((double)((u64)count[i] << 34) - (double)(bin & ((1ull << kCountBit) - 1))) * (1.0 / kFine) * power(-0.25 * tid - 0.125 * i);
+    }
+    int n = count[0] + count[1];
+    double m = mass[0] + mass[1];
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int n = __shfl_up(count, d);
-        const double m = __shfl_up(mass, d);
-        if (lane >= d) count += n, mass += m;
+        const int u = __shfl_up(n, d);
+        const double v = __shfl_up(m, d);
+        if (lane >= d) n += u, m += v;
     }
-    if (lane == 63) firsts[wave] = count, sums[wave] = mass;
+    if (lane == 63) firsts[wave] = n, sums[wave] = m;
+    const int own_n = __shfl_up(n, 1);
+    const double own_m = __shfl_up(m, 1);
+    n = lane > 0 ? own_n : 0, m = lane > 0 ? own_m : 0.0;
     __syncthreads();
-    int n = 0;
-    double m = 0.0;
 #pragma unroll
     for (int w = 0; w < NW; ++w)
         if (w < wave) n += firsts[w], m += sums[w];
-    count += n, mass = m + mass;
-    t.upto[(int64_t)blockIdx.x * kBins + tid] = Upto{mass, count};
-    if (tid == kBins - 1) *out = Chunk{top, 0, mass};
+    Upto out2[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        n += count[i], m += mass[i];
+        out2[i] = Upto{(u64)n << kUptoCount | (u64)(m * kUptoUnit + 0.5)};
+    }
+    *reinterpret_cast<u32x4 *>(t.upto + (int64_t)blockIdx.x * kBins + 2 * tid) = __builtin_bit_cast(u32x4, out2);
+    if (tid == kChunkThreads - 1) *out = Chunk{top, 0, m};
     if (tid == 0 && c == 0) t.rows[local].listed = 0;
 }
-static_assert(kChunkThreads == kBins, "a thread for each bin");
+static_assert(2 * kChunkThreads == kBins, "two bins a thread");
 
 constexpr int kFew = 128;  // tokens that are compared each with each
 
@@ -385,7 +451,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_border(Sample a, Tables t,
         for (int c = half; c < chunks; c += NT / kBins) {
             const int i = b - shifts[c];
             const Upto u = upto[c * kBins + max(i, 0)];
-            if (i >= 0) m += u.mass * scales[c], n += u.count;
+            if (i >= 0) m += mass_of(u) * scales[c], n += count_of(u);
         }
         if (half) masses[b] = m, counts[b] = n;
         __syncthreads();
@@ -421,34 +487,36 @@ __global__ __launch_bounds__(kRowThreads) void sample_border(Sample a, Tables t,
     for (int i = tid; i < min(listed, kList - at); i += NT) out.list[at + i] = list[i];
 }
 
+template <bool F>
 struct RowLds {
     float tops[kChunksMost];
     int shift[kChunksMost];  // bins between the row's largest logit and the chunk's; kBins: its weights are none
     double scale[kChunksMost], kept[kChunksMost];
     u64 part[kChunksMost];  // what the border's bin adds to a chunk
-    double masses[kBins];   // of the bins up to each
-    int counts[kBins];
-    u64 list[kList];
-    Token few[kFew];
+    double masses[F ? kBins : 1];  // of the bins up to each
+    int counts[F ? kBins : 1];
+    u64 list[F ? kList : 1];
+    Token few[F ? kFew : 1];
     int listed;
-    int digit_counts[256];
-    u64 digit_masses[256];
+    int digit_counts[F ? 256 : 1];
+    u64 digit_masses[F ? 256 : 1];
     u64 found_mass;
     int found, found_n;
     u64 cut;
     u64 fronts[kRowThreads / 64];
+    double powers[32];
     int chosen;
     double rest;
 };
 
 // One row by one workgroup.  What takes it is one trip to memory after another, and its own code, which each compute unit reads
-// once, from memory: so everything that looks at tokens stands here once, in loops.
-template <class T>
+// once, from memory: so everything that looks at tokens stands here once, in loops.  F: rows may have filters.
+template <class T, bool F>
 __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, int64_t row0, int chunks)
 {
     constexpr int NT = kRowThreads, N = 16 / sizeof(T);
     constexpr float kInf = __builtin_inff();
-    __shared__ RowLds l;
+    __shared__ RowLds<F> l;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = (int)a.V;
     const int64_t r = row0 + blockIdx.x;
     const T *const row = reinterpret_cast<const T *>(a.logits) + r * a.ld;
@@ -458,9 +526,10 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     const Setting s = setting_of(a, r);
     Chunk own{-kInf, 0, 0.0};
     if (tid < chunks) own = parts[tid], l.tops[tid] = own.top;
-    const bool filters = s.filters && !s.largest;
-    const int listed = filters ? known.listed : 0;
-    if (filters) {
+    if (tid < 32) l.powers[tid] = power(0.03125 * tid);
+    const bool filters = F && s.filters && !s.largest;
+    [[maybe_unused]] const int listed = filters ? known.listed : 0;
+    if (F && filters) {
         if (tid < kBins) l.masses[tid] = known.masses[tid], l.counts[tid] = known.counts[tid];
 #pragma unroll
         for (int i = 0; i < kList / NT; ++i)
@@ -510,7 +579,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
 
     // The least number that is kept, and its bin: the filters' borders are such numbers, and the highest of them counts
     u64 cut = number_of<T>(top == kInf ? 0xff800000u : 0x00800000u, 0xfffff);
-    if (filters) {
+    if constexpr (F) if (filters) {
         auto mass_to = [&](int b) { return b > 0 ? l.masses[b - 1] : 0.0; };  // of the bins in front of b
         auto count_in = [&](int b) { return l.counts[b] - (b > 0 ? l.counts[b - 1] : 0); };
         auto reaching = [&](double limit) { return __syncthreads_count(tid < kBins && l.masses[tid] < limit); };
@@ -649,18 +718,23 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
             // the few left: how many are in front of each, and their mass; the one with which the limit is reached
             if (tid == 0) l.cut = lo, l.found_mass = mass;
             __syncthreads();
-            if (tid < count) {
-                const Token x = l.few[tid];
-                int fn = n;
-                u64 fm = mass;
+            {
+                constexpr int kLanes = NT / kFew;  // that share a token's comparisons
+                const int own = min(tid / kLanes, max(count - 1, 0));
+                const Token x = l.few[own];
+                int fn = 0;
+                u64 fm = 0;
 #pragma unroll 4
-                for (int i = 0; i < count; ++i) {
+                for (int i = tid % kLanes; i < count; i += kLanes) {
                     const Token y = l.few[i];
                     const bool front = y.number > x.number;
                     fn += front, fm += front ? y.weight : 0;
                 }
+#pragma unroll
+                for (int d = 1; d < kLanes; d <<= 1) fn += __shfl_xor(fn, d), fm += (u64)__shfl_xor((long long)fm, d);
+                fn += n, fm += mass;
                 const bool reached = task == kCount ? (double)(fn + 1) == limit : (double)fm < limit && (double)(fm + x.weight) >= limit;
-                if (reached) l.cut = x.number, l.found_mass = fm + x.weight;
+                if (reached && tid / kLanes < count && tid % kLanes == 0) l.cut = x.number, l.found_mass = fm + x.weight;
             }
             __syncthreads();
             cut = max(cut, l.cut);
@@ -670,7 +744,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
         const int border = min(min(bin_k, bin_p), bin_m);
         if (border < kBins && tid < chunks) {
             const int b = border - l.shift[tid] + whole;
-            const double m = b > 0 && l.shift[tid] < kBins ? upto[tid * kBins + b - 1].mass : 0.0;
+            const double m = b > 0 && l.shift[tid] < kBins ? mass_of(upto[tid * kBins + b - 1]) : 0.0;
             l.kept[tid] = m * l.scale[tid] + (double)l.part[tid] * 0x1p-40 * power(-0.125 * border);
         }
         __syncthreads();
@@ -705,19 +779,21 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     u32x4 x[kVectors];
 #pragma unroll
     for (int j = 0; j < kVectors; ++j) x[j] = load16(row, min(first + j * N, V), V);
-    const double from = (floor(pos_of(l.tops[chosen], top, s.scale)) + 1.0) * 0.125;
+    const double from = (floor(pos_of(l.tops[chosen], top, s.scale)) + 1.0) * -4.0;
     u64 before = 0, aim = 0;
     bool mine = false;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
         u64 sum = 0;
         int token = -1;
-#pragma unroll 1
+#pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            u32x4 w = x[0];
-            if constexpr (kVectors == 2) w = i >= N ? x[1] : w;
-            const float y = pick<T>(w, i % N);
-            if (y == y && number_of<T>(key_of(y), first + i) >= cut && first + i < V) sum += (u64)(power(pos_of(y, top, s.scale) * 0.125 - from) * 0x1p43 + 0.5);
+            const float y = bits_of<T>(x[i / N], i % N);
+            // (2^52 more than the weight, which is then in the low bits; NaN and -infinity weigh nothing)
+            const double w = power32(__builtin_fma(pos_of(y, top, s.scale), 4.0, from), l.powers);
+            bool kept = top != kInf || y == top;
+            if (F) kept = y == y && number_of<T>(key_of(y), first + i) >= cut;
+            sum += kept ? __builtin_bit_cast(u64, __builtin_fma(w, 0x1p43, 0x1p52)) - 0x4330000000000000ull : 0;
             if (token < 0 && before + sum > aim) token = first + i;
         }
         if (pass) {
@@ -752,6 +828,8 @@ constexpr int64_t kSampleSpace = (int64_t)64 << 20;
 static int64_t chunks_of(int64_t V) { return (V + kChunk - 1) / kChunk; }
 static int64_t row_bytes(int64_t chunks) { return chunks * kChunkBytes + sizeof(Row); }
 static int64_t rows_of(int64_t rows, int64_t chunks) { return std::min(rows, std::max<int64_t>(kSampleSpace / row_bytes(chunks), 1)); }
+// (a launch whose rows have no filters needs the Chunks alone: as many rows as the same space holds)
+static int64_t plain_rows_of(int64_t rows, int64_t chunks) { return std::min(rows, rows_of(rows, chunks) * row_bytes(chunks) / (chunks * (int64_t)sizeof(Chunk))); }
 
 int64_t sample_workspace(int64_t rows, int64_t V)
 {
@@ -762,7 +840,8 @@ int64_t sample_workspace(int64_t rows, int64_t V)
 template <class T>
 static int sample_typed(const Sample &a, hipStream_t s)
 {
-    const int64_t chunks = chunks_of(a.V), most = rows_of(a.rows, chunks);
+    const bool filters = a.top_k || a.top_p || a.min_p;
+    const int64_t chunks = chunks_of(a.V), most = filters ? rows_of(a.rows, chunks) : plain_rows_of(a.rows, chunks);
     Chunk *const first = static_cast<Chunk *>(a.ws);
     Upto *const upto = reinterpret_cast<Upto *>(first + most * chunks);
     const Tables t{first, upto, reinterpret_cast<Row *>(upto + most * chunks * kBins)};
@@ -772,11 +851,11 @@ static int sample_typed(const Sample &a, hipStream_t s)
             return enqueue(kernel, dim3((unsigned)groups), dim3(threads), 0, s, a, t, r, (int)chunks, more...);
         };
         if (int rc = go(sample_chunks<T>, n * chunks, kChunkThreads)) return rc;
-        if (a.top_k || a.top_p || a.min_p) {
+        if (filters) {
             const int64_t parts = std::min(chunks, std::max<int64_t>(512 / n, 1));
             if (int rc = go(sample_border<T>, n * parts, kRowThreads, (int)parts)) return rc;
         }
-        if (int rc = go(sample_rows<T>, n, kRowThreads)) return rc;
+        if (int rc = filters ? go(sample_rows<T, true>, n, kRowThreads) : go(sample_rows<T, false>, n, kRowThreads)) return rc;
     }
     return MQ_OK;
 }

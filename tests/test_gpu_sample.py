@@ -97,7 +97,7 @@ def test_draws_at_the_ends():
 def test_settings_at_the_ends():
     r = np.random.default_rng(4)
     inf, nan = np.inf, np.nan
-    for V in (9, 5000):
+    for V in (9, 5000, 30000):
         for name, values in (("temperature", [0.0, -0.0, -1.0, nan, inf, -inf, 1e-30, 1e-45, 1e30, 3e38, 1e-3, 100.0]),
                              ("top_k", [0, -1, -(2 ** 31), 1, 2, V - 1, V, V + 1, 2 ** 31 - 1, 3, 4, 5]),
                              ("top_p", [0.0, -1.0, nan, 1.0, 2.0, inf, 1e-30, 1 - 2 ** -24, 2 ** -20, 0.5, -inf, 1e-45]),
