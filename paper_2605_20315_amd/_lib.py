@@ -147,7 +147,7 @@ def load_binding():
         return NoBinding()
     names = ("nvfp4_global_scale", "nvfp4_quantize", "nvfp4_quantize_silu_mul", "nvfp4_quantize_rmsnorm",
              "nvfp4_relayout", "nvfp4_gemm_ws", "bf16_gemm_ws", "nvfp4_matvec", "mq_nvfp4_matvec_workspace_bytes", "kv8_append",
-             "kv8_attention")
+             "kv8_attention", "kv8_tree_attention", "mq_draft_tree", "mq_draft_accept", "kv8_compact", "mq_sample", "mq_sample_workspace_bytes")
     _binding.bind(check, {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names})
     return _binding
 

@@ -21,6 +21,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <initializer_list>
 
 #include "../../include/mixquant.h"
 
@@ -37,6 +38,12 @@ decltype(&::nvfp4_matvec) p_matvec;
 decltype(&::mq_nvfp4_matvec_workspace_bytes) p_matvec_workspace;
 decltype(&::kv8_append) p_append;
 decltype(&::kv8_attention) p_attention;
+decltype(&::kv8_tree_attention) p_tree_attention;
+decltype(&::mq_draft_tree) p_draft_tree;
+decltype(&::mq_draft_accept) p_draft_accept;
+decltype(&::kv8_compact) p_compact;
+decltype(&::mq_sample) p_sample;
+decltype(&::mq_sample_workspace_bytes) p_sample_workspace;
 PyObject *g_check;
 
 // "Not of the plain form" is a return value (false, a null pointer, None) and no C++ exception: one of those takes 3.7 us, as
@@ -542,6 +549,186 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// Whether the tensors (of the arguments that are no None) live on the current stream's device
+bool here(std::initializer_list<const at::Tensor *> tensors)
+{
+    const auto index = c10::hip::getCurrentHIPStream().device_index();
+    for (const at::Tensor *t : tensors)
+        if (t && t->get_device() != index) return false;
+    return true;
+}
+
+// a contiguous vector of n (-1: any) int32 or float values
+const at::Tensor *vector_of(PyObject *o, int64_t n, at::ScalarType type = at::kInt)
+{
+    const at::Tensor *t = typed(o, type);
+    return t && t->dim() == 1 && (n < 0 || t->size(0) == n) && t->is_contiguous() ? t : nullptr;
+}
+
+// one that may be None; false: neither
+bool maybe_vector(PyObject *o, int64_t n, at::ScalarType type, const at::Tensor *&t)
+{
+    return o == Py_None ? (t = nullptr, true) : (t = vector_of(o, n, type)) != nullptr;
+}
+
+bool out_vector(Out &out, PyObject *o, int64_t n, const at::Tensor &like)
+{
+    if (!out.read(o)) return false;
+    if (out.obj) return vector_of(o, n) != nullptr;
+    out.made = at::empty({n}, at::TensorOptions().dtype(at::kInt).device(like.device()));
+    out.t = &out.made;
+    return true;
+}
+
+PyObject *give_all(std::initializer_list<const Out *> outs)
+{
+    PyObject *const tuple = PyTuple_New((Py_ssize_t)outs.size());
+    Py_ssize_t i = 0;
+    if (tuple)
+        for (const Out *o : outs) {
+            PyObject *const x = give(*o);
+            if (!x) {
+                Py_DECREF(tuple);
+                return nullptr;
+            }
+            PyTuple_SET_ITEM(tuple, i++, x);
+        }
+    return tuple;
+}
+
+int32_t *ints_of(const at::Tensor *t) { return t ? static_cast<int32_t *>(t->data_ptr()) : nullptr; }
+const float *floats_of(const at::Tensor *t) { return t ? static_cast<const float *>(t->data_ptr()) : nullptr; }
+
+PyObject *draft_tree(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 7, [&]() -> PyObject * {
+        // parents, cu_q, kv_lens, words, window, tree, positions
+        const at::Tensor *parents = vector_of(a[0], -1), *lens = vector_of(a[2], -1), *cu = lens ? vector_of(a[1], lens->size(0) + 1) : nullptr;
+        int words, window;
+        Out tree, positions;
+        if (!parents || !cu || !integer(a[3], words) || words < 0 || !integer(a[4], window) || !tree.read(a[5])) return general();
+        const int64_t T = parents->size(0), B = lens->size(0);
+        if (tree.obj && (tree.t->scalar_type() != at::kInt || tree.t->dim() != 2 || tree.t->size(0) != T || tree.t->size(1) != words || !tree.t->is_contiguous()))
+            return general();
+        if (!here({parents, cu, lens, tree.t}) || !out_vector(positions, a[6], T, *parents) || !here({positions.t})) return general();
+        allocate(tree, T, words, at::kInt, *parents);
+        void *const st = current_stream();
+        const int32_t *pp = ints_of(parents), *cp = ints_of(cu), *lp = ints_of(lens);
+        uint32_t *tp = reinterpret_cast<uint32_t *>(ints_of(tree.t));
+        int32_t *op = ints_of(positions.t);
+        if (!enqueue("mq_draft_tree", [&] { return p_draft_tree(pp, cp, lp, B, T, words, window, tp, op, st); })) return nullptr;
+        return give_all({&tree, &positions});
+    });
+}
+
+PyObject *draft_accept(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 9, [&]() -> PyObject * {
+        // parents, tokens, sampled, cu_q, kv_lens, path, counts, next, lens
+        const at::Tensor *parents = vector_of(a[0], -1), *lens = vector_of(a[4], -1);
+        if (!parents || !lens) return general();
+        const int64_t T = parents->size(0), B = lens->size(0);
+        const at::Tensor *tokens = vector_of(a[1], T), *sampled = vector_of(a[2], T), *cu = vector_of(a[3], B + 1);
+        Out path, counts, next, out;
+        if (!tokens || !sampled || !cu || !here({parents, tokens, sampled, cu, lens})) return general();
+        if (!out_vector(path, a[5], T, *parents) || !out_vector(counts, a[6], B, *parents) || !out_vector(next, a[7], B, *parents) ||
+            !out_vector(out, a[8], B, *parents) || !here({path.t, counts.t, next.t, out.t}))
+            return general();
+        void *const st = current_stream();
+        const int32_t *pp = ints_of(parents), *tp = ints_of(tokens), *sp = ints_of(sampled), *cp = ints_of(cu), *lp = ints_of(lens);
+        int32_t *o0 = ints_of(path.t), *o1 = ints_of(counts.t), *o2 = ints_of(next.t), *o3 = ints_of(out.t);
+        if (!enqueue("mq_draft_accept", [&] { return p_draft_accept(pp, tp, sp, cp, lp, B, T, o0, o1, o2, o3, st); })) return nullptr;
+        return give_all({&path, &counts, &next, &out});
+    });
+}
+
+PyObject *compact(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 9, [&]() -> PyObject * {
+        // cache and sequences (7), path, counts; gives True, as the Python form gives None
+        Cache c;
+        const at::Tensor *path = vector_of(a[7], -1);
+        if (!path || !c.read(a)) return general();
+        const at::Tensor *counts = vector_of(a[8], c.B);
+        if (!counts || !here({c.kc, c.ks, c.vc, c.vs, c.pt, c.cu, c.lens, path, counts})) return general();
+        void *const st = current_stream();
+        const int64_t T = path->size(0);
+        const int32_t *pp = ints_of(path), *np = ints_of(counts);
+        if (!enqueue("kv8_compact", [&] {
+                return p_compact(Cache::bytes(c.kc), Cache::bytes(c.ks), Cache::bytes(c.vc), Cache::bytes(c.vs), c.pages,
+                                 (int)std::min<int64_t>(c.P, INT32_MAX), (int)c.Hkv, (int)std::min<int64_t>(c.D, INT32_MAX), Cache::ints(c.pt), c.pt_ld,
+                                 c.W, Cache::ints(c.cu), Cache::ints(c.lens), c.B, T, pp, np, st);
+            }))
+            return nullptr;
+        Py_RETURN_TRUE;
+    });
+}
+
+PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 14, [&]() -> PyObject * {
+        // q, cache and sequences (7), tree, sm_scale, window, positions, y, workspace
+        Heads q, y;
+        Cache c;
+        Out out;
+        float scale;
+        int window;
+        const at::Tensor *tree = typed(a[8], at::kInt), *positions, *work = nullptr;
+        if (!tree || !q.read(a[0]) || !c.read(a + 1) || !real(a[9], scale) || !integer(a[10], window) || !out.read(a[12])) return general();
+        if (q.D != c.D || q.H > INT32_MAX || !maybe_vector(a[11], q.T, at::kInt, positions)) return general();
+        if (tree->dim() != 2 || tree->size(0) != q.T || tree->size(1) > INT32_MAX || !tree->is_contiguous()) return general();
+        if (out.obj && (!y.read(a[12]) || out.t->sizes() != q.t->sizes())) return general();
+        if (a[13] != Py_None && (!(work = tensor(a[13])) || !work->is_contiguous())) return general();
+        if (!here({q.t, c.kc, c.ks, c.vc, c.vs, c.pt, c.cu, c.lens, tree, positions, out.t, work})) return general();
+        if (!out.obj) out.made = make_heads(q), out.t = &out.made, y.ld = q.H * q.D;
+        void *const st = current_stream(), *const op = out.t->data_ptr(), *const ws = work ? work->data_ptr() : nullptr;
+        const int64_t ws_bytes = work ? work->numel() * work->element_size() : 0;
+        const void *qp = q.t->data_ptr();
+        const uint32_t *tp = reinterpret_cast<const uint32_t *>(ints_of(tree));
+        const int32_t *pp = ints_of(positions);
+        if (!enqueue("kv8_tree_attention", [&] {
+                return p_tree_attention(qp, q.ld, Cache::bytes(c.kc), Cache::bytes(c.ks), Cache::bytes(c.vc), Cache::bytes(c.vs), c.pages,
+                                        (int)std::min<int64_t>(c.P, INT32_MAX), (int)q.H, (int)c.Hkv, (int)std::min<int64_t>(c.D, INT32_MAX),
+                                        Cache::ints(c.pt), c.pt_ld, c.W, Cache::ints(c.cu), Cache::ints(c.lens), c.B, q.T, tp, (int)tree->size(1), pp,
+                                        scale, window, op, y.ld, ws, ws_bytes, st);
+            }))
+            return nullptr;
+        return give(out);
+    });
+}
+
+PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 8, [&]() -> PyObject * {
+        // logits, uniform, temperature, top_k, top_p, min_p, tokens, workspace
+        const at::Tensor *x = tensor(a[0]), *t, *k, *p, *m, *work = nullptr;
+        Rows r;
+        Out tokens;
+        if (!x || (x->scalar_type() != at::kBFloat16 && x->scalar_type() != at::kFloat) || !r.read(*x)) return general();
+        const at::Tensor *u = vector_of(a[1], r.rows, at::kFloat);
+        if (!u || !maybe_vector(a[2], r.rows, at::kFloat, t) || !maybe_vector(a[3], r.rows, at::kInt, k) || !maybe_vector(a[4], r.rows, at::kFloat, p) ||
+            !maybe_vector(a[5], r.rows, at::kFloat, m))
+            return general();
+        if (a[7] != Py_None && (!(work = tensor(a[7])) || !work->is_contiguous())) return general();
+        if (!here({x, u, t, k, p, m, work}) || !out_vector(tokens, a[6], r.rows, *x) || !here({tokens.t})) return general();
+        at::Tensor made;
+        if (!work)
+            if (const int64_t bytes = p_sample_workspace(r.rows, r.K)) {
+                made = at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(x->device()));
+                work = &made;
+            }
+        void *const st = current_stream(), *const ws = work ? work->data_ptr() : nullptr;
+        const int64_t ws_bytes = work ? work->numel() * work->element_size() : 0;
+        const void *xp = x->data_ptr();
+        const int type = x->scalar_type() == at::kBFloat16 ? MQ_OUT_BF16 : MQ_OUT_FP32;
+        const float *up = floats_of(u), *tp = floats_of(t), *pp = floats_of(p), *mp = floats_of(m);
+        const int32_t *kp = ints_of(k);
+        int32_t *op = ints_of(tokens.t);
+        if (!enqueue("mq_sample", [&] { return p_sample(xp, r.rows, r.K, r.ld, type, up, tp, kp, pp, mp, op, ws, ws_bytes, st); })) return nullptr;
+        return give(tokens);
+    });
+}
+
 // bind(check, addresses by name): where the library's functions are
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -565,6 +752,12 @@ PyObject *bind(PyObject *, PyObject *args)
     get("mq_nvfp4_matvec_workspace_bytes", p_matvec_workspace);
     get("kv8_append", p_append);
     get("kv8_attention", p_attention);
+    get("kv8_tree_attention", p_tree_attention);
+    get("mq_draft_tree", p_draft_tree);
+    get("mq_draft_accept", p_draft_accept);
+    get("kv8_compact", p_compact);
+    get("mq_sample", p_sample);
+    get("mq_sample_workspace_bytes", p_sample_workspace);
     if (!ok) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "bind: a function of the library is missing");
         return nullptr;
@@ -577,6 +770,8 @@ PyObject *bind(PyObject *, PyObject *args)
 PyMethodDef methods[] = {MQ_FAST(global_scale), MQ_FAST(quantize), MQ_FAST(quantize_silu_mul), MQ_FAST(quantize_rmsnorm),
                          MQ_FAST(relayout),     MQ_FAST(gemm_ws),  MQ_FAST(linear),            MQ_FAST(bf16_gemm_ws),
                          MQ_FAST(matvec),       MQ_FAST(append),  MQ_FAST(attention),
+                         MQ_FAST(draft_tree),   MQ_FAST(draft_accept), MQ_FAST(compact),       MQ_FAST(tree_attention),
+                         MQ_FAST(sample),
                          {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Plain-form calls of the mixquant library.", -1, methods};
 

@@ -506,6 +506,9 @@ def mq_draft_tree(parents: torch.Tensor, cu_q: torch.Tensor, kv_lens: torch.Tens
     or is it, and int32 [T], for kv8_tree_attention and kv8_append.  parents int32 [T]: the number of each token's parent among its
     sequence's new tokens, -1 for none.  words: 32 tokens each, for the longest of the sequences.  window > 0: only the window - 1
     tokens next above."""
+    done = _fast.draft_tree(parents, cu_q, kv_lens, words, window, tree, positions)
+    if done is not None:
+        return done
     T, B = _new_tokens(parents, cu_q, kv_lens)
     words = int(words)
     if tree is None:
@@ -530,6 +533,10 @@ def kv8_tree_attention(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.T
     sequences: each sees the places before its sequence's new tokens, and of those its mask's; BF16 [T, Hq, D].  tree: int32 [T, words], what
     mq_draft_tree gives.  window > 0: of the places before them only those behind position - window; positions int32 [T], else
     the tokens' places.  workspace: as in kv8_attention."""
+    done = _fast.tree_attention(q, k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, tree, sm_scale, window, positions, y,
+                                workspace)
+    if done is not None:
+        return done
     _here(q, k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, tree)
     T, Hq, D, ldq = _heads_ld(q)
     pages, P, Hkv, pt_ld, W, B = _cache(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, T, D)
@@ -570,6 +577,9 @@ def mq_sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: torch.Te
     weight; then the lowest index up to which the kept ones have more than `uniform` of their mass.  The settings are float32 (top_k
     int32) [rows], or None for 1, none, none and none; a temperature of 0 gives the largest logit's index.  workspace: any contiguous GPU
     tensor of mq_sample_workspace_bytes; without one it is taken from torch's allocator for the call."""
+    done = _fast.sample(logits, uniform, temperature, top_k, top_p, min_p, tokens, workspace)
+    if done is not None:
+        return done
     _here(logits, uniform)
     if logits.dtype not in (torch.bfloat16, torch.float32):
         raise MixQuantError("expected BF16 or FP32 logits")
@@ -605,6 +615,9 @@ def mq_draft_accept(parents: torch.Tensor, tokens: torch.Tensor, sampled: torch.
     """The drafted tokens that the sampled ones confirm: (path, counts, next, lens).  From token 0 of a sequence's new ones on, the lowest
     child whose token is the one sampled at its parent.  path int32 [T]: at cu_q[b] the numbers of b's path, then -1; counts int32 [B]: its
     length; next int32 [B]: the token sampled at its end; lens int32 [B]: the sequence's length with the path alone."""
+    done = _fast.draft_accept(parents, tokens, sampled, cu_q, kv_lens, path, counts, next, lens)
+    if done is not None:
+        return done
     T, B = _new_tokens(parents, cu_q, kv_lens)
     _here(tokens, sampled)
     _vector("tokens", tokens, T)
@@ -625,6 +638,8 @@ def kv8_compact(k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Te
                 cu_q: torch.Tensor, kv_lens: torch.Tensor, path: torch.Tensor, counts: torch.Tensor) -> None:
     """Brings the tokens of the paths together in the paged FP8 cache, in place: path and counts as mq_draft_accept gives them, cu_q and
     kv_lens those of the step that appended the drafted tokens."""
+    if _fast.compact(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, path, counts) is not None:
+        return
     _here(k_codes, k_scales, v_codes, v_scales, page_table, cu_q, kv_lens, path, counts)
     if k_codes.dim() != 4:
         raise MixQuantError("expected a cache of codes [pages, heads, tokens, D]")
