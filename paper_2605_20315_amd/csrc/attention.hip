@@ -1,14 +1,15 @@
 // Attention over the paged FP8 cache: y = softmax(scale * q K^T) V per query head, causal, with an optional window.
 //
 // Queries of one sequence and one key head are rows: row r is head r % G of the group, token r / G, so the G query heads that
-// share a key head read its cache once.  One pass over the keys with a running maximum and sum.  Two kernels:
+// share a key head read its cache once.  One pass over the keys with a running maximum and sum.  Three kernels:
 //   attend_few    tiles of 16 or 32 rows, no LDS in its loop: bound by reading the cache
 //   attend_many   tiles of 128 rows, the cache's tiles expanded once per workgroup into LDS: bound by the matrix and vector pipes
-// Both compute the transposes S^T = K Q^T and O^T = V^T P^T: a lane then holds, of one row, the very scores that it has to
+//   attend_tree   tiles of 16 or 32 rows of drafted tokens, which see of each other what a mask of bits says
+// All compute the transposes S^T = K Q^T and O^T = V^T P^T: a lane then holds, of one row, the very scores that it has to
 // supply as its slots of P^T in the second product, so the probabilities never move between lanes.  MFMA slots are matched
 // to tokens and head elements by whatever order the loads have; both operands of a product only have to agree.
 //
-// Work is cut in the same way in both: (sequence, tile of rows, chunk of tokens, key head) is an item, one workgroup each,
+// Work is cut in the same way in all: (sequence, tile of rows, chunk of tokens, key head) is an item, one workgroup each,
 // chunk lengths chosen on the device from the sequences' own lengths so that the items are about `target` (a batch of uneven
 // lengths is cut evenly, and the host needs to know no lengths).  A sequence with several chunks leaves its partial sums in
 // the workspace, and attend_join adds them in ascending order.
@@ -17,7 +18,7 @@
 // probabilities are rounded to BF16 for the product with the values, 2^-8 of each at most, since a value with its page's
 // exponent (-112 .. 119) fits no 16-bit operand but BF16, and both operands of a product are of one type: a prompt of 8192 is
 // 0.0020 from 64 bits so, where a result whose only rounding is its own is 0.0016 (single tokens: 0.0017 and 0.0017).  The sum they are divided
-// by is of the unrounded ones.
+// by is of the unrounded ones, but in attend_tree of the rounded ones.
 // Ranges.  The output's sums are not divided before the end: with values of 2^119 over the number of places seen and more they may
 // overflow.  Scores beyond 2^30 leave less of the exponential of a row's own maximum than 32 bits hold.
 #include "kv8.h"
@@ -236,9 +237,9 @@ static __device__ __forceinline__ int position_of(const Kv8TreeAttend &a, const 
 static __device__ __forceinline__ uint32_t bits_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
 
 // Which of the places t .. t + 31 a token sees, as bits; `first` is the first that its window leaves.
-static __device__ __forceinline__ uint32_t seen_word(const Kv8TreeAttend &a, const Span &sp, const uint32_t *mask, int first, int t)
+static __device__ __forceinline__ uint32_t seen_word(const Kv8TreeAttend &a, int start, const uint32_t *mask, int first, int t)
 {
-    const int64_t at = (int64_t)t - sp.start;  // the number of place t among the new tokens
+    const int64_t at = (int64_t)t - start;  // the number of place t among the new tokens
     uint32_t seen = 0;
     if (at < 0) seen = bits_below((int)min(-at, (int64_t)32)) & ~bits_below((int)max(min((int64_t)first - t, (int64_t)32), (int64_t)0));
     if (at > -32 && at < 32 * a.words) {
@@ -312,8 +313,8 @@ constexpr int kFewWaves = 4, kFewThreads = 64 * kFewWaves;
 // waiting for memory (vector instructions 15 % of the time); two sequences of 105000, 435 MB, 83 us.  A branch around the loads
 // ahead would make every wait one for all of them (125 and 92 us with the join, so 120.5 and 89).
 // RT tiles of 16 rows: what a wave has expanded serves all of them (109 sequences of 23000, 52 rows each: 365 us with one, 233 with two).
-template <int D, int RT, bool TREE>
-__global__ __launch_bounds__(kFewThreads) void attend_few(Attend<TREE> a, Cut c)
+template <int D, int RT>
+__global__ __launch_bounds__(kFewThreads) void attend_few(Kv8Attend a, Cut c)
 {
     constexpr int KW = D / 16;  // dwords of a key row's quarter, and MFMA steps over the head elements per 2 of them
     constexpr int VW = D / 64;  // dwords of a value row's sixteenth
@@ -326,19 +327,13 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Attend<TREE> a, Cut c)
     if (!it.found) return;
     const int G = a.Hq / a.Hkv, rows = it.sp.n * G, row0 = it.tile * kRows;
     int pos[RT], first[RT];  // the places that the lane's row of each tile sees: from first to pos
-    [[maybe_unused]] const uint32_t *mask[RT];
     u32x4 q[RT][D / 32];
     f32x4 acc[RT][D / 16];
     float mb[RT], l[RT];  // the running maximum times the scale, and the lane's share of the sum
 #pragma unroll
     for (int f = 0; f < RT; ++f) {
         const int row = min(row0 + 16 * f + col, rows - 1), token = row / G, head = it.head * G + row - token * G;
-        if constexpr (TREE) {
-            pos[f] = position_of(a, it.sp, token);
-            mask[f] = a.tree + (int64_t)(it.sp.q0 + token) * a.words;
-        } else {
-            pos[f] = it.sp.start + token;
-        }
+        pos[f] = it.sp.start + token;
         first[f] = first_seen(a, pos[f]);
         const uint16_t *const p = a.q + (int64_t)(it.sp.q0 + token) * a.ldq + (int64_t)head * D + g * (D / 4);
 #pragma unroll
@@ -348,20 +343,9 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Attend<TREE> a, Cut c)
         mb[f] = kNone, l[f] = 0.0f;
     }
     // what every row of the item, and what any of them sees
-    int lo, hi, all_lo, all_hi;
-    if constexpr (TREE) {
-        hi = min(it.hi, it.sp.start + it.sp.n), lo = max(it.lo, first_seen(a, it.sp.start));
-        all_lo = first[0], all_hi = min(it.hi, it.sp.start);
-#pragma unroll
-        for (int f = 1; f < RT; ++f) all_lo = max(all_lo, first[f]);
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) all_lo = max(all_lo, __shfl_xor(all_lo, d));
-        all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-    } else {
-        const int pos_lo = it.sp.start + row0 / G, pos_hi = it.sp.start + (min(row0 + kRows, rows) - 1) / G;
-        hi = min(it.hi, pos_hi + 1), lo = max(it.lo, first_seen(a, pos_lo));
-        all_lo = first_seen(a, pos_hi), all_hi = min(it.hi, pos_lo + 1);
-    }
+    const int pos_lo = it.sp.start + row0 / G, pos_hi = it.sp.start + (min(row0 + kRows, rows) - 1) / G;
+    const int hi = min(it.hi, pos_hi + 1), lo = max(it.lo, first_seen(a, pos_lo));
+    const int all_lo = first_seen(a, pos_hi), all_hi = min(it.hi, pos_lo + 1);
     bool marked = false;  // whether the wave's part of `sums` holds NaN for what rows have seen
 
     const int P = 1 << a.s.page_shift;
@@ -434,10 +418,6 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Attend<TREE> a, Cut c)
             bool odd = false;
 #pragma unroll
             for (int f = 0; f < RT; ++f) seen[f] = 0;
-            [[maybe_unused]] uint32_t word[RT];  // of the lane's row, from its places on
-            if constexpr (TREE)
-#pragma unroll
-                for (int f = 0; f < RT; ++f) word[f] = seen_word(a, it.sp, mask[f], first[f], t) >> (4 * g);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -446,12 +426,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Attend<TREE> a, Cut c)
                     const bool there = at >= lo && at < hi && (h ? id1 : id0) >= 0;
 #pragma unroll
                     for (int f = 0; f < RT; ++f) {
-                        bool sees;
-                        if constexpr (TREE)
-                            sees = word[f] >> (16 * h + j) & 1;
-                        else
-                            sees = at >= first[f] && at <= pos[f];
-                        if (there && sees)
+                        if (there && at >= first[f] && at <= pos[f])
                             seen[f] |= 1u << (4 * h + j);
                         else
                             s[f][h][j] = kNone;
@@ -603,11 +578,7 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Attend<TREE> a, Cut c)
             continue;
         }
         const int token = row / G;
-        float inv;
-        if constexpr (TREE)
-            inv = tree_inverse_of(a, it.b, it.sp, token, total);
-        else
-            inv = inverse_of(a, it.b, it.sp, it.sp.start + token, total);
+        const float inv = inverse_of(a, it.b, it.sp, it.sp.start + token, total);
         uint32_t *const y = reinterpret_cast<uint32_t *>(a.y + (int64_t)(it.sp.q0 + token) * a.ldy + (int64_t)(it.head * G + row - token * G) * D + e0);
 #pragma unroll
         for (int e = 0; e < D / 16; e += 2) y[e / 2] = pack2(o[e] * inv, o[e + 1] * inv);
@@ -631,8 +602,8 @@ __global__ __launch_bounds__(kFewThreads) void attend_few(Attend<TREE> a, Cut c)
 // 8192^3 reaches here.  Compared while it took 635 (its page numbers were looked at where they were read): without the keys
 // ahead 747; one wave a SIMD with 64 rows, which reads LDS half as often, 945 (it has no second wave to fill its waits);
 // eight waves in one workgroup 635, and less even shares of short work.
-template <int D, bool TREE>
-__global__ __launch_bounds__(64 * kManyWaves) void attend_many(Attend<TREE> a, Cut c)
+template <int D>
+__global__ __launch_bounds__(64 * kManyWaves) void attend_many(Kv8Attend a, Cut c)
 {
     constexpr int NW = kManyWaves, NT = 64 * NW, TN = 4 * D / NT;  // tasks of a thread: 32 bytes of codes each
     static_assert(TN * NT == 4 * D && (TN > 1 || NT == 2 * 2 * D), "every thread has the same tasks, or half of the waves those of keys");
@@ -649,29 +620,15 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Attend<TREE> a, C
     const int G = a.Hq / a.Hkv, rows = it.sp.n * G, tile0 = it.tile * kRows, wave0 = tile0 + 32 * wave;
     // the lane's row (rows beyond the last are computed again and not stored) and the places that it sees
     const int row = min(wave0 + col, rows - 1), token = row / G, head = it.head * G + row - token * G;
-    int pos, first;
-    // places that any row of the workgroup sees, that every row of the wave sees, and that every row of the workgroup sees
-    int group_lo, group_hi, all_lo, all_hi, rows_lo, rows_hi;
-    [[maybe_unused]] const uint32_t *mask = nullptr;
-    if constexpr (TREE) {
-        pos = position_of(a, it.sp, token), first = first_seen(a, pos);
-        mask = a.tree + (int64_t)(it.sp.q0 + token) * a.words;
-        group_hi = min(it.hi, it.sp.start + it.sp.n), group_lo = max(it.lo, first_seen(a, it.sp.start));
-        all_lo = first;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) all_lo = max(all_lo, __shfl_xor(all_lo, d));
-        all_lo = max(group_lo, __builtin_amdgcn_readfirstlane(all_lo)), all_hi = min(group_hi, it.sp.start);
-        // (the rows' positions are in no order: with a window none are taken for seen by all, which costs a look for NaN codes)
-        rows_lo = a.window > 0 ? group_hi : group_lo, rows_hi = all_hi;
-    } else {
-        pos = it.sp.start + token, first = first_seen(a, pos);
-        group_hi = min(it.hi, it.sp.start + (min(tile0 + kRows, rows) - 1) / G + 1);
-        group_lo = max(it.lo, first_seen(a, it.sp.start + tile0 / G));
-        const int pos_lo = it.sp.start + min(wave0, rows - 1) / G, pos_hi = it.sp.start + (min(wave0 + 32, rows) - 1) / G;
-        all_lo = max(group_lo, first_seen(a, pos_hi)), all_hi = min(group_hi, pos_lo + 1);
-        rows_lo = max(group_lo, first_seen(a, it.sp.start + (min(tile0 + kRows, rows) - 1) / G));
-        rows_hi = min(group_hi, it.sp.start + tile0 / G + 1);
-    }
+    const int pos = it.sp.start + token, first = first_seen(a, pos);
+    // places that any row of the workgroup sees, that any and that every row of the wave sees
+    const int group_hi = min(it.hi, it.sp.start + (min(tile0 + kRows, rows) - 1) / G + 1);
+    const int group_lo = max(it.lo, first_seen(a, it.sp.start + tile0 / G));
+    const int pos_lo = it.sp.start + min(wave0, rows - 1) / G, pos_hi = it.sp.start + (min(wave0 + 32, rows) - 1) / G;
+    const int all_lo = max(group_lo, first_seen(a, pos_hi)), all_hi = min(group_hi, pos_lo + 1);
+    // places that every row of the workgroup sees
+    const int rows_lo = max(group_lo, first_seen(a, it.sp.start + (min(tile0 + kRows, rows) - 1) / G));
+    const int rows_hi = min(group_hi, it.sp.start + tile0 / G + 1);
 
     bf16x8 q[D / 16];
     {
@@ -802,15 +759,6 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Attend<TREE> a, C
         top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale;
     };
     auto sees = [&](int at, int no_page) { return at >= max(first, group_lo) && at <= pos && at < group_hi && !no_page; };
-    // TREE: the places t .. t + 31 that the lane's row sees, without those that have no page (bad: of the first and second 16)
-    [[maybe_unused]] auto seen_of = [&](int t, int bad) {
-        uint32_t w = 0;
-        if constexpr (TREE) {
-            w = seen_word(a, it.sp, mask, first, t) & bits_below(group_hi - t) & ~bits_below(group_lo - t);
-            w &= (bad & 1 ? 0xffff0000u : ~0u) & (bad & 2 ? 0xffffu : ~0u);
-        }
-        return w;
-    };
     const unsigned char *key_at, *value_at;
     auto half_step = [&](int i, int half, int flag) {
         const unsigned char *const next = key_at + half * (D / 16) * kBlock16, *const from = value_at + 2 * half * (D / 32) * kBlock16;
@@ -818,11 +766,6 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Attend<TREE> a, C
         const int t = begin + i * kTile + 32 * half, bad = flag >> (2 * half) & 3;
         const bool edge = t < all_lo || t + 32 > all_hi || bad;
         if (edge) {
-            [[maybe_unused]] const uint32_t word = seen_of(t, bad) >> (4 * h);
-            if constexpr (TREE) {
-#pragma unroll
-                for (int j = 0; j < 16; ++j) s[half][j] = word >> (8 * (j / 4) + j % 4) & 1 ? s[half][j] : kNone;
-            } else
 #pragma unroll
             for (int j = 0; j < 16; ++j) s[half][j] = sees(t + 8 * (j / 4) + 4 * h + j % 4, bad >> (j / 8) & 1) ? s[half][j] : kNone;
             maxima(half);
@@ -881,9 +824,8 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Attend<TREE> a, C
                 }
         }
         __syncthreads();
-        [[maybe_unused]] const uint32_t words[2] = {seen_of(begin + i * kTile, flag & 3), seen_of(begin + i * kTile + 32, flag >> 2 & 3)};
         for (int j = 0; j < kTile; ++j)
-            if (TREE ? (words[j >> 5] >> (j & 31) & 1) != 0 : sees(begin + i * kTile + j, flag >> (j / 16) & 1))
+            if (sees(begin + i * kTile + j, flag >> (j / 16) & 1))
                 for (int d = 0; d < D / 32; ++d) marks[d][tid] |= nans[j][d];
         __syncthreads();
     };
@@ -924,11 +866,7 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Attend<TREE> a, C
     float *const part = slot_at(c, D, it.slot);
     if (split && h == 0) part[c.rows * D + local] = mb, part[c.rows * D + c.rows + local] = l;
     // (the item is read from LDS again: kept through the loop it spills 16 more scalar registers, 595 us for the long prompt's 591)
-    float inv = 1.0f;
-    if constexpr (TREE)
-        inv = split ? 1.0f : tree_inverse_of(a, plan.found.b, plan.found.sp, token, l);
-    else
-        inv = split ? 1.0f : inverse_of(a, plan.found.b, plan.found.sp, pos, l);
+    const float inv = split ? 1.0f : inverse_of(a, plan.found.b, plan.found.sp, pos, l);
     uint16_t *const y = a.y + (int64_t)(it.sp.q0 + token) * a.ldy + (int64_t)head * D;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -972,6 +910,360 @@ __global__ __launch_bounds__(64 * kManyWaves) void attend_many(Attend<TREE> a, C
                 }
             }
         }
+}
+
+// ------------------------------------------------------------------------------------------------ rows of drafted tokens
+
+// N KB from memory into LDS at `to`, 16 bytes a lane and KB from `lane_at` bytes behind `from` on (the instruction's offset counts for
+// both).  In inline assembly because the compiler holds every LDS read until all such loads have landed; the waits for them are
+// written where they are read.
+template <int N>
+static __device__ __forceinline__ void lds_load(uint32_t to, uint32_t lane_at, const uint8_t *from)
+{
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    static_assert(N == 1 || N == 2, "");
+    if constexpr (N == 1)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(lane_at), "s"(from) : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024"
+                     :
+                     : "s"(to), "v"(lane_at), "s"(from)
+                     : "memory", "m0");
+#pragma clang diagnostic pop
+}
+
+// As attend_few, for drafted tokens, which have tens of rows a key head where single ones have a few: a tile's arithmetic counts as
+// much as its memory, and a wave by itself issues a vector instruction only every other time that its SIMD could.  So registers are
+// spared for a third wave a SIMD: the queries stand in LDS, and keys and values come through it (from memory straight into LDS, the next
+// group's on their way while this one's are multiplied), into the same registers one after the other.  32 heads of 128 on 8:
+// 64 sequences of 8 to 26 tokens after 100 to 8000 take 203 us, 237 by the kernels for single tokens and prompts; 60 tokens after 2000
+// in one 22 and 26.9; two of 64 after 100000 to 131000 294 to 303 and 288; 32 of 30 to 60 after 500 to 6000, 16 heads of 256 on 4, 212 and 338.
+// Of the 203, reading the cache (530 MB) is 108 at a large copy's rate; the vector instructions that expand and turn round the codes and take
+// the exponentials bound the rest.
+template <int D, int RT>
+__global__ __launch_bounds__(kFewThreads, D <= 128 ? 3 : 2) void attend_tree(Kv8TreeAttend a, Cut c)
+{
+    constexpr int KW = D / 16;  // dwords of a key row's quarter
+    constexpr int VW = D / 64;  // dwords of a value row's sixteenth
+    constexpr int kRows = 16 * RT, kHalf = 32 * D, kPieces = D / 16, kLoads = D / 32;  // bytes, 16-byte pieces of a row, and loads of a group's keys or values
+    constexpr int kSums = 2 * kRows * (D + 4) * 4, kRing = kFewWaves * 2 * kHalf;
+    __shared__ PlanLds plan;
+    __shared__ float stat[kFewWaves][2][kRows];
+    __shared__ uint32_t marks[kFewWaves][kRows][D / 32];  // the rows' elements that have seen NaN, a bit each
+    constexpr int kTurn = D == 64 ? 7 : 15;
+    __shared__ u32x4 queries[kRows][D / 8];               // piece p of row r in place p ^ (r & kTurn)
+    __shared__ int firsts[kRows], tokens[kRows];          // the first place that a row sees, and its token's number in the call
+    __shared__ __attribute__((aligned(16))) unsigned char pool[kRing > kSums ? kRing : kSums];  // keys and values of each wave's group, then sums
+    float(*const sums)[kRows][D + 4] = reinterpret_cast<float(*)[kRows][D + 4]>(pool);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g = lane >> 4;
+    const Item it = item_of<kFewThreads>(a, c, blockIdx.x, plan, tid);
+    if (!it.found) return;
+    const int G = a.Hq / a.Hkv, rows = it.sp.n * G, row0 = it.tile * kRows;
+    // (rows beyond the last are computed again and not stored)
+    for (int i = tid; i < kRows * (D / 8); i += kFewThreads) {
+        const int r = i / (D / 8), p = i % (D / 8), row = min(row0 + r, rows - 1), token = row / G;
+        queries[r][p ^ (r & kTurn)] = *reinterpret_cast<const u32x4 *>(a.q + (int64_t)(it.sp.q0 + token) * a.ldq + (int64_t)(it.head * G + row - token * G) * D + 8 * p);
+    }
+    f32x4 acc[RT][D / 16];
+    // the running maximum times the scale, and the sum of the probabilities as the product takes them: that of ones in the values' place
+    // (kLow: none yet; any score is 2^8 above it)
+    constexpr float kLow = -0x1p120f;
+    float mb[RT];
+    f32x4 sum[RT];
+    const bf16x8 ones = four(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+    int all_lo = 0;  // what every row of the item sees
+#pragma unroll
+    for (int f = 0; f < RT; ++f) {
+        const int token = min(row0 + 16 * f + col, rows - 1) / G, first = first_seen(a, position_of(a, it.sp, token));
+        if (wave == 0 && g == 0) firsts[16 * f + col] = first, tokens[16 * f + col] = it.sp.q0 + token;
+        all_lo = max(all_lo, first);
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) acc[f][d] = f32x4{0, 0, 0, 0};
+        mb[f] = kLow, sum[f] = f32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) all_lo = max(all_lo, __shfl_xor(all_lo, d));
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    // (uniform, and in scalar registers only if the compiler is told so)
+    const int start = __builtin_amdgcn_readfirstlane(it.sp.start), head = __builtin_amdgcn_readfirstlane(it.head);
+    const int hi = __builtin_amdgcn_readfirstlane(min(it.hi, it.sp.start + it.sp.n)), lo = __builtin_amdgcn_readfirstlane(max(it.lo, first_seen(a, it.sp.start)));
+    const int all_hi = min(hi, start);
+    bool marked = false;
+
+    const int P = 1 << a.s.page_shift, unit_shift = a.s.page_shift + (D == 64 ? 6 : D == 128 ? 7 : 8);
+    const int32_t *const table = a.s.page_table + it.b * a.s.pt_ld;
+    const int begin = (lo & ~31) + 32 * wave;
+    __syncthreads();
+
+    // pages of the wave's next 32 groups: lane 2i + h holds half h of group i, as its (page, head), whose bytes memory has room for; -1: none
+    int units = 0;
+    float ks = 0.0f, vs = 0.0f;
+    auto look_up = [&](int t) {
+        const int at = t + (lane >> 1) * 32 * kFewWaves + (lane & 1) * 16, page = at >> a.s.page_shift;
+        int id = at < hi && page < a.s.width ? table[page] : -1;
+        if ((unsigned)id >= (uint64_t)a.s.pages) id = -1;
+        const int64_t u = (int64_t)max(id, 0) * a.Hkv + head;
+        units = id < 0 ? -1 : (int)u;
+        ks = exp2_of(min((int)a.k_scales[u], 254) - 127);
+        vs = exp2_of(min((int)a.v_scales[u], 254) - 127);
+    };
+    // A group is 32 tokens' keys and then their values, a row as it is in the page but for its pieces, which stand in an order that spreads
+    // the reads over the banks: piece c of token t in place c ^ t.
+    unsigned char *const ring = pool + wave * 2 * kHalf;
+    const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)ring;
+    const uint32_t lane_at = (lane / kPieces) * D + ((lane % kPieces) ^ (lane / kPieces % kPieces)) * 16;
+    // where group i's tokens t .. t + 31 are, in bytes of either array
+    auto where = [&](int t, int i, int64_t (&at)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int own = max(__builtin_amdgcn_readlane(units, 2 * i + h), 0), place = (t + 16 * h) & (P - 1);
+            at[h] = ((int64_t)own << unit_shift) + place * D;
+        }
+    };
+    auto fetch = [&](const int64_t (&at)[2], bool value) {
+        const uint8_t *const codes = value ? a.v_codes : a.k_codes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t to = ring_at + (value ? kHalf : 0) + 16 * h * D;
+            if constexpr (D <= 128) {
+                lds_load<D / 64>(to, lane_at, codes + at[h]);
+            } else {
+                // (a load of heads of 256 holds four tokens: the pieces' order goes on with the fifth)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) lds_load<1>(to + 1024 * u, lane_at ^ (64 * u), codes + at[h] + 1024 * u);
+            }
+        }
+    };
+    auto wait = [](int left) {  // until at most so many loads are on their way
+        if (left)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
+    auto scales_of = [&](float x, int i, float (&to)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) to[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 2 * i + h));
+    };
+
+    auto group = [&](int t, int i, bool more) {
+        const int unit0 = __builtin_amdgcn_readlane(units, 2 * i), unit1 = __builtin_amdgcn_readlane(units, 2 * i + 1);
+        float scale[2];
+        scales_of(ks, i, scale);
+        int64_t next[2];
+        where(t + 32 * kFewWaves, more ? i + 1 : i, next);
+        f32x4 s[RT][2];
+#pragma unroll
+        for (int f = 0; f < RT; ++f) s[f][0] = s[f][1] = f32x4{0, 0, 0, 0};
+        wait(1);  // (its values may still be on their way)
+        {
+            u32x4 k[2][KW / 4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int w = 0; w < KW / 4; ++w)
+                    k[h][w] = *reinterpret_cast<const u32x4 *>(ring + (16 * h + col) * D + ((g * (KW / 4) + w) ^ (col % kPieces)) * 16);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read: their place is filled again
+            if (more) fetch(next, false);
+#pragma unroll
+            for (int w = 0; w < D / 32; ++w)
+#pragma unroll
+                for (int f = 0; f < RT; ++f) {
+                    const bf16x8 q = __builtin_bit_cast(bf16x8, queries[16 * f + col][(g * (D / 32) + w) ^ (col & kTurn)]);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        s[f][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(expand8(k[h][w / 2][2 * (w % 2)], k[h][w / 2][2 * (w % 2) + 1], scale[h]), q, s[f][h], 0, 0, 0);
+                }
+        }
+        const bool edge = t < all_lo || t + 32 > all_hi || unit0 < 0 || unit1 < 0;
+        uint32_t seen[RT], there = 0;  // of the lane's eight tokens: those that its row sees, and those that are any row's
+        if (edge) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int at = t + 16 * h + 4 * g + j;
+                    there |= (uint32_t)(at >= lo && at < hi && (h ? unit1 : unit0) >= 0) << (4 * h + j);
+                }
+#pragma unroll
+            for (int f = 0; f < RT; ++f) {
+                const int r = 16 * f + col;
+                const uint32_t word = seen_word(a, start, a.tree + (int64_t)tokens[r] * a.words, firsts[r], t) >> (4 * g);
+                seen[f] = ((word & 15) | (word >> 12 & 0xf0)) & there;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[f][j / 4][j % 4] = seen[f] >> j & 1 ? s[f][j / 4][j % 4] : kNone;
+            }
+        }
+        // The exponents above the maximum in use.  That only follows where a lane finds one of its row's scores to have outgrown it by 2^8,
+        // as in attend_many (a chunk's early groups raise one of 32 rows' nearly always), and only then do lanes have to exchange theirs.
+        bool grown = false;
+#pragma unroll
+        for (int f = 0; f < RT; ++f) {
+            float top = kLow;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fmaf(s[f][j / 4][j % 4], a.scale, -mb[f]));
+            grown |= top > 8.0f;
+        }
+        if (__any(grown))
+#pragma unroll
+            for (int f = 0; f < RT; ++f) {
+                float top = kNone;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top = fmaxf(top, s[f][j / 4][j % 4]);
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32)) * a.scale;
+                const float next_mb = fmaxf(mb[f], top), by = __builtin_amdgcn_exp2f(mb[f] - next_mb);
+                mb[f] = next_mb;
+                sum[f] *= by;
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) acc[f][d] *= by;
+            }
+        bf16x8 pb[RT];
+#pragma unroll
+        for (int f = 0; f < RT; ++f) {
+            float p[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[f][j / 4][j % 4], a.scale, -mb[f]));
+            pb[f] = four(pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7]));
+            sum[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[f], sum[f], 0, 0, 0);
+        }
+        scales_of(vs, i, scale);
+        wait(more);
+        uint32_t v[VW][8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int token = 16 * (j / 4) + 4 * g + j % 4;
+            const unsigned char *const p = ring + kHalf + token * D + ((col * VW / 4) ^ (token % kPieces)) * 16 + col * VW % 4 * 4;
+            if constexpr (VW == 1) v[0][j] = *reinterpret_cast<const uint32_t *>(p);
+            if constexpr (VW == 2) {
+                const u32x2 y = *reinterpret_cast<const u32x2 *>(p);
+                v[0][j] = y[0], v[1][j] = y[1];
+            }
+            if constexpr (VW == 4) {
+                const u32x4 y = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) v[w][j] = y[w];
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) fetch(next, true);
+        if (edge) {
+            // places that no row sees may hold anything, NaN codes among it: a zero probability would not hide those
+            bool odd = false;
+#pragma unroll
+            for (int w = 0; w < VW; ++w)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[w][j] = there >> j & 1 ? v[w][j] : 0u;
+                    odd |= nan_bytes(v[w][j]) != 0;
+                }
+            if (__any(odd)) {
+                // NaN values that some rows see and others do not: out of the product, and a mark for the rows that see them
+                if (!marked)
+                    for (int n = lane; n < kRows * (D / 32); n += 64) (&marks[wave][0][0])[n] = 0;
+                marked = true;
+#pragma unroll 1
+                for (int r = 0; r < kRows; ++r) {
+                    const uint32_t own = RT == 1 || r < 16 ? seen[0] : seen[RT - 1], sees = (uint32_t)__shfl((int)own, (r & 15) + 16 * g);
+#pragma unroll
+                    for (int w = 0; w < VW; ++w)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (const uint32_t n = nan_bytes(v[w][j]); n && (sees >> j & 1))
+#pragma unroll 1
+                                for (int b = 0; b < 4; ++b)
+                                    if (n >> (8 * b) & 1) {
+                                        const int e = col * (D / 16) + 4 * w + b;
+                                        atomicOr(&marks[wave][r][e / 32], 1u << (e % 32));
+                                    }
+                }
+#pragma unroll
+                for (int w = 0; w < VW; ++w)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[w][j] &= ~(nan_bytes(v[w][j]) * 0xffu);
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+            bf16x8 turned[4];
+            turn8(v[w], scale, turned);
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int f = 0; f < RT; ++f) acc[f][4 * w + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(turned[d], pb[f], acc[f][4 * w + d], 0, 0, 0);
+        }
+    };
+
+    constexpr int kStride = 32 * kFewWaves;
+    for (int t0 = begin; t0 < hi; t0 += 32 * kStride) {
+        look_up(t0);
+        const int count = min(32, (hi - t0 + kStride - 1) / kStride);
+        int64_t at[2];
+        where(t0, 0, at);
+        fetch(at, false);
+        fetch(at, true);
+#pragma unroll 1
+        for (int i = 0; i < count; ++i) group(t0 + i * kStride, i, i + 1 < count);
+    }
+
+    // The four waves' results, two and two: lane (col, g) holds, of row col, the elements (4g + i) * D / 16 + d for i < 4, d < D / 16
+#pragma unroll
+    for (int f = 0; f < RT; ++f) {
+        mb[f] = mb[f] == kLow ? kNone : mb[f];
+        if (g == 0) stat[wave][0][16 * f + col] = mb[f], stat[wave][1][16 * f + col] = sum[f][0];
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int turn = 1; turn >= 0; --turn) {
+        if (wave >> 1 == turn)
+#pragma unroll
+            for (int f = 0; f < RT; ++f) {
+                const int r = 16 * f + col;
+                float top = kNone;
+#pragma unroll
+                for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, stat[w][0][r]);
+                const float by = weight_of(mb[f], sum[f][0], top);
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = (4 * g + i) * (D / 16) + d;
+                        float &to = sums[wave & 1][r][e];
+                        float x = acc[f][d][i] * by;
+                        if (marked && (marks[wave][r][e / 32] >> (e % 32) & 1)) x = __builtin_nanf("");
+                        to = turn ? x : x + to;
+                    }
+            }
+        __syncthreads();
+    }
+    // 16 threads a row, D / 16 elements each (the item from LDS again, which spares its registers in the loop)
+    const Item &own = plan.found;
+    const int own_row0 = own.tile * kRows, own_rows = own.sp.n * G;
+#pragma unroll
+    for (int f = 0; f < RT; ++f) {
+        const int r = 16 * f + (tid >> 4), e0 = (tid & 15) * (D / 16), row = own_row0 + r;
+        if (row >= own_rows) return;
+        float best = kNone, total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) best = fmaxf(best, stat[w][0][r]);
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) total += stat[w][1][r] * weight_of(stat[w][0][r], stat[w][1][r], best);
+        float o[D / 16];
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) o[e] = sums[0][r][e0 + e] + sums[1][r][e0 + e];
+        if (own.chunks > 1) {
+            float *const p = slot_at(c, D, own.slot);
+#pragma unroll
+            for (int e = 0; e < D / 16; e += 4) *reinterpret_cast<f32x4 *>(p + r * D + e0 + e) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
+            if ((tid & 15) == 0) p[kRows * D + r] = best, p[kRows * D + kRows + r] = total;
+            continue;
+        }
+        const int token = row / G;
+        const float inv = tree_inverse_of(a, own.b, own.sp, token, total);
+        uint32_t *const y = reinterpret_cast<uint32_t *>(a.y + (int64_t)(own.sp.q0 + token) * a.ldy + (int64_t)(own.head * G + row - token * G) * D + e0);
+#pragma unroll
+        for (int e = 0; e < D / 16; e += 2) y[e / 2] = pack2(o[e] * inv, o[e + 1] * inv);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ partial sums
@@ -1061,6 +1353,10 @@ constexpr int64_t kWorkspace = (int64_t)64 << 20;
 constexpr int kFewTarget = 768;
 // workgroups of attend_many that a compute unit holds, by registers and LDS: three, two and one
 static int many_target(int D) { return 256 * (D == 64 ? 3 : D == 128 ? 2 : 1); }
+// workgroups of attend_tree with two tiles of rows that the GPU holds, by registers and LDS
+static int tree_places(int D) { return 256 * (D == 64 ? 4 : 3); }
+// (query row, place) pairs above which attend_tree takes two tiles of rows
+constexpr int64_t kTreeRowPlaces = (int64_t)48 << 20;
 static int slots_of(int rows, int D) { return (int)((kWorkspace - kPartsBytes) / ((int64_t)rows * (D + 2) * 4)); }
 static int target_of(int most, int rows, int D) { return std::min(slots_of(rows, D) / 2, most); }
 
@@ -1132,8 +1428,47 @@ static int plan_attention(const Kv8Attend &a, Launch *out)
     return n;
 }
 
+// Drafted tokens.  All of a call's sequences go to one kernel: they have about as many tokens each, and a second kernel that finds
+// nothing to do costs 14 us.  Two tiles of rows from one expansion where there is enough work that arithmetic bounds it (32 heads of
+// 128 on 8: two sequences of 64 tokens after 100000 to 131000 294 us, 406 with one tile; 64 of 16 after 4000 134 and 165), not where the latency of an
+// item does (4 of 60 after 500 to 1000: 29.6, 21.3 with one; one of 60 after 2000 28 and 23.4; 8 of 30 to 60 after 1000 to 4000 50 and 47).
+// Few items of two tiles are cut into as many as the GPU holds at a time, others into 512: what comes after a first round then is short.
+static Launch plan_tree(const Kv8TreeAttend &a)
+{
+    const int D = a.D;
+    const int64_t G = a.Hq / a.Hkv, T = a.s.T, B = a.s.B, places = (int64_t)a.s.width << a.s.page_shift;
+    const bool ws = a.ws && a.ws_bytes >= kWorkspace && B <= kPartsMost;
+    const bool two = D <= 128 && T * G > B * kFewRows && T * G * a.Hkv * places > kTreeRowPlaces;
+    const int rows = two ? 2 * kFewRows : kFewRows;
+    Launch p{false, Cut{rows, 0, 2, 0, INT32_MAX, true, false, a.ws, slots_of(rows, D), 0}, 0};
+    const int64_t whole = row_tiles_most(p.cut, T, B, G) * a.Hkv, tiles = places / kTile + 1;
+    p.cut.target = target_of(two && whole <= 256 ? tree_places(D) : 512, rows, D);
+    p.cut.split = ws && whole < 2 * p.cut.target && tiles >= 2 * p.cut.least;
+    p.items = p.cut.split ? std::min(whole + 2 * p.cut.target, whole * (tiles / p.cut.least + 1)) : whole;
+    return p;
+}
+
 template <int D, bool TREE>
-static int launch_attention(const Attend<TREE> &a, hipStream_t s)
+static int launch_join(const Attend<TREE> &a, const Cut &cut, hipStream_t s)
+{
+    constexpr int kPer = 1024 / D;
+    const int64_t T = cut.tokens ? (int64_t)a.s.B * cut.tokens : a.s.T;
+    return T * a.Hq >= 2048 ? enqueue(attend_join<D, true, TREE>, dim3((unsigned)(T * ((a.Hq + kPer - 1) / kPer))), dim3(256), 0, s, a, cut)
+                            : enqueue(attend_join<D, false, TREE>, dim3((unsigned)(T * a.Hq)), dim3(256), 0, s, a, cut);
+}
+
+template <int D>
+static int launch_tree(const Kv8TreeAttend &a, hipStream_t s)
+{
+    const Launch p = plan_tree(a);
+    if (p.items > 0x7fffffff) return MQ_ERR_SHAPE;
+    auto go = [&](auto kernel) { return enqueue(kernel, dim3((unsigned)p.items), dim3(kFewThreads), 0, s, a, p.cut); };
+    const int rc = p.cut.rows == kFewRows ? go(attend_tree<D, 1>) : go(attend_tree<D, D <= 128 ? 2 : 1>);
+    return rc || !p.cut.split ? rc : launch_join<D, true>(a, p.cut, s);
+}
+
+template <int D>
+static int launch_attention(const Kv8Attend &a, hipStream_t s)
 {
     Launch plan[2];
     const int n = plan_attention(a, plan);
@@ -1143,17 +1478,14 @@ static int launch_attention(const Attend<TREE> &a, hipStream_t s)
         auto go = [&](auto kernel, int threads) { return enqueue(kernel, dim3((unsigned)p.items), dim3(threads), 0, s, a, p.cut); };
         int rc;
         if (p.many)
-            rc = go(attend_many<D, TREE>, 64 * kManyWaves);
+            rc = go(attend_many<D>, 64 * kManyWaves);
         else if (p.cut.rows == kFewRows)
-            rc = go(attend_few<D, 1, TREE>, kFewThreads);
+            rc = go(attend_few<D, 1>, kFewThreads);
         else
-            rc = go(attend_few<D, D <= 128 ? 2 : 1, TREE>, kFewThreads);
+            rc = go(attend_few<D, D <= 128 ? 2 : 1>, kFewThreads);
         if (rc) return rc;
         if (!p.cut.split) continue;
-        constexpr int kPer = 1024 / D;
-        const int64_t T = p.cut.tokens ? (int64_t)a.s.B * p.cut.tokens : a.s.T;
-        rc = T * a.Hq >= 2048 ? enqueue(attend_join<D, true, TREE>, dim3((unsigned)(T * ((a.Hq + kPer - 1) / kPer))), dim3(256), 0, s, a, p.cut)
-                              : enqueue(attend_join<D, false, TREE>, dim3((unsigned)(T * a.Hq)), dim3(256), 0, s, a, p.cut);
+        rc = launch_join<D, false>(a, p.cut, s);
         if (rc) return rc;
     }
     return MQ_OK;
@@ -1172,13 +1504,13 @@ int describe_kv8_attention(const Kv8Attend &a, mq_kv8_launch *out)
 int launch_kv8_attention(const Kv8Attend &a, hipStream_t s)
 {
     if (a.s.T == 0 || a.s.B == 0) return MQ_OK;
-    return a.D == 64 ? launch_attention<64, false>(a, s) : a.D == 128 ? launch_attention<128, false>(a, s) : launch_attention<256, false>(a, s);
+    return a.D == 64 ? launch_attention<64>(a, s) : a.D == 128 ? launch_attention<128>(a, s) : launch_attention<256>(a, s);
 }
 
 int launch_kv8_tree_attention(const Kv8TreeAttend &a, hipStream_t s)
 {
     if (a.s.T == 0 || a.s.B == 0) return MQ_OK;
-    return a.D == 64 ? launch_attention<64, true>(a, s) : a.D == 128 ? launch_attention<128, true>(a, s) : launch_attention<256, true>(a, s);
+    return a.D == 64 ? launch_tree<64>(a, s) : a.D == 128 ? launch_tree<128>(a, s) : launch_tree<256>(a, s);
 }
 
 }  // namespace mq

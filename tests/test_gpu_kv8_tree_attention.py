@@ -90,11 +90,15 @@ def test_tokens_beyond_the_masks():
 
 
 def test_a_chain_is_causal_attention():
+    """To the tolerance that either has of its definition: the kernels may leave a row's maximum up to 2^8 behind at other places, which
+    changes which numbers are rounded but not how far a rounding goes, 2^-8 of a probability and 2^-24 of a sum."""
     for n, past in (([5, 1, 7], [300, 20, 0]), ([100, 64], [900, 0])):
         p = Problem(4, n, past, 8, 2, 128, 64, spread=1)
         args = p.device()
-        chain, causal = mq.kv8_tree_attention(*args, p.scale), mq.kv8_attention(*args[:-1], p.scale)
-        assert torch.equal(chain.view(torch.int16), causal.view(torch.int16))
+        y, a, s = p.reference()
+        assert np.array_equal(y, ref.attention(p.q, p.kc, p.ks, p.vc, p.vs, p.pt, p.cu, p.lens, p.scale)[0])
+        for got in (mq.kv8_tree_attention(*args, p.scale), mq.kv8_attention(*args[:-1], p.scale)):
+            assert (np.abs(got.float().cpu().numpy() - y) <= ref.attention_tolerance(y, a, s, 128)).all()
 
 
 def test_long_histories_are_cut_and_joined():
