@@ -31,14 +31,26 @@ struct Chunk {
     double mass;  // over that of the top of the largest logit's bin
 };
 
-// Count and mass of a chunk up to a bin in one word: count << 50 | mass in 2^-36 of the top of its largest logit's bin
+// Count and mass of a chunk up to a bin in one word: count << 50 | mass in 2^-36 of the weight at the end of the octave that the largest logit is
+// in (an octave is eight bins, the ends at multiples of eight), so that one chunk's masses become another's by shifts
 struct Upto {
     u64 word;
 };
 constexpr int kUptoCount = 50;
 constexpr double kUptoUnit = 0x1p36;
-static __device__ __forceinline__ double mass_of(Upto u) { return (double)(u.word & ((1ull << kUptoCount) - 1)) * (1.0 / kUptoUnit); }
+static __device__ __forceinline__ u64 mass_of(Upto u) { return u.word & ((1ull << kUptoCount) - 1); }
 static __device__ __forceinline__ int count_of(Upto u) { return (int)(u.word >> kUptoCount); }
+// the octave's end over eight, and the bins from the end of bin `edge` to it, 0 to 7
+static __device__ __forceinline__ double octave_of(double edge) { return ceil((edge + 1.0) * 0.125); }
+static __device__ __forceinline__ int bins_to_octave(double edge) { return (int)fmin(fmax(8.0 * octave_of(edge) - (edge + 1.0), 0.0), 7.0); }
+
+// What of a row's borders goes by the bins alone: the bins of the three borders, those of the mass's between what it is at least
+// and at most (what the first k have is only known to a bin)
+struct Borders {
+    int k, m, p0, p1;
+    bool part_k;     // whether the first k end inside their bin
+    double limit_m;  // the pos of min_p's
+};
 
 // What is known of a row with filters: the masses and counts up to each bin below its largest logit's, and the tokens, as numbers, of the
 // bins that a border may be in (listed may be more than there is room for)
@@ -46,7 +58,9 @@ constexpr int kList = 4096;
 struct Row {
     double masses[kBins];
     int counts[kBins];
-    int listed, pad;
+    double min_bits;  // bins from the largest logit's pos to the min_p border's, less than zero
+    Borders borders;
+    int listed;
     u64 list[kList];
 };
 
@@ -128,6 +142,13 @@ static __device__ __forceinline__ double power32(double v, const double *powers)
     return __builtin_ldexp(w * powers[n & 31], n >> 5);
 }
 
+// 2^(-b / 8)
+static __device__ __forceinline__ double eighth(int b)
+{
+    constexpr double e1 = 0.91700404320467123175, e2 = 0.84089641525371454303, e4 = 0.70710678118654752440;  // of one, two and four eighths
+    return __builtin_ldexp((b & 1 ? e1 : 1.0) * (b & 2 ? e2 : 1.0) * (b & 4 ? e4 : 1.0), -(b >> 3));
+}
+
 // Logits as unsigned numbers of the same order, the two zeros as one
 static __device__ __forceinline__ uint32_t key_of(float x)
 {
@@ -135,6 +156,18 @@ static __device__ __forceinline__ uint32_t key_of(float x)
     return u >> 31 ? ~u : u | 0x80000000u;
 }
 static __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
+
+// The lowest logit (as a key) with a pos of at least `limit` that has weight: pos is monotonous in it, and the quotient less than a step off
+static __device__ __forceinline__ uint32_t lowest(const Setting &s, float top, double limit)
+{
+    if (top == __builtin_inff()) return 0xff800000u;
+    if (s.scale == 0.0) return 0x00800000u;
+    const float y = (float)fmin(fmax(limit * s.inverse, -3.4028234663852886e38), 3.4028234663852886e38);
+    uint32_t key = key_of(y) - 2;
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) key += (double)value_of(key) * s.scale < limit;
+    return max(key, 0x00800000u);
+}
 
 typedef uint32_t words2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(4)));
@@ -189,13 +222,55 @@ static __device__ __forceinline__ float pick(u32x4 w, int j)
     return __uint_as_float(v);
 }
 
-template <class T, class F>
-static __device__ __forceinline__ T wave_fold(T v, F &&f)
+// v of the lane that a cross-lane control names, `none` where it names none.  (In registers: a step of a scan through LDS waits 100 cycles, and
+// these kernels have little else to do meanwhile.)
+template <int CONTROL, int ROWS, class T>
+static __device__ __forceinline__ T moved(T v, T none)
 {
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) / 4)));
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CONTROL, ROWS, 0xf, false));
+    } else {
+        words x = __builtin_bit_cast(words, v);
+        const words y = __builtin_bit_cast(words, none);
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = f(v, __shfl_xor(v, d));
-    return v;
+        for (int i = 0; i < 2; ++i) x[i] = (uint32_t)__builtin_amdgcn_update_dpp((int)y[i], (int)x[i], CONTROL, ROWS, 0xf, false);
+        return __builtin_bit_cast(T, x);
+    }
 }
+
+// Of each lane what f makes of it and the lanes in front: rows of 16 lanes by shifts of 1, 2, 4 and 8, then each row's last to the next
+// row, and the lower half's last to the upper.  none: what f leaves all values as they are with.
+template <class T, class F>
+static __device__ __forceinline__ T wave_scan(T v, T none, F &&f)
+{
+    v = f(v, moved<0x111, 0xf>(v, none));
+    v = f(v, moved<0x112, 0xf>(v, none));
+    v = f(v, moved<0x114, 0xf>(v, none));
+    v = f(v, moved<0x118, 0xf>(v, none));
+    v = f(v, moved<0x142, 0xa>(v, none));
+    return f(v, moved<0x143, 0xc>(v, none));
+}
+
+template <class T>
+static __device__ __forceinline__ T lane_of(T v, int lane)
+{
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+    } else {
+        typedef uint32_t words __attribute__((ext_vector_type(2)));
+        words x = __builtin_bit_cast(words, v);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[i] = (uint32_t)__builtin_amdgcn_readlane((int)x[i], lane);
+        return __builtin_bit_cast(T, x);
+    }
+}
+
+static __device__ __forceinline__ float wave_max(float v) { return lane_of(wave_scan(v, -__builtin_inff(), [](float x, float y) { return fmaxf(x, y); }), 63); }
+static __device__ __forceinline__ int wave_min(int v) { return lane_of(wave_scan(v, 0x7fffffff, [](int x, int y) { return min(x, y); }), 63); }
+// the sum of a lane's and those in front
+template <class T>
+static __device__ __forceinline__ T sum_to(T v) { return wave_scan(v, T(0), [](T x, T y) { return x + y; }); }
 
 // One chunk of kChunk logits.  They stay in LDS, so that the loop over them is no longer than its body: unrolled, the
 // code alone (12 KB read once by each compute unit) takes longer than the logits.
@@ -227,7 +302,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
         }
     }
     const float mine = top;
-    top = wave_fold(top, [](float u, float v) { return fmaxf(u, v); });
+    top = wave_max(top);
     if (lane == 0) tops[wave] = top;
     bins[2 * tid] = bins[2 * tid + 1] = 0, largest[2 * tid] = largest[2 * tid + 1] = 0;
     __syncthreads();
@@ -243,7 +318,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
             for (int i = N - 1; i >= 0; --i)
                 if (logit_of<T>(x, i) == top) first = base + (j * kChunkThreads + tid) * N + i;
         }
-        first = wave_fold(first, [](int u, int v) { return min(u, v); });
+        first = wave_min(first);
         if (lane == 0) firsts[wave] = first;
         __syncthreads();
         if (tid == 0) {
@@ -254,8 +329,9 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
         return;
     }
     const double edge = floor(pos_of(top, top, s.scale));  // the largest logit's bin
+    const double min_bits = s.min_p > 0.0f && (c == 0 || s.p >= 1.0f) ? 8.0 * log2((double)s.min_p) : 0.0;
+    if (s.filters && tid == 0 && c == 0) t.rows[local].listed = 0, t.rows[local].min_bits = min_bits;
     if (!s.filters || top == -__builtin_inff()) {
-        if (s.filters && tid == 0 && c == 0) t.rows[local].listed = 0;
         // (in 64 bits these few instructions take as long as the loads; NaN and -infinity come out as 2^-1000)
         if (tid < 32) powers[tid] = power(0.03125 * tid);
         __syncthreads();
@@ -276,8 +352,8 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
                 }
             }
         }
-        sum = wave_fold(sum, [](double u, double v) { return u + v; });
-        if (lane == 0) sums[wave] = sum;
+        sum = sum_to(sum);
+        if (lane == 63) sums[wave] = sum;
         __syncthreads();
         if (tid == 0) {
             sum = 0.0;
@@ -295,12 +371,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
         if (weighs(mine, top) && below < kBins) atomicAdd(&largest[(int)below], 1);
         __syncthreads();
         const int n0 = largest[2 * tid], n1 = n0 + largest[2 * tid + 1];
-        int n = n1;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int u = __shfl_up(n, d);
-            if (lane >= d) n += u;
-        }
+        int n = sum_to(n1);
         if (lane == 63) firsts[wave] = n;
         __syncthreads();
 #pragma unroll
@@ -309,19 +380,19 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
         const int before = n - n1;
         last = fmin(last, (double)(__syncthreads_count(n < s.k) + __syncthreads_count(before + n0 < s.k)));
     }
-    if (s.min_p > 0.0f && s.p >= 1.0f) last = fmin(last, 1.0 - floor(8.0 * log2((double)s.min_p)));
-    const bool finite = top != __builtin_inff();
+    if (s.min_p > 0.0f && s.p >= 1.0f) last = fmin(last, 1.0 - floor(min_bits));
+    const float least = value_of(lowest(s, top, edge - last));
 #pragma unroll 1
     for (int j = 0; j < NV; ++j) {
         const u32x4 x = stage[j][tid];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float y = bits_of<T>(x, i);
-            const double pos = finite ? (double)y * s.scale : y == top ? 0.0 : -0x1p1000, q = floor(pos), below = edge - q;
-            if (below <= last) {  // (not for NaN and -infinity)
+            if (y >= least) {  // (not for NaN and -infinity)
+                const double pos = pos_of(y, top, s.scale), q = floor(pos);
                 // 2^52 more than the shortfall, whose bits are then the low ones
                 const double d = __builtin_fma(in_bin(pos - q), -kFine, kFine + 0x1p52);
-                atomicAdd(&bins[(int)below], (1ull << kCountBit) + (__builtin_bit_cast(u64, d) - 0x4330000000000000ull));
+                atomicAdd(&bins[(int)(edge - q)], (1ull << kCountBit) + (__builtin_bit_cast(u64, d) - 0x4330000000000000ull));
             }
         }
     }
@@ -333,33 +404,25 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
     for (int i = 0; i < 2; ++i) {
         const u64 bin = bins[2 * tid + i];
         count[i] = (int)(bin >> kCountBit);
-        mass[i] = ((double)((u64)count[i] << 34) - (double)(bin & ((1ull << kCountBit) - 1))) * (1.0 / kFine) * power(-0.25 * tid - 0.125 * i);
+        mass[i] = ((double)((u64)count[i] << 34) - (double)(bin & ((1ull << kCountBit) - 1))) * (1.0 / kFine) * eighth(2 * tid + i);
     }
-    int n = count[0] + count[1];
-    double m = mass[0] + mass[1];
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int u = __shfl_up(n, d);
-        const double v = __shfl_up(m, d);
-        if (lane >= d) n += u, m += v;
-    }
+    int n = sum_to(count[0] + count[1]);
+    double m = sum_to(mass[0] + mass[1]);
     if (lane == 63) firsts[wave] = n, sums[wave] = m;
-    const int own_n = __shfl_up(n, 1);
-    const double own_m = __shfl_up(m, 1);
-    n = lane > 0 ? own_n : 0, m = lane > 0 ? own_m : 0.0;
+    n -= count[0] + count[1], m -= mass[0] + mass[1];
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < NW; ++w)
         if (w < wave) n += firsts[w], m += sums[w];
     Upto out2[2];
+    const double unit = kUptoUnit * eighth(bins_to_octave(edge));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         n += count[i], m += mass[i];
-        out2[i] = Upto{(u64)n << kUptoCount | (u64)(m * kUptoUnit + 0.5)};
+        out2[i] = Upto{(u64)n << kUptoCount | (u64)(m * unit + 0.5)};
     }
     *reinterpret_cast<u32x4 *>(t.upto + (int64_t)blockIdx.x * kBins + 2 * tid) = __builtin_bit_cast(u32x4, out2);
     if (tid == kChunkThreads - 1) *out = Chunk{top, 0, m};
-    if (tid == 0 && c == 0) t.rows[local].listed = 0;
 }
 static_assert(2 * kChunkThreads == kBins, "two bins a thread");
 
@@ -377,20 +440,13 @@ static __device__ __forceinline__ u64 number_of(uint32_t key, int i)
     return (u64)(sizeof(T) == 2 ? key >> 16 : key) << 20 | (0xfffff - i);
 }
 
-// What of a row's borders goes by the bins alone: the bins of the three borders, those of the mass's between what it is at least
-// and at most (what the first k have is only known to a bin)
-struct Borders {
-    int k, m, p0, p1;
-    bool part_k;  // whether the first k end inside their bin
-};
 template <class F>
-static __device__ __forceinline__ Borders borders_of(const Setting &s, double peak, double edge, const double *masses, const int *counts, int tid, double &limit_m, F &&sync_count)
+static __device__ __forceinline__ Borders borders_of(const Setting &s, double peak, double edge, double min_bits, const double *masses, const int *counts, int tid, F &&sync_count)
 {
-    Borders b{kBins, kBins, kBins, kBins, false};
-    limit_m = -__builtin_inf();
+    Borders b{kBins, kBins, kBins, kBins, false, -__builtin_inf()};
     if (s.min_p > 0.0f) {
-        limit_m = peak + 8.0 * log2((double)s.min_p);
-        b.m = (int)fmin(edge - floor(limit_m), (double)kBins);
+        b.limit_m = peak + min_bits;
+        b.m = (int)fmin(edge - floor(b.limit_m), (double)kBins);
     }
     if (s.k > 0) b.k = sync_count(tid < kBins && counts[tid] < s.k);
     double most = masses[kBins - 1], least = most;
@@ -414,10 +470,10 @@ __global__ __launch_bounds__(kRowThreads) void sample_border(Sample a, Tables t,
     constexpr int NT = kRowThreads, N = 16 / sizeof(T);
     constexpr float kInf = __builtin_inff();
     __shared__ float tops[kChunksMost];
-    __shared__ int shifts[kChunksMost];
-    __shared__ double scales[kChunksMost], masses[kBins];
+    __shared__ int2 shifts[kChunksMost];  // bins below the row's largest logit's, and octaves
+    __shared__ double masses[kBins];
+    __shared__ u64 sums[kBins];
     __shared__ int counts[kBins];
-    __shared__ bool need[kBins + 1];
     __shared__ u64 list[kList];
     __shared__ int listed, at;
     const int tid = threadIdx.x, lane = tid & 63, V = (int)a.V, local = blockIdx.x / parts, part = blockIdx.x - local * parts;
@@ -427,55 +483,66 @@ __global__ __launch_bounds__(kRowThreads) void sample_border(Sample a, Tables t,
     const Chunk *const heads = t.chunks + (int64_t)local * chunks;
     const Upto *const upto = t.upto + (int64_t)local * chunks * kBins;
     Row &out = t.rows[local];
+    const double min_bits = out.min_bits;
     float own = -kInf;
     if (tid < chunks) tops[tid] = own = heads[tid].top;
     __syncthreads();
     float top = -kInf;
     for (int c = lane; c < chunks; c += 64) top = fmaxf(top, tops[c]);
-    top = wave_fold(top, [](float u, float v) { return fmaxf(u, v); });
+    top = wave_max(top);
     if (top == -kInf) return;
     const double peak = pos_of(top, top, s.scale), edge = floor(peak);
     if (tid < chunks) {
         const double below = own == top ? 0.0 : !weighs(own, top) ? kBins : fmin(edge - floor(own * s.scale), (double)kBins);
-        shifts[tid] = (int)below;
-        scales[tid] = power(-0.125 * below);
+        shifts[tid] = int2{(int)below, below < kBins ? (int)(octave_of(edge) - octave_of(edge - below)) : 63};
     }
-    if (tid <= kBins) need[tid] = false;
     if (tid == 0) listed = 0;
     __syncthreads();
     {  // half of the chunks by each half of the threads
         const int b = tid & (kBins - 1), half = tid / kBins;
-        double m = 0.0;
+        u64 m = 0;
         int n = 0;
 #pragma unroll 8
         for (int c = half; c < chunks; c += NT / kBins) {
-            const int i = b - shifts[c];
-            const Upto u = upto[c * kBins + max(i, 0)];
-            if (i >= 0) m += mass_of(u) * scales[c], n += count_of(u);
+            const int2 shift = shifts[c];
+            const Upto u{shift.x > b ? 0 : upto[c * kBins + b - min(shift.x, b)].word};
+            m += ((mass_of(u) << 1 >> shift.y) + 1) >> 1, n += count_of(u);
         }
-        if (half) masses[b] = m, counts[b] = n;
+        if (half) sums[b] = m, counts[b] = n;
         __syncthreads();
-        if (!half) masses[b] += m, counts[b] += n;
+        if (!half) masses[b] = (double)(m + sums[b]) * (1.0 / kUptoUnit) * eighth(-bins_to_octave(edge)), counts[b] += n;
         __syncthreads();
         if (part == 0 && !half) out.masses[b] = masses[b], out.counts[b] = counts[b];
     }
     static_assert(NT == 2 * kBins, "two halves");
-    double limit_m;
-    const Borders b = borders_of(s, peak, edge, masses, counts, tid, limit_m, [](bool x) { return __syncthreads_count(x); });
-    if (tid < kBins)
-        need[tid] = (tid == b.k && b.part_k && (s.p < 1.0f || b.k <= b.m)) || (tid >= b.p0 && tid <= b.p1 && tid <= b.m) || (tid == b.m && b.m <= b.k && b.m <= b.p1);
-    __syncthreads();
+    const Borders b = borders_of(s, peak, edge, min_bits, masses, counts, tid, [](bool x) { return __syncthreads_count(x); });
+    if (part == 0 && tid == 0) out.borders = b;
+    // The bins that a border is in.  The logits between the first of them and the last are few as a rule: two comparisons in 32 bits find them (
+    // -0 may count as in front of 0 there), and what has bins is asked of them alone.
+    const bool need_k = b.k < kBins && b.part_k && (s.p < 1.0f || b.k <= b.m), need_m = b.m < kBins && b.m <= b.k && b.m <= b.p1;
+    const int p1 = min(min(b.p1, b.m), kBins - 1);
+    const bool need_p = b.p0 <= p1;
+    const int from = min(min(need_k ? b.k : kBins, need_m ? b.m : kBins), need_p ? b.p0 : kBins);
+    const int to = max(max(need_k ? b.k : -1, need_m ? b.m : -1), need_p ? p1 : -1);
+    if (to < 0) return;
+    const float least = value_of(lowest(s, top, edge - to)), most = from > 0 ? value_of(lowest(s, top, edge - from + 1) - 1) : kInf;
     const T *const row = reinterpret_cast<const T *>(a.logits) + r * a.ld;
     const int first = (int)((int64_t)chunks * part / parts) * kChunk, end = min(V, (int)((int64_t)chunks * (part + 1) / parts) * kChunk);
-    // the bins' numbers, a token's in 64 bits
 #pragma unroll 1
     for (int i0 = first + tid * N; i0 < end; i0 += NT * N) {
         const u32x4 x = load16(row, i0, V);
+        uint32_t some = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float y = logit_of<T>(x, i);
-            const double below = edge - floor(pos_of(y, top, s.scale));
-            if (weighs(y, top) && below < kBins && need[(int)below]) {
+            const float y = bits_of<T>(x, i);
+            some |= (uint32_t)(y >= least && y <= most) << i;
+        }
+#pragma unroll 1
+        for (; some; some &= some - 1) {
+            const int i = __builtin_ctz(some);
+            const float y = pick<T>(x, i);
+            const int bin = (int)(edge - floor(pos_of(y, top, s.scale)));
+            if ((need_k && bin == b.k) || (need_m && bin == b.m) || (bin >= b.p0 && bin <= p1)) {
                 const int slot = atomicAdd(&listed, 1);
                 if (slot < kList) list[slot] = number_of<T>(key_of(y), i0 + i);
             }
@@ -529,6 +596,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     if (tid < 32) l.powers[tid] = power(0.03125 * tid);
     const bool filters = F && s.filters && !s.largest;
     [[maybe_unused]] const int listed = filters ? known.listed : 0;
+    Borders known_to{};
+    if (F && filters) known_to = known.borders;
     if (F && filters) {
         if (tid < kBins) l.masses[tid] = known.masses[tid], l.counts[tid] = known.counts[tid];
 #pragma unroll
@@ -538,13 +607,13 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     __syncthreads();
     float top = -kInf;
     for (int c = lane; c < chunks; c += 64) top = fmaxf(top, l.tops[c]);
-    top = wave_fold(top, [](float u, float v) { return fmaxf(u, v); });
+    top = wave_max(top);
     if (s.largest || top == -kInf) {
         if (wave == 0) {
             int first = 0x7fffffff;
             for (int c = lane; c < chunks; c += 64)
                 if (l.tops[c] == top) first = min(first, parts[c].first);
-            first = wave_fold(first, [](int u, int v) { return min(u, v); });
+            first = wave_min(first);
             if (lane == 0) a.tokens[r] = top == -kInf ? -1 : first;
         }
         return;
@@ -553,7 +622,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     if (tid < chunks) {
         const double below = own.top == top ? 0.0 : !weighs(own.top, top) ? kBins : fmin(edge - floor(own.top * s.scale), (double)kBins);
         l.shift[tid] = (int)below;
-        l.scale[tid] = below < kBins ? power(-0.125 * below) : 0.0;
+        l.scale[tid] = below < kBins ? eighth((int)below) : 0.0;
         l.kept[tid] = own.mass * l.scale[tid];
         l.part[tid] = 0;
     }
@@ -563,19 +632,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
         const uint32_t key = (uint32_t)(number >> 20);
         return value_of(sizeof(T) == 4 ? key : key << 16 | (key >> 15 ? 0u : 0xffffu));
     };
-    // The lowest logit (as a key) with a pos of at least `limit` that has weight: pos is monotonous in it, and the quotient less than a step off
-    auto lowest = [&](double limit) -> uint32_t {
-        if (top == kInf) return 0xff800000u;
-        if (s.scale == 0.0) return 0x00800000u;
-        const float y = (float)fmin(fmax(limit * s.inverse, -3.4028234663852886e38), 3.4028234663852886e38);
-        uint32_t key = key_of(y) - 2;
-#pragma unroll 1
-        for (int i = 0; i < 4; ++i) key += (double)value_of(key) * s.scale < limit;
-        return max(key, 0x00800000u);
-    };
     // the lowest number of a logit from `key` on (16 bits of a key stand for the first of 65536 above zero, below for the last)
     auto number_from = [&](uint32_t key) { return number_of<T>(sizeof(T) == 2 && key >> 31 ? key + 0xffffu : key, 0xfffff); };
-    auto first_of = [&](int b) { return lowest(edge - b); };                       // of bin b's logits
+    auto first_of = [&](int b) { return lowest(s, top, edge - b); };                       // of bin b's logits
 
     // The least number that is kept, and its bin: the filters' borders are such numbers, and the highest of them counts
     u64 cut = number_of<T>(top == kInf ? 0xff800000u : 0x00800000u, 0xfffff);
@@ -583,11 +642,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
         auto mass_to = [&](int b) { return b > 0 ? l.masses[b - 1] : 0.0; };  // of the bins in front of b
         auto count_in = [&](int b) { return l.counts[b] - (b > 0 ? l.counts[b - 1] : 0); };
         auto reaching = [&](double limit) { return __syncthreads_count(tid < kBins && l.masses[tid] < limit); };
-        double limit_m;
-        const Borders known_to = borders_of(s, peak, edge, l.masses, l.counts, tid, limit_m, [](bool x) { return __syncthreads_count(x); });
         const int bin_m = known_to.m, bin_k = known_to.k;
         int bin_p = kBins;
-        if (s.min_p > 0.0f) cut = max(cut, number_from(lowest(limit_m)));
+        if (s.min_p > 0.0f) cut = max(cut, number_from(lowest(s, top, known_to.limit_m)));
         double all = l.masses[min(bin_k, kBins - 1)], limit_p = 0.0;
 
         // The border of the first k in its bin, that of the mass in its, and what is kept of the last bin, each where it is needed.
@@ -625,7 +682,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
                     if (bin_p < kBins && bin_p <= bin_m) {
                         task = kMass;
                         look_at(bin_p);
-                        limit = (limit_p - mass_to(bin_p)) * (0x1p40 / power(-0.125 * bin_p));
+                        limit = (limit_p - mass_to(bin_p)) * (0x1p40 * eighth(-bin_p));
                     }
                 }
             }
@@ -683,14 +740,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
                     u64 dm[4], sm = 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) dn[i] = l.digit_counts[255 - 4 * lane - i], dm[i] = l.digit_masses[255 - 4 * lane - i], sn += dn[i], sm += dm[i];
-                    int fn = sn;
-                    u64 fm = sm;
-#pragma unroll
-                    for (int d = 1; d < 64; d <<= 1) {
-                        const int un = __shfl_up(fn, d);
-                        const u64 um = (u64)__shfl_up((long long)fm, d);
-                        if (lane >= d) fn += un, fm += um;
-                    }
+                    int fn = sum_to(sn);
+                    u64 fm = sum_to(sm);
                     auto reaches = [&](int number, u64 sum) { return (task == kMass ? (double)sum : (double)number) >= limit; };
                     const u64 hits = __ballot(reaches(n + fn, mass + fm));
                     if (lane == (hits ? __ffsll(hits) - 1 : 63)) {  // (rounding may leave the limit behind all of them)
@@ -738,14 +789,14 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
             }
             __syncthreads();
             cut = max(cut, l.cut);
-            if (task == kCount) all = mass_to(bin_k) + (double)l.found_mass * 0x1p-40 * power(-0.125 * bin_k);
+            if (task == kCount) all = mass_to(bin_k) + (double)l.found_mass * 0x1p-40 * eighth(bin_k);
             task = kNew + task + 1;
         }
         const int border = min(min(bin_k, bin_p), bin_m);
         if (border < kBins && tid < chunks) {
             const int b = border - l.shift[tid] + whole;
-            const double m = b > 0 && l.shift[tid] < kBins ? mass_of(upto[tid * kBins + b - 1]) : 0.0;
-            l.kept[tid] = m * l.scale[tid] + (double)l.part[tid] * 0x1p-40 * power(-0.125 * border);
+            const double m = b > 0 && l.shift[tid] < kBins ? (double)mass_of(upto[tid * kBins + b - 1]) * (1.0 / kUptoUnit) * eighth(-bins_to_octave(edge - l.shift[tid])) : 0.0;
+            l.kept[tid] = m * l.scale[tid] + (double)l.part[tid] * 0x1p-40 * eighth(border);
         }
         __syncthreads();
     }
@@ -754,13 +805,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     if (wave == 0) {
         static_assert(kChunksMost == 128, "two a lane");
         const double m0 = 2 * lane < chunks ? l.kept[2 * lane] : 0.0, m1 = 2 * lane + 1 < chunks ? l.kept[2 * lane + 1] : 0.0, sum = m0 + m1;
-        double front = sum;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const double u = __shfl_up(front, d);
-            if (lane >= d) front += u;
-        }
-        const double total = __shfl(front, 63), u = (double)a.uniform[r];
+        const double front = sum_to(sum), total = lane_of(front, 63), u = (double)a.uniform[r];
         const double aim = u > 0.0 ? fmin(u, 1.0 - 0x1p-40) * total : 0.0;
         const u64 hits = __ballot(front > aim && sum > 0.0), some = __ballot(sum > 0.0);
         if (lane == (hits ? __ffsll(hits) - 1 : 63 - __clzll((long long)some))) {  // (rounding may leave the draw behind the last)
@@ -789,10 +834,13 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const float y = bits_of<T>(x[i / N], i % N);
+            bool kept = top != kInf || y == top;
+            if (F) {
+                kept = y == y && number_of<T>(key_of(y), first + i) >= cut;
+                if (!__any(kept)) continue;
+            }
             // (2^52 more than the weight, which is then in the low bits; NaN and -infinity weigh nothing)
             const double w = power32(__builtin_fma(pos_of(y, top, s.scale), 4.0, from), l.powers);
-            bool kept = top != kInf || y == top;
-            if (F) kept = y == y && number_of<T>(key_of(y), first + i) >= cut;
             sum += kept ? __builtin_bit_cast(u64, __builtin_fma(w, 0x1p43, 0x1p52)) - 0x4330000000000000ull : 0;
             if (token < 0 && before + sum > aim) token = first + i;
         }
@@ -800,12 +848,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
             if (mine) a.tokens[r] = token;
             break;
         }
-        u64 front = sum;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const u64 u = (u64)__shfl_up((long long)front, d);
-            if (lane >= d) front += u;
-        }
+        const u64 front = sum_to(sum);
         if (lane == 63) l.fronts[wave] = front;
         __syncthreads();
         u64 total = 0;
