@@ -9,10 +9,14 @@
 // together by shifting.  Weights in a bin lie between 2^-1/8 and 1 of its top, and a bin's mass is its count less
 // what its weights fall short of one: 64 bits hold both, 2^-34 of a weight fine, and one addition in LDS counts a token.
 //
-// Two kernels.  sample_chunks reads the logits once, a chunk of a row by a workgroup: the largest, the mass, and where the row has
-// filters the count and mass up to each of the 512 bins below the chunk's largest (weights down to 2^-64).  sample_rows, a
-// workgroup a row: the border's bin from the sums of the chunks', the border in it, the chunk that the draw falls into, the token.
-// Bound by reading the logits, and for few rows by the trips to memory that one kernel and the other take one after another.
+// Three kernels.  sample_chunks reads the logits once, a chunk of a row by a workgroup: the largest, the mass, and where the row has
+// filters the count and mass up to each of the 512 bins below the chunk's largest (weights down to 2^-64).  sample_border, several workgroups a row:
+// the row's own sums from those, the bins that the borders are in, and their tokens.  sample_rows, a workgroup a row: the borders among those
+// tokens, the chunk that the draw falls into, the token.  Without filters the first and the last are all.
+// 64 rows of 151673 with all filters, BF16: 47 to 48 us (16, 13 and 17 and what lies between); a large copy would read them in 4.  Counting in 64 bits bounds
+// the first (22 vector instructions and an addition in LDS a logit), trips to memory and to a barrier one after another the others, as they do
+// all of one row's 23 us.  500 rows of 100003 in FP32 by temperature alone: 56 to 70 us, 41 by a large copy; reading takes as long as the 20
+// instructions of each weight's power of two, and the two overlap in part.
 #include "kv8.h"
 
 namespace mq {
@@ -21,7 +25,7 @@ typedef unsigned long long u64;
 constexpr int kBins = 512;
 constexpr int kCountBit = 47;  // a bin of a chunk: count << 47 | shortfall in 2^-34, at most 2^14 * 2^30.4
 constexpr double kFine = (double)(1ll << 34);
-constexpr int kChunkThreads = 256, kRowThreads = 1024;
+constexpr int kChunkThreads = 256, kBorderThreads = 1024, kRowThreads = 512;
 constexpr int kChunk = 8192;  // logits
 constexpr int kChunksMost = (int)(kSampleTokens / kChunk);  // of a row
 
@@ -157,16 +161,15 @@ static __device__ __forceinline__ uint32_t key_of(float x)
 }
 static __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
 
-// The lowest logit (as a key) with a pos of at least `limit` that has weight: pos is monotonous in it, and the quotient less than a step off
+// The lowest logit (as a key) with a pos of at least `limit` that has weight: pos is monotonous in it, and the quotient less than a step off,
+// so a lane tries each of the four around it.  (Of the whole wave.)
 static __device__ __forceinline__ uint32_t lowest(const Setting &s, float top, double limit)
 {
     if (top == __builtin_inff()) return 0xff800000u;
     if (s.scale == 0.0) return 0x00800000u;
     const float y = (float)fmin(fmax(limit * s.inverse, -3.4028234663852886e38), 3.4028234663852886e38);
-    uint32_t key = key_of(y) - 2;
-#pragma unroll 1
-    for (int i = 0; i < 4; ++i) key += (double)value_of(key) * s.scale < limit;
-    return max(key, 0x00800000u);
+    const uint32_t key = key_of(y) - 2;
+    return max(key + __popcll(__ballot((double)value_of(key + (threadIdx.x & 3)) * s.scale < limit) & 15), 0x00800000u);
 }
 
 typedef uint32_t words2 __attribute__((ext_vector_type(4), aligned(2)));
@@ -298,7 +301,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
         for (int j = 0; j < NV; ++j) {
             stage[j][tid] = x[j];
 #pragma unroll
-            for (int i = 0; i < N; ++i) top = fmaxf(top, logit_of<T>(x[j], i));
+            for (int i = 0; i < N; i += 2) top = fmaxf(top, fmaxf(bits_of<T>(x[j], i), bits_of<T>(x[j], i + 1)));  // (the maximum of a number and NaN is the number)
         }
     }
     const float mine = top;
@@ -364,7 +367,8 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
         return;
     }
     // Bins behind which nothing counts: behind those of the largest k of the threads' largest, and behind what min_p leaves where the
-    // mass of the others is not asked for.  An addition in LDS to a bin that lanes share waits for them (all filters on 64 rows of 151673: 22.4 us, 14.9 so).
+    // mass of the others is not asked for.  An addition in LDS
+    // to a bin that lanes share waits for them (64 rows of 151673 with all filters: sample_chunks 18 us, 22 without).  What is behind is found by its logit.
     double last = kBins - 1;
     if (s.k > 0 && s.k <= kChunkThreads) {
         const double below = edge - floor(pos_of(mine, top, s.scale));
@@ -440,15 +444,23 @@ static __device__ __forceinline__ u64 number_of(uint32_t key, int i)
     return (u64)(sizeof(T) == 2 ? key >> 16 : key) << 20 | (0xfffff - i);
 }
 
-template <class F>
-static __device__ __forceinline__ Borders borders_of(const Setting &s, double peak, double edge, double min_bits, const double *masses, const int *counts, int tid, F &&sync_count)
+// How many of the sums up to each bin (which rise) are below a limit: each wave looks at all of them, which takes no barrier
+template <class T>
+static __device__ __forceinline__ int bins_below(const T *upto, T limit, int lane)
+{
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kBins; i += 64) n += __popcll(__ballot(upto[i + lane] < limit));
+    return n;
+}
+static __device__ __forceinline__ Borders borders_of(const Setting &s, double peak, double edge, double min_bits, const double *masses, const int *counts, int lane)
 {
     Borders b{kBins, kBins, kBins, kBins, false, -__builtin_inf()};
     if (s.min_p > 0.0f) {
         b.limit_m = peak + min_bits;
         b.m = (int)fmin(edge - floor(b.limit_m), (double)kBins);
     }
-    if (s.k > 0) b.k = sync_count(tid < kBins && counts[tid] < s.k);
+    if (s.k > 0) b.k = bins_below(counts, s.k, lane);
     double most = masses[kBins - 1], least = most;
     if (b.k < kBins) {
         most = least = masses[b.k];
@@ -456,18 +468,19 @@ static __device__ __forceinline__ Borders borders_of(const Setting &s, double pe
         if (b.part_k) least = b.k > 0 ? masses[b.k - 1] : 0.0;
     }
     if (s.p < 1.0f) {
-        b.p0 = min(sync_count(tid < kBins && masses[tid] < (double)s.p * least), b.k);
-        b.p1 = min(sync_count(tid < kBins && masses[tid] < (double)s.p * most), b.k);
+        b.p0 = min(bins_below(masses, (double)s.p * least, lane), b.k);
+        b.p1 = min(bins_below(masses, (double)s.p * most, lane), b.k);
     }
     return b;
 }
 
 // A row's counts and masses up to each bin, and the tokens of the bins that a border is in, a part of the row's chunks by each
-// workgroup.
+// workgroup: as many in all as there are compute units, since each adds up all chunks' sums first (64 rows in 256 workgroups 13 us, in 512
+// 15.5; the additions as integers, which 64-bit ones of floating numbers took 1.2 us more for).
 template <class T>
-__global__ __launch_bounds__(kRowThreads) void sample_border(Sample a, Tables t, int64_t row0, int chunks, int parts)
+__global__ __launch_bounds__(kBorderThreads) void sample_border(Sample a, Tables t, int64_t row0, int chunks, int parts)
 {
-    constexpr int NT = kRowThreads, N = 16 / sizeof(T);
+    constexpr int NT = kBorderThreads, N = 16 / sizeof(T);
     constexpr float kInf = __builtin_inff();
     __shared__ float tops[kChunksMost];
     __shared__ int2 shifts[kChunksMost];  // bins below the row's largest logit's, and octaves
@@ -515,7 +528,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_border(Sample a, Tables t,
         if (part == 0 && !half) out.masses[b] = masses[b], out.counts[b] = counts[b];
     }
     static_assert(NT == 2 * kBins, "two halves");
-    const Borders b = borders_of(s, peak, edge, min_bits, masses, counts, tid, [](bool x) { return __syncthreads_count(x); });
+    const Borders b = borders_of(s, peak, edge, min_bits, masses, counts, lane);
     if (part == 0 && tid == 0) out.borders = b;
     // The bins that a border is in.  The logits between the first of them and the last are few as a rule: two comparisons in 32 bits find them (
     // -0 may count as in front of 0 there), and what has bins is asked of them alone.
@@ -577,7 +590,8 @@ struct RowLds {
 };
 
 // One row by one workgroup.  What takes it is one trip to memory after another, and its own code, which each compute unit reads
-// once, from memory: so everything that looks at tokens stands here once, in loops.  F: rows may have filters.
+// once, from memory: so everything that looks at tokens stands here once, in loops.  512 threads, since much of it is done by every wave alike and four
+// waves a SIMD wait for each other there (a pass over a border's tokens 1.2 us, 1.7 with 1024).  F: rows may have filters.
 template <class T, bool F>
 __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, int64_t row0, int chunks)
 {
@@ -641,7 +655,6 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     if constexpr (F) if (filters) {
         auto mass_to = [&](int b) { return b > 0 ? l.masses[b - 1] : 0.0; };  // of the bins in front of b
         auto count_in = [&](int b) { return l.counts[b] - (b > 0 ? l.counts[b - 1] : 0); };
-        auto reaching = [&](double limit) { return __syncthreads_count(tid < kBins && l.masses[tid] < limit); };
         const int bin_m = known_to.m, bin_k = known_to.k;
         int bin_p = kBins;
         if (s.min_p > 0.0f) cut = max(cut, number_from(lowest(s, top, known_to.limit_m)));
@@ -678,7 +691,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
                 task = kNew + kRest;
                 if (s.p < 1.0f) {
                     limit_p = (double)s.p * all;
-                    bin_p = min(reaching(limit_p), bin_k);
+                    bin_p = min(bins_below(l.masses, limit_p, lane), bin_k);
                     if (bin_p < kBins && bin_p <= bin_m) {
                         task = kMass;
                         look_at(bin_p);
@@ -817,7 +830,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     }
     __syncthreads();
 
-    // The token in it, eight side by side to a thread: weights in whole 2^-43 of the top of the chunk's first bin, so that all sums
+    // The token in it, sixteen side by side to a thread: weights in whole 2^-43 of the top of the chunk's first bin, so that all sums
     // agree (what is kept of a chunk has its largest logit in it).
     constexpr int kEach = kChunk / NT, kVectors = kEach / N;
     const int chosen = l.chosen, first = chosen * kChunk + tid * kEach;
@@ -831,18 +844,25 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     for (int pass = 0; pass < 2; ++pass) {
         u64 sum = 0;
         int token = -1;
+#pragma unroll 1
+        for (int j = 0; j < kVectors; ++j) {
+            u32x4 v = x[0];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const float y = bits_of<T>(x[i / N], i % N);
-            bool kept = top != kInf || y == top;
-            if (F) {
-                kept = y == y && number_of<T>(key_of(y), first + i) >= cut;
-                if (!__any(kept)) continue;
+            for (int q = 1; q < kVectors; ++q) v = j == q ? x[q] : v;
+            uint32_t kept = 0;  // a bit each
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float y = bits_of<T>(v, i);
+                kept |= (uint32_t)(F ? y == y && number_of<T>(key_of(y), first + j * N + i) >= cut : top != kInf || y == top) << i;
             }
-            // (2^52 more than the weight, which is then in the low bits; NaN and -infinity weigh nothing)
-            const double w = power32(__builtin_fma(pos_of(y, top, s.scale), 4.0, from), l.powers);
-            sum += kept ? __builtin_bit_cast(u64, __builtin_fma(w, 0x1p43, 0x1p52)) - 0x4330000000000000ull : 0;
-            if (token < 0 && before + sum > aim) token = first + i;
+            if (F && !__any(kept)) continue;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                // (2^52 more than the weight, which is then in the low bits; NaN and -infinity weigh nothing)
+                const double w = power32(__builtin_fma(pos_of(bits_of<T>(v, i), top, s.scale), 4.0, from), l.powers);
+                sum += kept >> i & 1 ? __builtin_bit_cast(u64, __builtin_fma(w, 0x1p43, 0x1p52)) - 0x4330000000000000ull : 0;
+                if (token < 0 && before + sum > aim) token = first + j * N + i;
+            }
         }
         if (pass) {
             if (mine) a.tokens[r] = token;
@@ -895,8 +915,8 @@ static int sample_typed(const Sample &a, hipStream_t s)
         };
         if (int rc = go(sample_chunks<T>, n * chunks, kChunkThreads)) return rc;
         if (filters) {
-            const int64_t parts = std::min(chunks, std::max<int64_t>(512 / n, 1));
-            if (int rc = go(sample_border<T>, n * parts, kRowThreads, (int)parts)) return rc;
+            const int64_t parts = std::min(chunks, std::max<int64_t>(256 / n, 1));
+            if (int rc = go(sample_border<T>, n * parts, kBorderThreads, (int)parts)) return rc;
         }
         if (int rc = filters ? go(sample_rows<T, true>, n, kRowThreads) : go(sample_rows<T, false>, n, kRowThreads)) return rc;
     }
