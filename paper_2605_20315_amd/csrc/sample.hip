@@ -507,7 +507,7 @@ __global__ __launch_bounds__(kBorderThreads) void sample_border(Sample a, Tables
     const double peak = pos_of(top, top, s.scale), edge = floor(peak);
     if (tid < chunks) {
         const double below = own == top ? 0.0 : !weighs(own, top) ? kBins : fmin(edge - floor(own * s.scale), (double)kBins);
-        shifts[tid] = int2{(int)below, below < kBins ? (int)(octave_of(edge) - octave_of(edge - below)) : 63};
+        shifts[tid] = int2{(int)below, (int)fmin(octave_of(edge) - octave_of(edge - below), 63.0)};
     }
     if (tid == 0) listed = 0;
     __syncthreads();

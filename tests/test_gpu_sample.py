@@ -138,6 +138,22 @@ def test_wide_ranges_of_logits():
         check(x, r.random(8).astype(np.float32), {"temperature": np.full(8, t, np.float32), "top_k": np.full(8, 900, np.int32), "top_p": np.full(8, 0.9, np.float32)})
 
 
+@pytest.mark.parametrize("below", [448, 503, 504, 505, 510, 511, 512, 520])
+def test_parts_of_a_row_that_lie_far_below_its_largest(below):
+    """A part of 8192 logits so many eighths of a power of two below the largest: its mass, next to nothing, is not to move the border of top_p."""
+    eighth = np.log(2.0) / 8
+    rows = []
+    for first in range(8):
+        x = np.full(16384, -np.inf)
+        x[0], x[1:51] = (32 + first + 0.5) * eighth, (32 + first + 0.5) * eighth - np.log(1000.0)
+        x[8192:] = (32 + first - below + 0.5) * eighth
+        rows.append(x)
+    x = torch.tensor(np.array(rows), dtype=torch.float32, device="cuda")
+    for p in (0.9, 0.9999, 1.0):
+        got = check(x, np.full(8, 0.99, np.float32), {"top_p": np.full(8, p, np.float32)})
+        assert p > 0.9 or got.tolist() == [0] * 8
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
 def test_rows_of_any_stride_and_alignment(dtype):
     r = np.random.default_rng(7)
