@@ -933,16 +933,49 @@ static __device__ __forceinline__ void lds_load(uint32_t to, uint32_t lane_at, c
 #pragma clang diagnostic pop
 }
 
+// As item_of, where no sequence is cut and there are at most NT: those with the longest histories first, so that no long item begins when the
+// others end (64 trees after 100 to 8000: 173 us, 203 in the order of the call; 32 of 30 to 60 tokens with heads of 256 175 and 212; equal lengths lose
+// nothing).  Each thread compares its sequence with all others, 0.5 us for 64.
+template <int NT>
+static __device__ Item longest_first(const Kv8Attend &a, const Cut &c, int idx, PlanLds &lds, uint2 *lengths, int tid)
+{
+    Span sp{};
+    Extent e{};
+    if (tid < a.s.B) sp = span_of(a.s, tid), e = extent_of(a, c, sp);
+    const int items = e.row_tiles * a.Hkv;
+    static_assert(NT <= 256, "a sequence's number in eight bits, the lowest first among equals");
+    const uint32_t own = (uint32_t)min(e.tiles, 0xffffff) << 8 | (255 - tid);
+    lengths[tid] = uint2{own, (uint32_t)items};
+    if (tid == 0) lds.found.found = false;
+    __syncthreads();
+    int first = 0;
+    if ((tid & ~63) < a.s.B)
+#pragma unroll 1
+        for (int i = 0; i < a.s.B; i += 16)  // (those behind the last have no items)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const uint2 other = lengths[i + k];
+                first += other.x > own ? (int)other.y : 0;
+            }
+    if (idx >= first && idx < first + items) {
+        const int local = idx - first, tile = local / a.Hkv;
+        lds.found = Item{true, sp, tid, e.row_tiles - 1 - tile, local - tile * a.Hkv, 1, e.lo, (int)min((int64_t)sp.len, (int64_t)e.lo + (int64_t)e.tiles * kTile), 0};
+    }
+    __syncthreads();
+    return lds.found;
+}
+
 // As attend_few, for drafted tokens, which have tens of rows a key head where single ones have a few: a tile's arithmetic counts as
 // much as its memory, and a wave by itself issues a vector instruction only every other time that its SIMD could.  So registers are
 // spared for a third wave a SIMD: the queries stand in LDS, and keys and values come through it (from memory straight into LDS, the next
 // group's on their way while this one's are multiplied), into the same registers one after the other.  32 heads of 128 on 8:
-// 64 sequences of 8 to 26 tokens after 100 to 8000 take 203 us, 237 by the kernels for single tokens and prompts; 60 tokens after 2000
-// in one 22 and 26.9; two of 64 after 100000 to 131000 294 to 303 and 288; 32 of 30 to 60 after 500 to 6000, 16 heads of 256 on 4, 212 and 338.
-// Of the 203, reading the cache (530 MB) is 108 at a large copy's rate; the vector instructions that expand and turn round the codes and take
-// the exponentials bound the rest.
+// 64 sequences of 8 to 26 tokens after 100 to 8000 take 173 us, 237 by the kernels for single tokens and prompts; 60 tokens after 2000
+// in one 22 and 26.9; two of 64 after 100000 to 131000 294 to 303 and 288; 32 of 30 to 60 after 500 to 6000, 16 heads of 256 on 4, 175 and 338.
+// Of the 173, reading the cache (530 MB) is 108 at a large copy's rate.  In the long one the vector instructions, which expand and turn round the codes and
+// take the exponentials, are 58 % of the time and the matrix pipes 37 %; reads of LDS are 14 % and their bank conflicts as much again, but an order without
+// those of keys and values takes no less time.
 template <int D, int RT>
-__global__ __launch_bounds__(kFewThreads, D <= 128 ? 3 : 2) void attend_tree(Kv8TreeAttend a, Cut c)
+__global__ __launch_bounds__(kFewThreads, D <= 128 ? 3 : 2) void attend_tree(Kv8TreeAttend a, Cut c, bool longest)
 {
     constexpr int KW = D / 16;  // dwords of a key row's quarter
     constexpr int VW = D / 64;  // dwords of a value row's sixteenth
@@ -957,7 +990,7 @@ __global__ __launch_bounds__(kFewThreads, D <= 128 ? 3 : 2) void attend_tree(Kv8
     __shared__ __attribute__((aligned(16))) unsigned char pool[kRing > kSums ? kRing : kSums];  // keys and values of each wave's group, then sums
     float(*const sums)[kRows][D + 4] = reinterpret_cast<float(*)[kRows][D + 4]>(pool);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g = lane >> 4;
-    const Item it = item_of<kFewThreads>(a, c, blockIdx.x, plan, tid);
+    const Item it = longest ? longest_first<kFewThreads>(a, c, blockIdx.x, plan, reinterpret_cast<uint2 *>(pool), tid) : item_of<kFewThreads>(a, c, blockIdx.x, plan, tid);
     if (!it.found) return;
     const int G = a.Hq / a.Hkv, rows = it.sp.n * G, row0 = it.tile * kRows;
     // (rows beyond the last are computed again and not stored)
@@ -1462,7 +1495,8 @@ static int launch_tree(const Kv8TreeAttend &a, hipStream_t s)
 {
     const Launch p = plan_tree(a);
     if (p.items > 0x7fffffff) return MQ_ERR_SHAPE;
-    auto go = [&](auto kernel) { return enqueue(kernel, dim3((unsigned)p.items), dim3(kFewThreads), 0, s, a, p.cut); };
+    const bool longest = !p.cut.split && a.s.B > 1 && a.s.B <= kFewThreads && p.items > tree_places(D);
+    auto go = [&](auto kernel) { return enqueue(kernel, dim3((unsigned)p.items), dim3(kFewThreads), 0, s, a, p.cut, longest); };
     const int rc = p.cut.rows == kFewRows ? go(attend_tree<D, 1>) : go(attend_tree<D, D <= 128 ? 2 : 1>);
     return rc || !p.cut.split ? rc : launch_join<D, true>(a, p.cut, s);
 }

@@ -77,6 +77,18 @@ def test_long_histories_are_cut_and_joined():
     Problem(9, [130, 140], [3000, 10], 8, 1, 256, 64).check("full")
 
 
+@pytest.mark.parametrize("D,window", [(64, 0), (128, 90), (256, 0)])
+def test_more_items_than_places_begin_with_the_longest(D, window):
+    r = np.random.default_rng(D)
+    for B, Hq, Hkv in ((256, 4, 4), (200, 8, 4), (2, 64, 8), (97, 8, 8)):
+        n = [int(x) for x in r.integers(0, 6, B)] if B > 2 else [130, 131]
+        past = [int(x) for x in r.integers(0, 300, B)] if B > 97 else [200] * B  # lengths of all kinds, and all alike
+        p = Problem(B, n, past, Hq, Hkv, D, 64, window)
+        p.lens[B // 2] = 0 if n[B // 2] > 5 else p.lens[B // 2]
+        p.check()
+        wide(p).check()
+
+
 def test_scores_that_grow_along_the_history():
     """The maximum is followed only where it is outgrown by 2^8: scores that rise by less, by more, and by much, and that fall."""
     for seed, by in enumerate((1.0, 30.0, 3000.0, -30.0)):
