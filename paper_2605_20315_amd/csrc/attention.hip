@@ -970,10 +970,10 @@ static __device__ Item longest_first(const Kv8Attend &a, const Cut &c, int idx, 
 // spared for a third wave a SIMD: the queries stand in LDS, and keys and values come through it (from memory straight into LDS, the next
 // group's on their way while this one's are multiplied), into the same registers one after the other.  32 heads of 128 on 8:
 // 64 sequences of 8 to 26 tokens after 100 to 8000 take 173 us, 237 by the kernels for single tokens and prompts; 60 tokens after 2000
-// in one 22 and 26.9; two of 64 after 100000 to 131000 294 to 303 and 288; 32 of 30 to 60 after 500 to 6000, 16 heads of 256 on 4, 175 and 338.
+// in one 22 and 26.9; two of 64 after 100000 to 131000 285 to 303 and 288; 32 of 30 to 60 after 500 to 6000, 16 heads of 256 on 4, 175 and 338.
 // Of the 173, reading the cache (530 MB) is 108 at a large copy's rate.  In the long one the vector instructions, which expand and turn round the codes and
-// take the exponentials, are 58 % of the time and the matrix pipes 37 %; reads of LDS are 14 % and their bank conflicts as much again, but an order without
-// those of keys and values takes no less time.
+// take the exponentials, are 58 % of the time and the matrix pipes 37 %; LDS is busy 37 %, nearly half of it by bank conflicts, but an order without those of
+// keys and values takes no less time.
 template <int D, int RT>
 __global__ __launch_bounds__(kFewThreads, D <= 128 ? 3 : 2) void attend_tree(Kv8TreeAttend a, Cut c, bool longest)
 {
