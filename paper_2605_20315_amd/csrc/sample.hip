@@ -168,8 +168,8 @@ static __device__ __forceinline__ uint32_t lowest(const Setting &s, float top, d
     if (top == __builtin_inff()) return 0xff800000u;
     if (s.scale == 0.0) return 0x00800000u;
     const float y = (float)fmin(fmax(limit * s.inverse, -3.4028234663852886e38), 3.4028234663852886e38);
-    const uint32_t key = key_of(y) - 2;
-    return max(key + __popcll(__ballot((double)value_of(key + (threadIdx.x & 3)) * s.scale < limit) & 15), 0x00800000u);
+    const uint32_t key = max(key_of(y) - 2, 0x00800000u);  // (what is in front of it is no number)
+    return key + __popcll(__ballot((double)value_of(key + (threadIdx.x & 3)) * s.scale < limit) & 15);
 }
 
 typedef uint32_t words2 __attribute__((ext_vector_type(4), aligned(2)));

@@ -138,6 +138,32 @@ def test_wide_ranges_of_logits():
         check(x, r.random(8).astype(np.float32), {"temperature": np.full(8, t, np.float32), "top_k": np.full(8, 900, np.int32), "top_p": np.full(8, 0.9, np.float32)})
 
 
+def test_the_lowest_logits_at_the_border_of_a_bin():
+    """Temperatures with which the lowest finite number lies just below a whole number of eighths of a power of two, and the next just above:
+    the first belongs to another bin than the second, which is the last that is kept."""
+    low = np.float32(np.finfo(np.float32).min)
+    following = np.nextafter(low, np.float32(0))
+    cases = []
+    for n in range(-3000, -600, 37):
+        t = np.float32(8 * np.log2(np.e) / (n / float(following)))
+        for t in (t, np.nextafter(t, np.float32(0)), np.nextafter(t, np.float32(np.inf))):
+            scale = 8.0 * 1.4426950408889634074 / float(t)
+            if np.floor(float(low) * scale) == n - 1 and np.floor(float(following) * scale) == n:
+                cases.append((t, n, scale))
+    assert len(cases) > 20
+    x = np.full((len(cases), 300), -np.inf, np.float32)
+    for row, (_, n, scale) in zip(x, cases):
+        row[7], row[10:13], row[20:25] = (n + 2.5) / scale, following, low
+    have = {"temperature": np.array([t for t, _, _ in cases], np.float32), "top_k": np.full(len(cases), 4, np.int32)}
+    got = check(torch.from_numpy(x).cuda(), np.full(len(cases), 0.99, np.float32), have)
+    assert set(got.tolist()) == {12}
+    # and 511 bins below the largest, the last that is counted
+    for row, (_, n, scale) in zip(x, cases):
+        row[7] = (n + 511.5) / scale
+    got = check(torch.from_numpy(x).cuda(), np.full(len(cases), 0.99, np.float32), {"temperature": have["temperature"], "top_p": np.full(len(cases), 0.9, np.float32)})
+    assert set(got.tolist()) == {7}
+
+
 @pytest.mark.parametrize("below", [448, 503, 504, 505, 510, 511, 512, 520])
 def test_parts_of_a_row_that_lie_far_below_its_largest(below):
     """A part of 8192 logits so many eighths of a power of two below the largest: its mass, next to nothing, is not to move the border of top_p."""
