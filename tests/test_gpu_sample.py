@@ -138,6 +138,21 @@ def test_wide_ranges_of_logits():
         check(x, r.random(8).astype(np.float32), {"temperature": np.full(8, t, np.float32), "top_k": np.full(8, 900, np.int32), "top_p": np.full(8, 0.9, np.float32)})
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_signalling_nans_are_nans(dtype):
+    r = np.random.default_rng(12)
+    x = logits_of(r, 12, 20001, dtype)
+    small = torch.int16 if dtype == torch.bfloat16 else torch.int32
+    codes = [0x7F81, 0x7FA3 - 0x10000 + 0x8000, 0x7FC1] if dtype == torch.bfloat16 else [0x7F800001, 0x7FA00000 - 2 ** 31, 0x7FC00001]
+    at = torch.from_numpy(r.random((12, 20001)) < 0.3).cuda()
+    at[:, 8192:16384] = True  # a part that holds nothing else
+    x.view(small)[at] = torch.tensor(codes, dtype=small, device="cuda")[torch.arange(int(at.sum()), device="cuda") % 3]
+    have = settings(r, 12)
+    check(x, r.random(12).astype(np.float32), {})
+    check(x, r.random(12).astype(np.float32), have)
+    check(x, r.random(12).astype(np.float32), {"temperature": np.zeros(12, np.float32)})
+
+
 def test_the_lowest_logits_at_the_border_of_a_bin():
     """Temperatures with which the lowest finite number lies just below a whole number of eighths of a power of two, and the next just above:
     the first belongs to another bin than the second, which is the last that is kept."""
