@@ -275,6 +275,20 @@ static __device__ __forceinline__ int wave_min(int v) { return lane_of(wave_scan
 template <class T>
 static __device__ __forceinline__ T sum_to(T v) { return wave_scan(v, T(0), [](T x, T y) { return x + y; }); }
 
+// One more token, and what its weight falls short of one
+static __device__ __forceinline__ void count_in_bin(float y, float top, double scale, double edge, u64 *bins)
+{
+    const double pos = pos_of(y, top, scale), q = floor(pos);
+    // 2^52 more than the shortfall, whose bits are then the low ones
+    const double d = __builtin_fma(in_bin(pos - q), -kFine, kFine + 0x1p52);
+    atomicAdd(&bins[(int)(edge - q)], (1ull << kCountBit) + (__builtin_bit_cast(u64, d) - 0x4330000000000000ull));
+}
+// the mass of bin b over that of the first bin's top
+static __device__ __forceinline__ double mass_in_bin(u64 bin, int b)
+{
+    return ((double)((bin >> kCountBit) << 34) - (double)(bin & ((1ull << kCountBit) - 1))) * (1.0 / kFine) * eighth(b);
+}
+
 // One chunk of kChunk logits.  They stay in LDS, so that the loop over them is no longer than its body: unrolled, the
 // code alone (12 KB read once by each compute unit) takes longer than the logits.
 template <class T>
@@ -393,10 +407,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
         for (int i = 0; i < N; ++i) {
             const float y = bits_of<T>(x, i);
             if (y >= least) {  // (not for NaN and -infinity)
-                const double pos = pos_of(y, top, s.scale), q = floor(pos);
-                // 2^52 more than the shortfall, whose bits are then the low ones
-                const double d = __builtin_fma(in_bin(pos - q), -kFine, kFine + 0x1p52);
-                atomicAdd(&bins[(int)(edge - q)], (1ull << kCountBit) + (__builtin_bit_cast(u64, d) - 0x4330000000000000ull));
+                count_in_bin(y, top, s.scale, edge, bins);
             }
         }
     }
@@ -408,7 +419,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunks(Sample a, Tables 
     for (int i = 0; i < 2; ++i) {
         const u64 bin = bins[2 * tid + i];
         count[i] = (int)(bin >> kCountBit);
-        mass[i] = ((double)((u64)count[i] << 34) - (double)(bin & ((1ull << kCountBit) - 1))) * (1.0 / kFine) * eighth(2 * tid + i);
+        mass[i] = mass_in_bin(bin, 2 * tid + i);
     }
     int n = sum_to(count[0] + count[1]);
     double m = sum_to(mass[0] + mass[1]);
@@ -474,6 +485,46 @@ static __device__ __forceinline__ Borders borders_of(const Setting &s, double pe
     return b;
 }
 
+// The bins that a border is in (-1: none), the first and the last of them
+struct Wanted {
+    int k, m, p0, p1, from, to;
+    __device__ __forceinline__ bool has(int bin) const { return bin == k || bin == m || (bin >= p0 && bin <= p1); }
+};
+static __device__ __forceinline__ Wanted wanted_of(const Setting &s, const Borders &b)
+{
+    Wanted w;
+    w.k = b.k < kBins && b.part_k && (s.p < 1.0f || b.k <= b.m) ? b.k : -1;
+    w.m = b.m < kBins && b.m <= b.k && b.m <= b.p1 ? b.m : -1;
+    w.p0 = b.p0, w.p1 = min(min(b.p1, b.m), kBins - 1);
+    const bool p = w.p0 <= w.p1;
+    w.from = min(min(w.k >= 0 ? w.k : kBins, w.m >= 0 ? w.m : kBins), p ? w.p0 : kBins);
+    w.to = max(max(w.k, w.m), p ? w.p1 : -1);
+    return w;
+}
+
+// Tokens into a list of numbers.  The logits between the first bin that is wanted and the last, `least` to `most`, are few as a rule: two
+// comparisons in 32 bits find them (-0 may count as in front of 0 there), and what has bins is asked of them alone.
+template <class T>
+static __device__ __forceinline__ void list_wanted(u32x4 x, int i0, float least, float most, const Setting &s, float top, double edge, const Wanted &w, u64 *list, int *listed)
+{
+    constexpr int N = 16 / sizeof(T);
+    uint32_t some = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float y = bits_of<T>(x, i);
+        some |= (uint32_t)(y >= least && y <= most) << i;
+    }
+#pragma unroll 1
+    for (; some; some &= some - 1) {
+        const int i = __builtin_ctz(some);
+        const float y = pick<T>(x, i);
+        if (w.has((int)(edge - floor(pos_of(y, top, s.scale))))) {
+            const int slot = atomicAdd(listed, 1);
+            if (slot < kList) list[slot] = number_of<T>(key_of(y), i0 + i);
+        }
+    }
+}
+
 // A row's counts and masses up to each bin, and the tokens of the bins that a border is in, a part of the row's chunks by each
 // workgroup: as many in all as there are compute units, since each adds up all chunks' sums first (64 rows in 256 workgroups 13 us, in 512
 // 15.5; the additions as integers, which 64-bit ones of floating numbers took 1.2 us more for).
@@ -530,44 +581,20 @@ __global__ __launch_bounds__(kBorderThreads) void sample_border(Sample a, Tables
     static_assert(NT == 2 * kBins, "two halves");
     const Borders b = borders_of(s, peak, edge, min_bits, masses, counts, lane);
     if (part == 0 && tid == 0) out.borders = b;
-    // The bins that a border is in.  The logits between the first of them and the last are few as a rule: two comparisons in 32 bits find them (
-    // -0 may count as in front of 0 there), and what has bins is asked of them alone.
-    const bool need_k = b.k < kBins && b.part_k && (s.p < 1.0f || b.k <= b.m), need_m = b.m < kBins && b.m <= b.k && b.m <= b.p1;
-    const int p1 = min(min(b.p1, b.m), kBins - 1);
-    const bool need_p = b.p0 <= p1;
-    const int from = min(min(need_k ? b.k : kBins, need_m ? b.m : kBins), need_p ? b.p0 : kBins);
-    const int to = max(max(need_k ? b.k : -1, need_m ? b.m : -1), need_p ? p1 : -1);
-    if (to < 0) return;
-    const float least = value_of(lowest(s, top, edge - to)), most = from > 0 ? value_of(lowest(s, top, edge - from + 1) - 1) : kInf;
+    const Wanted w = wanted_of(s, b);
+    if (w.to < 0) return;
+    const float least = value_of(lowest(s, top, edge - w.to)), most = w.from > 0 ? value_of(lowest(s, top, edge - w.from + 1) - 1) : kInf;
     const T *const row = reinterpret_cast<const T *>(a.logits) + r * a.ld;
     const int first = (int)((int64_t)chunks * part / parts) * kChunk, end = min(V, (int)((int64_t)chunks * (part + 1) / parts) * kChunk);
 #pragma unroll 1
-    for (int i0 = first + tid * N; i0 < end; i0 += NT * N) {
-        const u32x4 x = load16(row, i0, V);
-        uint32_t some = 0;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float y = bits_of<T>(x, i);
-            some |= (uint32_t)(y >= least && y <= most) << i;
-        }
-#pragma unroll 1
-        for (; some; some &= some - 1) {
-            const int i = __builtin_ctz(some);
-            const float y = pick<T>(x, i);
-            const int bin = (int)(edge - floor(pos_of(y, top, s.scale)));
-            if ((need_k && bin == b.k) || (need_m && bin == b.m) || (bin >= b.p0 && bin <= p1)) {
-                const int slot = atomicAdd(&listed, 1);
-                if (slot < kList) list[slot] = number_of<T>(key_of(y), i0 + i);
-            }
-        }
-    }
+    for (int i0 = first + tid * N; i0 < end; i0 += NT * N) list_wanted<T>(load16(row, i0, V), i0, least, most, s, top, edge, w, list, &listed);
     __syncthreads();
     if (tid == 0) at = listed > 0 ? atomicAdd(&out.listed, listed) : 0;
     __syncthreads();
     for (int i = tid; i < min(listed, kList - at); i += NT) out.list[at + i] = list[i];
 }
 
-template <bool F>
+template <bool F, bool ONE>
 struct RowLds {
     float tops[kChunksMost];
     int shift[kChunksMost];  // bins between the row's largest logit and the chunk's; kBins: its weights are none
@@ -587,17 +614,23 @@ struct RowLds {
     double powers[32];
     int chosen;
     double rest;
+    u64 bins[F && ONE ? kBins : 1];
+    float wave_tops[kRowThreads / 64];
+    int wave_counts[kRowThreads / 64];
+    double wave_masses[kRowThreads / 64];
 };
 
 // One row by one workgroup.  What takes it is one trip to memory after another, and its own code, which each compute unit reads
 // once, from memory: so everything that looks at tokens stands here once, in loops.  512 threads, since much of it is done by every wave alike and four
 // waves a SIMD wait for each other there (a pass over a border's tokens 1.2 us, 1.7 with 1024).  F: rows may have filters.
-template <class T, bool F>
+// ONE: rows of one chunk, of which it does all in one launch (sample_chunks' counts and sample_border's tokens included): 7
+// rows of 1529 with all filters 15.0 us, 25.6 by three kernels; 500 of 8000 24.4 and 36.5; one without filters 5.9 and 11.3.
+template <class T, bool F, bool ONE>
 __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, int64_t row0, int chunks)
 {
     constexpr int NT = kRowThreads, N = 16 / sizeof(T);
     constexpr float kInf = __builtin_inff();
-    __shared__ RowLds<F> l;
+    __shared__ RowLds<F, ONE> l;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = (int)a.V;
     const int64_t r = row0 + blockIdx.x;
     const T *const row = reinterpret_cast<const T *>(a.logits) + r * a.ld;
@@ -605,42 +638,123 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     const Upto *const upto = t.upto + (int64_t)blockIdx.x * chunks * kBins;
     const Row &known = t.rows[blockIdx.x];
     const Setting s = setting_of(a, r);
-    Chunk own{-kInf, 0, 0.0};
-    if (tid < chunks) own = parts[tid], l.tops[tid] = own.top;
-    if (tid < 32) l.powers[tid] = power(0.03125 * tid);
+    constexpr int kEach = kChunk / NT, kVectors = kEach / N;  // logits of a chunk side by side to a thread
     const bool filters = F && s.filters && !s.largest;
-    [[maybe_unused]] const int listed = filters ? known.listed : 0;
-    Borders known_to{};
-    if (F && filters) known_to = known.borders;
-    if (F && filters) {
-        if (tid < kBins) l.masses[tid] = known.masses[tid], l.counts[tid] = known.counts[tid];
+    [[maybe_unused]] int listed = 0;
+    [[maybe_unused]] Borders known_to{};
+    u32x4 x[kVectors];
+    // the next of them: the first, which goes to the end (registers have no numbers that a loop could go by)
+    auto next_vector = [&] {
+        const u32x4 v = x[0];
 #pragma unroll
-        for (int i = 0; i < kList / NT; ++i)
-            if (i * NT + tid < listed) l.list[i * NT + tid] = known.list[i * NT + tid];
-    }
-    __syncthreads();
+        for (int q = 1; q < kVectors; ++q) x[q - 1] = x[q];
+        return x[kVectors - 1] = v;
+    };
     float top = -kInf;
-    for (int c = lane; c < chunks; c += 64) top = fmaxf(top, l.tops[c]);
-    top = wave_max(top);
-    if (s.largest || top == -kInf) {
-        if (wave == 0) {
-            int first = 0x7fffffff;
-            for (int c = lane; c < chunks; c += 64)
-                if (l.tops[c] == top) first = min(first, parts[c].first);
-            first = wave_min(first);
-            if (lane == 0) a.tokens[r] = top == -kInf ? -1 : first;
+    double peak, edge;
+    if (tid < 32) l.powers[tid] = power(0.03125 * tid);
+    if constexpr (ONE) {
+        constexpr int NW = NT / 64;
+        static_assert(NT == kBins, "a bin a thread");
+#pragma unroll
+        for (int j = 0; j < kVectors; ++j) x[j] = load16(row, min(tid * kEach + j * N, V), V);
+#pragma unroll
+        for (int j = 0; j < kVectors; ++j)
+#pragma unroll
+            for (int i = 0; i < N; i += 2) top = fmaxf(top, fmaxf(bits_of<T>(x[j], i), bits_of<T>(x[j], i + 1)));
+        const float mine = top;
+        top = wave_max(top);
+        if (lane == 0) l.wave_tops[wave] = top;
+        if (F) l.bins[tid] = 0;
+        if (tid == 0) l.listed = 0;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w) top = fmaxf(top, l.wave_tops[w]);
+        if (s.largest || top == -kInf) {
+            // (threads and waves have their logits in the order of the row)
+            const u64 hits = __ballot(mine == top);
+            if (lane == 0) l.wave_counts[wave] = hits ? __ffsll(hits) - 1 : -1;
+            __syncthreads();
+            int from = 0;
+            while (from < NW - 1 && l.wave_counts[from] < 0) ++from;
+            if (wave == from && lane == l.wave_counts[from]) {
+                int first = 0;
+#pragma unroll
+                for (int j = kVectors - 1; j >= 0; --j)
+#pragma unroll
+                    for (int i = N - 1; i >= 0; --i)
+                        if (bits_of<T>(x[j], i) == top) first = tid * kEach + j * N + i;
+                a.tokens[r] = top == -kInf ? -1 : first;
+            }
+            return;
         }
-        return;
+        peak = pos_of(top, top, s.scale), edge = floor(peak);
+        if constexpr (F) if (filters) {
+            {
+                const float least = value_of(lowest(s, top, edge - (kBins - 1)));
+#pragma unroll 1
+                for (int j = 0; j < kVectors; ++j) {
+                    const u32x4 v = next_vector();
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        if (bits_of<T>(v, i) >= least) count_in_bin(bits_of<T>(v, i), top, s.scale, edge, l.bins);
+                }
+            }
+            __syncthreads();
+            const u64 bin = l.bins[tid];
+            int n = sum_to((int)(bin >> kCountBit));
+            double m = sum_to(mass_in_bin(bin, tid));
+            if (lane == 63) l.wave_counts[wave] = n, l.wave_masses[wave] = m;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+                if (w < wave) n += l.wave_counts[w], m += l.wave_masses[w];
+            l.counts[tid] = n, l.masses[tid] = m;
+            __syncthreads();
+            known_to = borders_of(s, peak, edge, s.min_p > 0.0f ? 8.0 * log2((double)s.min_p) : 0.0, l.masses, l.counts, lane);
+            const Wanted w = wanted_of(s, known_to);
+            if (w.to >= 0) {
+                const float least = value_of(lowest(s, top, edge - w.to)), most = w.from > 0 ? value_of(lowest(s, top, edge - w.from + 1) - 1) : kInf;
+#pragma unroll 1
+                for (int j = 0; j < kVectors; ++j) list_wanted<T>(next_vector(), tid * kEach + j * N, least, most, s, top, edge, w, l.list, &l.listed);
+            }
+            __syncthreads();
+            listed = l.listed;
+            __syncthreads();
+        }
+    } else {
+        Chunk own{-kInf, 0, 0.0};
+        if (tid < chunks) own = parts[tid], l.tops[tid] = own.top;
+        if (F && filters) {
+            listed = known.listed, known_to = known.borders;
+            if (tid < kBins) l.masses[tid] = known.masses[tid], l.counts[tid] = known.counts[tid];
+#pragma unroll
+            for (int i = 0; i < kList / NT; ++i)
+                if (i * NT + tid < listed) l.list[i * NT + tid] = known.list[i * NT + tid];
+        }
+        __syncthreads();
+        for (int c = lane; c < chunks; c += 64) top = fmaxf(top, l.tops[c]);
+        top = wave_max(top);
+        if (s.largest || top == -kInf) {
+            if (wave == 0) {
+                int first = 0x7fffffff;
+                for (int c = lane; c < chunks; c += 64)
+                    if (l.tops[c] == top) first = min(first, parts[c].first);
+                first = wave_min(first);
+                if (lane == 0) a.tokens[r] = top == -kInf ? -1 : first;
+            }
+            return;
+        }
+        peak = pos_of(top, top, s.scale), edge = floor(peak);
+        if (tid < chunks) {
+            const double below = own.top == top ? 0.0 : !weighs(own.top, top) ? kBins : fmin(edge - floor(own.top * s.scale), (double)kBins);
+            l.shift[tid] = (int)below;
+            l.scale[tid] = below < kBins ? eighth((int)below) : 0.0;
+            l.kept[tid] = own.mass * l.scale[tid];
+            l.part[tid] = 0;
+        }
+        __syncthreads();
     }
-    const double peak = pos_of(top, top, s.scale), edge = floor(peak);
-    if (tid < chunks) {
-        const double below = own.top == top ? 0.0 : !weighs(own.top, top) ? kBins : fmin(edge - floor(own.top * s.scale), (double)kBins);
-        l.shift[tid] = (int)below;
-        l.scale[tid] = below < kBins ? eighth((int)below) : 0.0;
-        l.kept[tid] = own.mass * l.scale[tid];
-        l.part[tid] = 0;
-    }
-    __syncthreads();
 
     auto value_of_number = [](u64 number) {
         const uint32_t key = (uint32_t)(number >> 20);
@@ -700,6 +814,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
                 }
             }
             if (task == kNew + kRest) {
+                if (ONE) break;
                 task = kRest;
                 const int b = min(min(bin_k, bin_p), bin_m);
                 if (b == kBins) break;
@@ -806,7 +921,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
             task = kNew + task + 1;
         }
         const int border = min(min(bin_k, bin_p), bin_m);
-        if (border < kBins && tid < chunks) {
+        if (!ONE && border < kBins && tid < chunks) {
             const int b = border - l.shift[tid] + whole;
             const double m = b > 0 && l.shift[tid] < kBins ? (double)mass_of(upto[tid * kBins + b - 1]) * (1.0 / kUptoUnit) * eighth(-bins_to_octave(edge - l.shift[tid])) : 0.0;
             l.kept[tid] = m * l.scale[tid] + (double)l.part[tid] * 0x1p-40 * eighth(border);
@@ -815,7 +930,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     }
 
     // the chunk that the draw falls into: sums over two chunks a lane
-    if (wave == 0) {
+    if (!ONE && wave == 0) {
         static_assert(kChunksMost == 128, "two a lane");
         const double m0 = 2 * lane < chunks ? l.kept[2 * lane] : 0.0, m1 = 2 * lane + 1 < chunks ? l.kept[2 * lane + 1] : 0.0, sum = m0 + m1;
         const double front = sum_to(sum), total = lane_of(front, 63), u = (double)a.uniform[r];
@@ -828,16 +943,16 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
             l.rest = aim - (second ? before + m0 : before);
         }
     }
-    __syncthreads();
+    if (!ONE) __syncthreads();
 
     // The token in it, sixteen side by side to a thread: weights in whole 2^-43 of the top of the chunk's first bin, so that all sums
     // agree (what is kept of a chunk has its largest logit in it).
-    constexpr int kEach = kChunk / NT, kVectors = kEach / N;
-    const int chosen = l.chosen, first = chosen * kChunk + tid * kEach;
-    u32x4 x[kVectors];
+    const int chosen = ONE ? 0 : l.chosen, first = chosen * kChunk + tid * kEach;
+    if constexpr (!ONE) {
 #pragma unroll
-    for (int j = 0; j < kVectors; ++j) x[j] = load16(row, min(first + j * N, V), V);
-    const double from = (floor(pos_of(l.tops[chosen], top, s.scale)) + 1.0) * -4.0;
+        for (int j = 0; j < kVectors; ++j) x[j] = load16(row, min(first + j * N, V), V);
+    }
+    const double chosen_edge = ONE ? edge : floor(pos_of(l.tops[chosen], top, s.scale)), from = (chosen_edge + 1.0) * -4.0;
     u64 before = 0, aim = 0;
     bool mine = false;
 #pragma unroll 1
@@ -846,9 +961,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
         int token = -1;
 #pragma unroll 1
         for (int j = 0; j < kVectors; ++j) {
-            u32x4 v = x[0];
-#pragma unroll
-            for (int q = 1; q < kVectors; ++q) v = j == q ? x[q] : v;
+            const u32x4 v = next_vector();
             uint32_t kept = 0;  // a bit each
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -879,7 +992,15 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
             if (w < wave) before += f;
             total += f;
         }
-        const double rest = l.rest / l.scale[chosen] * 0x1p43;
+        double rest;
+        if constexpr (ONE) {
+            const double u = (double)a.uniform[r];
+            rest = u > 0.0 ? fmin(u, 1.0 - 0x1p-40) * (double)total : 0.0;
+        } else {
+            rest = l.rest / l.scale[chosen] * 0x1p43;
+            // (the weights here are those of the bins but where a pos of 2^53 and more leaves the one of its bin's top no bit)
+            if (filters) rest *= eighth((int)(chosen_edge + 1.0 - chosen_edge) - 1);
+        }
         aim = min(rest > 0.0 ? (u64)fmin(rest, 0x1p62) : 0ull, total - 1);
         mine = sum > 0 && before <= aim && aim < before + sum;
         if (!__any(mine)) break;
@@ -897,7 +1018,7 @@ static int64_t plain_rows_of(int64_t rows, int64_t chunks) { return std::min(row
 int64_t sample_workspace(int64_t rows, int64_t V)
 {
     const int64_t chunks = chunks_of(V);
-    return rows_of(rows, chunks) * row_bytes(chunks);
+    return chunks == 1 ? 0 : rows_of(rows, chunks) * row_bytes(chunks);
 }
 
 template <class T>
@@ -908,6 +1029,10 @@ static int sample_typed(const Sample &a, hipStream_t s)
     Chunk *const first = static_cast<Chunk *>(a.ws);
     Upto *const upto = reinterpret_cast<Upto *>(first + most * chunks);
     const Tables t{first, upto, reinterpret_cast<Row *>(upto + most * chunks * kBins)};
+    if (chunks == 1) {
+        auto go = [&](auto kernel) { return enqueue(kernel, dim3((unsigned)a.rows), dim3(kRowThreads), 0, s, a, t, (int64_t)0, 1); };
+        return filters ? go(sample_rows<T, true, true>) : go(sample_rows<T, false, true>);
+    }
     for (int64_t r = 0; r < a.rows; r += most) {
         const int64_t n = std::min(most, a.rows - r);
         auto go = [&](auto kernel, int64_t groups, int threads, auto... more) {
@@ -918,7 +1043,7 @@ static int sample_typed(const Sample &a, hipStream_t s)
             const int64_t parts = std::min(chunks, std::max<int64_t>(256 / n, 1));
             if (int rc = go(sample_border<T>, n * parts, kBorderThreads, (int)parts)) return rc;
         }
-        if (int rc = filters ? go(sample_rows<T, true>, n, kRowThreads) : go(sample_rows<T, false>, n, kRowThreads)) return rc;
+        if (int rc = filters ? go(sample_rows<T, true, false>, n, kRowThreads) : go(sample_rows<T, false, false>, n, kRowThreads)) return rc;
     }
     return MQ_OK;
 }

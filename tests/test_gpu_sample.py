@@ -139,6 +139,25 @@ def test_wide_ranges_of_logits():
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("V", [17, 4097, 8192, 8193, 16384])
+def test_rows_about_one_workgroups_size(V, dtype):
+    """Rows of at most 8192 logits take one launch, longer ones three."""
+    r = np.random.default_rng(V)
+    for kind in ("mixed", "steps", "equal", "flat"):
+        x = logits_of(r, 24, V, dtype, kind)
+        x[1] = float("-inf")
+        x[2] = float("nan")
+        x[3, : V // 2] = float("nan")
+        x[4, V // 3] = x[4, V - 1] = float("inf")
+        x[5, 1:] = float("-inf")
+        x[6, : V - 1] = float("-inf")
+        x[7] = torch.finfo(dtype).min
+        for have in ({}, settings(r, 24), {"top_p": np.full(24, 0.9, np.float32)}, {"top_k": np.full(24, 300, np.int32)},
+                     {"min_p": np.full(24, 0.05, np.float32)}, {"temperature": np.zeros(24, np.float32)}):
+            check(x, r.random(24).astype(np.float32), have)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
 def test_signalling_nans_are_nans(dtype):
     r = np.random.default_rng(12)
     x = logits_of(r, 12, 20001, dtype)
