@@ -12,7 +12,7 @@
 // Three kernels.  sample_chunks reads the logits once, a chunk of a row by a workgroup: the largest, the mass, and where the row has
 // filters the count and mass up to each of the 512 bins below the chunk's largest (weights down to 2^-64).  sample_border, several workgroups a row:
 // the row's own sums from those, the bins that the borders are in, and their tokens.  sample_rows, a workgroup a row: the borders among those
-// tokens, the chunk that the draw falls into, the token.  Without filters the first and the last are all.
+// tokens, the chunk that the draw falls into, the token.  Without filters the first and the last are all; a row of one chunk needs only the last.
 // 64 rows of 151673 with all filters, BF16: 47 to 48 us (16, 13 and 17 and what lies between); a large copy would read them in 4.  Counting in 64 bits bounds
 // the first (22 vector instructions and an addition in LDS a logit), trips to memory and to a barrier one after another the others, as they do
 // all of one row's 23 us.  500 rows of 100003 in FP32 by temperature alone: 56 to 70 us, 41 by a large copy; reading takes as long as the 20
@@ -634,9 +634,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = (int)a.V;
     const int64_t r = row0 + blockIdx.x;
     const T *const row = reinterpret_cast<const T *>(a.logits) + r * a.ld;
-    const Chunk *const parts = t.chunks + (int64_t)blockIdx.x * chunks;
-    const Upto *const upto = t.upto + (int64_t)blockIdx.x * chunks * kBins;
-    const Row &known = t.rows[blockIdx.x];
+    [[maybe_unused]] const Chunk *const parts = t.chunks + (int64_t)blockIdx.x * chunks;
+    [[maybe_unused]] const Upto *const upto = t.upto + (int64_t)blockIdx.x * chunks * kBins;
+    [[maybe_unused]] const Row &known = t.rows[blockIdx.x];
     const Setting s = setting_of(a, r);
     constexpr int kEach = kChunk / NT, kVectors = kEach / N;  // logits of a chunk side by side to a thread
     const bool filters = F && s.filters && !s.largest;
@@ -1025,14 +1025,15 @@ template <class T>
 static int sample_typed(const Sample &a, hipStream_t s)
 {
     const bool filters = a.top_k || a.top_p || a.min_p;
-    const int64_t chunks = chunks_of(a.V), most = filters ? rows_of(a.rows, chunks) : plain_rows_of(a.rows, chunks);
+    const int64_t chunks = chunks_of(a.V);
+    if (chunks == 1) {  // (no workspace)
+        auto go = [&](auto kernel) { return enqueue(kernel, dim3((unsigned)a.rows), dim3(kRowThreads), 0, s, a, Tables{}, (int64_t)0, 1); };
+        return filters ? go(sample_rows<T, true, true>) : go(sample_rows<T, false, true>);
+    }
+    const int64_t most = filters ? rows_of(a.rows, chunks) : plain_rows_of(a.rows, chunks);
     Chunk *const first = static_cast<Chunk *>(a.ws);
     Upto *const upto = reinterpret_cast<Upto *>(first + most * chunks);
     const Tables t{first, upto, reinterpret_cast<Row *>(upto + most * chunks * kBins)};
-    if (chunks == 1) {
-        auto go = [&](auto kernel) { return enqueue(kernel, dim3((unsigned)a.rows), dim3(kRowThreads), 0, s, a, t, (int64_t)0, 1); };
-        return filters ? go(sample_rows<T, true, true>) : go(sample_rows<T, false, true>);
-    }
     for (int64_t r = 0; r < a.rows; r += most) {
         const int64_t n = std::min(most, a.rows - r);
         auto go = [&](auto kernel, int64_t groups, int threads, auto... more) {
