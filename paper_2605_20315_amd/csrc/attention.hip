@@ -1464,8 +1464,10 @@ static int plan_attention(const Kv8Attend &a, Launch *out)
 // Drafted tokens.  All of a call's sequences go to one kernel: they have about as many tokens each, and a second kernel that finds
 // nothing to do costs 14 us.  Two tiles of rows from one expansion where there is enough work that arithmetic bounds it (32 heads of
 // 128 on 8: two sequences of 64 tokens after 100000 to 131000 294 us, 406 with one tile; 64 of 16 after 4000 134 and 165), not where the latency of an
-// item does (4 of 60 after 500 to 1000: 29.6, 21.3 with one; one of 60 after 2000 28 and 23.4; 8 of 30 to 60 after 1000 to 4000 50 and 47).
+// item does (4 of 60 after 500 to 1000, cut: 29.6, 21.3 with one; one of 60 after 2000 28 and 23.4; 8 of 30 to 60 after 1000 to 4000 50 and 47).
 // Few items of two tiles are cut into as many as the GPU holds at a time, others into 512: what comes after a first round then is short.
+// Chunks of 8 tiles at least and histories of three of them, since a join costs 6 us (30 tokens after 300 in one sequence 11.5 us, 17.7 with chunks of two
+// tiles; 5 of 60 to 120 after 100 to 900, heads of 256, 27.7 and 41.3; longer histories the same; with chunks of 12 16 tokens after 8000 21.8 and 20.7).
 static Launch plan_tree(const Kv8TreeAttend &a)
 {
     const int D = a.D;
@@ -1473,10 +1475,10 @@ static Launch plan_tree(const Kv8TreeAttend &a)
     const bool ws = a.ws && a.ws_bytes >= kWorkspace && B <= kPartsMost;
     const bool two = D <= 128 && T * G > B * kFewRows && T * G * a.Hkv * places > kTreeRowPlaces;
     const int rows = two ? 2 * kFewRows : kFewRows;
-    Launch p{false, Cut{rows, 0, 2, 0, INT32_MAX, true, false, a.ws, slots_of(rows, D), 0}, 0};
+    Launch p{false, Cut{rows, 0, 8, 0, INT32_MAX, true, false, a.ws, slots_of(rows, D), 0}, 0};
     const int64_t whole = row_tiles_most(p.cut, T, B, G) * a.Hkv, tiles = places / kTile + 1;
     p.cut.target = target_of(two && whole <= 256 ? tree_places(D) : 512, rows, D);
-    p.cut.split = ws && whole < 2 * p.cut.target && tiles >= 2 * p.cut.least;
+    p.cut.split = ws && whole < 2 * p.cut.target && tiles >= 3 * p.cut.least;
     p.items = p.cut.split ? std::min(whole + 2 * p.cut.target, whole * (tiles / p.cut.least + 1)) : whole;
     return p;
 }
