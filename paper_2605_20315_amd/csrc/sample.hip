@@ -13,9 +13,9 @@
 // filters the count and mass up to each of the 512 bins below the chunk's largest (weights down to 2^-64).  sample_border, several workgroups a row:
 // the row's own sums from those, the bins that the borders are in, and their tokens.  sample_rows, a workgroup a row: the borders among those
 // tokens, the chunk that the draw falls into, the token.  Without filters the first and the last are all; a row of one chunk needs only the last.
-// 64 rows of 151673 with all filters, BF16: 47 to 48 us (16, 13 and 17 and what lies between); a large copy would read them in 4.  Counting in 64 bits bounds
+// 64 rows of 151673 with all filters, BF16: 46 us (16, 13 and 15 and what lies between); a large copy would read them in 4.  Counting in 64 bits bounds
 // the first (22 vector instructions and an addition in LDS a logit), trips to memory and to a barrier one after another the others, as they do
-// all of one row's 23 us.  500 rows of 100003 in FP32 by temperature alone: 56 to 70 us, 41 by a large copy; reading takes as long as the 20
+// all of one row's 22 us.  500 rows of 100003 in FP32 by temperature alone: 56 to 70 us, 41 by a large copy; reading takes as long as the 20
 // instructions of each weight's power of two, and the two overlap in part.
 #include "kv8.h"
 
@@ -623,8 +623,9 @@ struct RowLds {
 // One row by one workgroup.  What takes it is one trip to memory after another, and its own code, which each compute unit reads
 // once, from memory: so everything that looks at tokens stands here once, in loops.  512 threads, since much of it is done by every wave alike and four
 // waves a SIMD wait for each other there (a pass over a border's tokens 1.2 us, 1.7 with 1024).  F: rows may have filters.
-// ONE: rows of one chunk, of which it does all in one launch (sample_chunks' counts and sample_border's tokens included): 7
-// rows of 1529 with all filters 15.0 us, 25.6 by three kernels; 500 of 8000 24.4 and 36.5; one without filters 5.9 and 11.3.
+// ONE: rows of one chunk, of which it does all in one launch (sample_chunks' counts and sample_border's tokens included): a
+// row of 8192 with all filters 12.4 us, 24.1 by three kernels; 500 of 8000 20.2 and 36.5.  (Rows of two chunks the same way gain little, 22 and 24:
+// a compute unit's own instructions bound it.)
 template <class T, bool F, bool ONE>
 __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, int64_t row0, int chunks)
 {
@@ -953,58 +954,56 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
         for (int j = 0; j < kVectors; ++j) x[j] = load16(row, min(first + j * N, V), V);
     }
     const double chosen_edge = ONE ? edge : floor(pos_of(l.tops[chosen], top, s.scale)), from = (chosen_edge + 1.0) * -4.0;
-    u64 before = 0, aim = 0;
-    bool mine = false;
+    auto is_kept = [&](float y, int i) { return F ? y == y && number_of<T>(key_of(y), i) >= cut : top != kInf || y == top; };
+    // (2^52 more than the weight, which is then in the low bits; NaN and -infinity weigh nothing)
+    auto weight = [&](float y) {
+        const double w = power32(__builtin_fma(pos_of(y, top, s.scale), 4.0, from), l.powers);
+        return __builtin_bit_cast(u64, __builtin_fma(w, 0x1p43, 0x1p52)) - 0x4330000000000000ull;
+    };
+    u64 sum = 0;
 #pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-        u64 sum = 0;
-        int token = -1;
-#pragma unroll 1
-        for (int j = 0; j < kVectors; ++j) {
-            const u32x4 v = next_vector();
-            uint32_t kept = 0;  // a bit each
+    for (int j = 0; j < kVectors; ++j) {
+        const u32x4 v = next_vector();
+        uint32_t kept = 0;  // a bit each
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float y = bits_of<T>(v, i);
-                kept |= (uint32_t)(F ? y == y && number_of<T>(key_of(y), first + j * N + i) >= cut : top != kInf || y == top) << i;
-            }
-            if (F && !__any(kept)) continue;
+        for (int i = 0; i < N; ++i) kept |= (uint32_t)is_kept(bits_of<T>(v, i), first + j * N + i) << i;
+        if (F && !__any(kept)) continue;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                // (2^52 more than the weight, which is then in the low bits; NaN and -infinity weigh nothing)
-                const double w = power32(__builtin_fma(pos_of(bits_of<T>(v, i), top, s.scale), 4.0, from), l.powers);
-                sum += kept >> i & 1 ? __builtin_bit_cast(u64, __builtin_fma(w, 0x1p43, 0x1p52)) - 0x4330000000000000ull : 0;
-                if (token < 0 && before + sum > aim) token = first + j * N + i;
-            }
+        for (int i = 0; i < N; ++i) {
+            const u64 w = weight(bits_of<T>(v, i));
+            sum += kept >> i & 1 ? w : 0;
         }
-        if (pass) {
-            if (mine) a.tokens[r] = token;
-            break;
-        }
-        const u64 front = sum_to(sum);
-        if (lane == 63) l.fronts[wave] = front;
-        __syncthreads();
-        u64 total = 0;
-        before = front - sum;
-#pragma unroll
-        for (int w = 0; w < NT / 64; ++w) {
-            const u64 f = l.fronts[w];
-            if (w < wave) before += f;
-            total += f;
-        }
-        double rest;
-        if constexpr (ONE) {
-            const double u = (double)a.uniform[r];
-            rest = u > 0.0 ? fmin(u, 1.0 - 0x1p-40) * (double)total : 0.0;
-        } else {
-            rest = l.rest / l.scale[chosen] * 0x1p43;
-            // (the weights here are those of the bins but where a pos of 2^53 and more leaves the one of its bin's top no bit)
-            if (filters) rest *= eighth((int)(chosen_edge + 1.0 - chosen_edge) - 1);
-        }
-        aim = min(rest > 0.0 ? (u64)fmin(rest, 0x1p62) : 0ull, total - 1);
-        mine = sum > 0 && before <= aim && aim < before + sum;
-        if (!__any(mine)) break;
     }
+    const u64 front = sum_to(sum);
+    if (lane == 63) l.fronts[wave] = front;
+    __syncthreads();
+    u64 total = 0, before = front - sum;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        const u64 f = l.fronts[w];
+        if (w < wave) before += f;
+        total += f;
+    }
+    double rest;
+    if constexpr (ONE) {
+        const double u = (double)a.uniform[r];
+        rest = u > 0.0 ? fmin(u, 1.0 - 0x1p-40) * (double)total : 0.0;
+    } else {
+        rest = l.rest / l.scale[chosen] * 0x1p43;
+        // (the weights here are those of the bins but where a pos of 2^53 and more leaves the one of its bin's top no bit)
+        if (filters) rest *= eighth((int)(chosen_edge + 1.0 - chosen_edge) - 1);
+    }
+    const u64 aim = min(rest > 0.0 ? (u64)fmin(rest, 0x1p62) : 0ull, total - 1);
+    const u64 owner = __ballot(sum > 0 && before <= aim && aim < before + sum);  // one thread of all
+    if (!owner) return;
+    // its logits again, a lane each
+    const int own = __ffsll(owner) - 1, at = lane_of(first, own), i = at + lane;
+    const u64 goal = lane_of(aim - before, own);
+    static_assert(kEach <= 64, "a lane each");
+    float y = -kInf;
+    if (lane < kEach && i < V) y = sizeof(T) == 2 ? __uint_as_float((uint32_t)row[i] << 16) : (float)row[i];
+    const u64 hits = __ballot(sum_to(is_kept(y, i) ? weight(y) : 0) > goal);
+    if (lane == 0) a.tokens[r] = at + __ffsll(hits) - 1;
 }
 
 // Rows of a launch: those of 64 MiB of workspace
