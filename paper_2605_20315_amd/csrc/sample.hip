@@ -13,9 +13,9 @@
 // filters the count and mass up to each of the 512 bins below the chunk's largest (weights down to 2^-64).  sample_border, several workgroups a row:
 // the row's own sums from those, the bins that the borders are in, and their tokens.  sample_rows, a workgroup a row: the borders among those
 // tokens, the chunk that the draw falls into, the token.  Without filters the first and the last are all; a row of one chunk needs only the last.
-// 64 rows of 151673 with all filters, BF16: 46 us (16, 13 and 15 and what lies between); a large copy would read them in 4.  Counting in 64 bits bounds
+// 64 rows of 151673 with all filters, BF16: 44 to 46 us (16, 13 and 15 and what lies between); a large copy would read them in 4.  Counting in 64 bits bounds
 // the first (22 vector instructions and an addition in LDS a logit), trips to memory and to a barrier one after another the others, as they do
-// all of one row's 22 us.  500 rows of 100003 in FP32 by temperature alone: 56 to 70 us, 41 by a large copy; reading takes as long as the 20
+// all of one row's 22 us.  500 rows of 100003 in FP32 by temperature alone: 53 to 69 us, 41 by a large copy; reading takes as long as the 20
 // instructions of each weight's power of two, and the two overlap in part.
 #include "kv8.h"
 
