@@ -565,7 +565,7 @@ def kv8_tree_attention(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.T
 
 
 def mq_sample_workspace_bytes(rows: int, V: int) -> int:
-    """Workspace size that mq_sample needs."""
+    """Workspace size that mq_sample needs; 0 for rows of at most 8192 logits."""
     return int(_lib.load().mq_sample_workspace_bytes(rows, V))
 
 
