@@ -1,9 +1,11 @@
-"""mq_sample with a workspace of just the size asked for: refusals, and both call paths."""
+"""mq_sample with a workspace of just the size asked for: refusals, both call paths, and more rows than it holds at a time."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2605_20315_amd as mq
 from test_gpu_draft_binding import check as same_by_both_paths
+from test_gpu_sample import check, logits_of, settings
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +39,34 @@ def test_both_call_paths_with_a_workspace_and_without(monkeypatch):
             same_by_both_paths(monkeypatch, lambda: mq.mq_sample(x, u, **more, workspace=ws))
             same_by_both_paths(monkeypatch, lambda: mq.mq_sample(x[:, 1:20002], u, **more, workspace=ws))
         assert (behind == 0xFF).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_more_rows_than_one_launch_holds(dtype):
+    """Rows of two parts, 64 MiB hold 1421 of them with filters: a second launch of 79."""
+    r = np.random.default_rng(11)
+    rows, V = 1500, 8193
+    ws, behind = workspace(rows, V)
+    assert len(ws) == mq.mq_sample_workspace_bytes(rows - 1, V) < rows * mq.mq_sample_workspace_bytes(1, V)
+    x, u = logits_of(r, rows, V, dtype), r.random(rows).astype(np.float32)
+    x[1421], x[1430, ::2], x[1440, 17] = float("-inf"), float("nan"), float("inf")
+    check(x, u, settings(r, rows), ws)
+    assert (behind == 0xFF).all()
+
+
+def test_more_long_rows_than_one_launch_holds():
+    """130 rows near the longest, 118 to a launch: the same tokens as from calls of one launch each."""
+    g = torch.Generator("cuda").manual_seed(5)
+    rows, V = 130, (1 << 20) - 3
+    x = (2.5 * torch.randn(rows, V, device="cuda", generator=g)).to(torch.bfloat16)
+    u = torch.rand(rows, device="cuda", generator=g)
+    have = {"temperature": 0.5 + torch.rand(rows, device="cuda", generator=g), "top_k": torch.randint(0, 3000, (rows,), device="cuda", generator=g).int(),
+            "top_p": 0.6 + 0.39 * torch.rand(rows, device="cuda", generator=g), "min_p": 0.01 * torch.rand(rows, device="cuda", generator=g)}
+    ws, behind = workspace(rows, V)
+    assert len(ws) < rows * mq.mq_sample_workspace_bytes(1, V)
+    got = mq.mq_sample(x, u, **have, workspace=ws)
+    assert (behind == 0xFF).all()
+    for a, b in ((0, 65), (65, 130), (117, 119)):
+        assert torch.equal(got[a:b], mq.mq_sample(x[a:b], u[a:b], **{k: v[a:b] for k, v in have.items()}))
+    at = [0, 64, 117, 118, 129]
+    check(x[at], u[at].cpu().numpy(), {k: v[at].cpu().numpy() for k, v in have.items()})
