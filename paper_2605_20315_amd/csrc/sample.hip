@@ -783,7 +783,31 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
         int count = 0, n = 0;          // tokens between lo and hi, and above hi
         u64 lo = 0, hi = 0, mass = 0;  // and the mass above hi
         bool whole = false;            // whether all of the last bin is kept
+        bool by_mass = false;          // whether a border is where a mass is reached, or a number of tokens
         double limit = 0.0;
+        // How many tokens have the largest logit (of the tokens of the first bin, if those are listed)
+        auto count_largest = [&] {
+            const u64 least = number_of<T>(key_of(top), 0xfffff);
+            int c = 0;
+            if (listed <= kList) {
+#pragma unroll 1
+                for (int i = tid; i < listed; i += NT) c += l.list[i] >= least;
+            } else {
+#pragma unroll 1
+                for (int i0 = tid * N; i0 < V; i0 += NT * N) {
+                    const u32x4 x = load16(row, i0, V);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) c += bits_of<T>(x, i) == top;
+                }
+            }
+            c = sum_to(c);
+            if (lane == 63) l.wave_counts[wave] = c;
+            __syncthreads();
+            c = 0;
+#pragma unroll
+            for (int w = 0; w < NT / 64; ++w) c += l.wave_counts[w];
+            return c;
+        };
         auto look_at = [&](int b) {
             n = 0, mass = 0, count = count_in(b);
             lo = number_from(first_of(b)), hi = b > 0 ? number_from(first_of(b - 1)) - 1 : number_of<T>(~0u, 0);
@@ -811,6 +835,14 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
                         task = kMass;
                         look_at(bin_p);
                         limit = (limit_p - mass_to(bin_p)) * (0x1p40 * eighth(-bin_p));
+                        by_mass = true;
+                        // Sums of weights of different logits are never equal (an exponential of no such difference is a fraction), but where
+                        // all that count have the same logit the border may fall exactly between two of them, which rounded masses do not
+                        // tell: a number of tokens does, top_p times theirs (24 bits by 20, exact).
+                        if (bin_p == 0 && count > 1 && all <= l.masses[0] * (1.0 + 0x1p-33)) {
+                            const int same = count_largest();
+                            if (same == count || (s.k > 0 && same >= s.k)) by_mass = false, limit = ceil((double)s.p * (s.k > 0 ? min(s.k, same) : same));
+                        }
                     }
                 }
             }
@@ -871,7 +903,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
                     for (int i = 0; i < 4; ++i) dn[i] = l.digit_counts[255 - 4 * lane - i], dm[i] = l.digit_masses[255 - 4 * lane - i], sn += dn[i], sm += dm[i];
                     int fn = sum_to(sn);
                     u64 fm = sum_to(sm);
-                    auto reaches = [&](int number, u64 sum) { return (task == kMass ? (double)sum : (double)number) >= limit; };
+                    auto reaches = [&](int number, u64 sum) { return (by_mass ? (double)sum : (double)number) >= limit; };
                     const u64 hits = __ballot(reaches(n + fn, mass + fm));
                     if (lane == (hits ? __ffsll(hits) - 1 : 63)) {  // (rounding may leave the limit behind all of them)
                         fn = n + fn - sn, fm = mass + fm - sm;
@@ -913,7 +945,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
 #pragma unroll
                 for (int d = 1; d < kLanes; d <<= 1) fn += __shfl_xor(fn, d), fm += (u64)__shfl_xor((long long)fm, d);
                 fn += n, fm += mass;
-                const bool reached = task == kCount ? (double)(fn + 1) == limit : (double)fm < limit && (double)(fm + x.weight) >= limit;
+                const bool reached = by_mass ? (double)fm < limit && (double)(fm + x.weight) >= limit : (double)(fn + 1) == limit;
                 if (reached && tid / kLanes < count && tid % kLanes == 0) l.cut = x.number, l.found_mass = fm + x.weight;
             }
             __syncthreads();
