@@ -153,6 +153,17 @@ static __device__ __forceinline__ double eighth(int b)
     return __builtin_ldexp((b & 1 ? e1 : 1.0) * (b & 2 ? e2 : 1.0) * (b & 4 ? e4 : 1.0), -(b >> 3));
 }
 
+// u times a total of less than 2^63, rounded down: exact, so that a sum that is u times the total is not below it.  For u <= 0
+// and NaN 0, for u >= 1 what 1 - 2^-40 gives.
+static __device__ __forceinline__ u64 share_of(float u, u64 total)
+{
+    if (!(u > 0.0f)) return 0;
+    if (!(u < 1.0f)) return total - ((total + ((1ull << 40) - 1)) >> 40);
+    const uint32_t bits = __float_as_uint(u), exponent = bits >> 23, by = 150 - max(exponent, 1u);  // u is m / 2^by
+    const u64 m = (bits & 0x7fffffu) | (exponent > 0 ? 0x800000u : 0u), lo = m * total, hi = __umul64hi(m, total);
+    return by < 64 ? lo >> by | hi << (64 - by) : by < 128 ? hi >> (by - 64) : 0;
+}
+
 // Logits as unsigned numbers of the same order, the two zeros as one
 static __device__ __forceinline__ uint32_t key_of(float x)
 {
@@ -1016,16 +1027,15 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
         if (w < wave) before += f;
         total += f;
     }
-    double rest;
+    u64 aim;
     if constexpr (ONE) {
-        const double u = (double)a.uniform[r];
-        rest = u > 0.0 ? fmin(u, 1.0 - 0x1p-40) * (double)total : 0.0;
+        aim = share_of(a.uniform[r], total);
     } else {
-        rest = l.rest / l.scale[chosen] * 0x1p43;
+        double rest = l.rest / l.scale[chosen] * 0x1p43;
         // (the weights here are those of the bins but where a pos of 2^53 and more leaves the one of its bin's top no bit)
         if (filters) rest *= eighth((int)(chosen_edge + 1.0 - chosen_edge) - 1);
+        aim = min(rest > 0.0 ? (u64)fmin(rest, 0x1p62) : 0ull, total - 1);
     }
-    const u64 aim = min(rest > 0.0 ? (u64)fmin(rest, 0x1p62) : 0ull, total - 1);
     const u64 owner = __ballot(sum > 0 && before <= aim && aim < before + sum);  // one thread of all
     if (!owner) return;
     // its logits again, a lane each

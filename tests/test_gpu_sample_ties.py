@@ -18,7 +18,7 @@ EIGHTHS = np.arange(256) / 8  # exact in BF16
 
 
 def dev(x, dtype=torch.float32):
-    return torch.from_numpy(np.ascontiguousarray(x, np.float32)).to(dtype).cuda()
+    return torch.from_numpy(np.array(x, np.float32)).to(dtype).cuda()
 
 
 def sampled(x, u, dtype, **have):
@@ -90,3 +90,15 @@ def test_top_p_of_nearly_equal_logits(dtype):
         x[:, 3 : 3 + V // 4] = -3.0
         for have in ({}, {"top_k": np.full(32, 3, np.int32)}, {"top_k": r.integers(2, V, 32).astype(np.int32)}):
             check(dev(x, dtype), r.random(32).astype(np.float32), {"top_p": r.uniform(0.1, 0.9, 32).astype(np.float32), **have})
+
+
+# ------------------------------------------------------------------------------------------------ the draw
+
+@TYPES
+@pytest.mark.parametrize("V,parts", [(8190, 2), (6144, 2048), (8192, 8192), (7168, 1024)])
+def test_draws_between_equal_logits_of_a_short_row(V, parts, dtype):
+    """The lowest index with more than u of the mass up to it: with u = i / parts the token number u * V."""
+    i = np.arange(256) * parts // 256
+    for temperature in (1.0, 0.7):
+        got = sampled(np.repeat(EIGHTHS[:, None], V, 1), i / parts, dtype, temperature=temperature)
+        assert (got == i * V // parts).all(), np.flatnonzero(got != i * V // parts)[:8]
