@@ -624,7 +624,8 @@ struct RowLds {
     u64 fronts[kRowThreads / 64];
     double powers[32];
     int chosen;
-    double rest;
+    double rest, total;
+    bool near;
     u64 bins[F && ONE ? kBins : 1];
     float wave_tops[kRowThreads / 64];
     int wave_counts[kRowThreads / 64];
@@ -973,79 +974,132 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
         __syncthreads();
     }
 
-    // the chunk that the draw falls into: sums over two chunks a lane
+    // The chunk that the draw falls into: sums over two chunks a lane
+    static_assert(kChunksMost == 128, "two a lane");
+    const float u = a.uniform[r];
     if (!ONE && wave == 0) {
-        static_assert(kChunksMost == 128, "two a lane");
         const double m0 = 2 * lane < chunks ? l.kept[2 * lane] : 0.0, m1 = 2 * lane + 1 < chunks ? l.kept[2 * lane + 1] : 0.0, sum = m0 + m1;
-        const double front = sum_to(sum), total = lane_of(front, 63), u = (double)a.uniform[r];
-        const double aim = u > 0.0 ? fmin(u, 1.0 - 0x1p-40) * total : 0.0;
+        const double front = sum_to(sum), total = lane_of(front, 63);
+        const double aim = u > 0.0f ? fmin((double)u, 1.0 - 0x1p-40) * total : 0.0;
         const u64 hits = __ballot(front > aim && sum > 0.0), some = __ballot(sum > 0.0);
         if (lane == (hits ? __ffsll(hits) - 1 : 63 - __clzll((long long)some))) {  // (rounding may leave the draw behind the last)
             const double before = front - sum;
             const bool second = !(m0 > 0.0) || (m1 > 0.0 && before + m0 <= aim);
             l.chosen = 2 * lane + second;
             l.rest = aim - (second ? before + m0 : before);
+            l.total = total;
+            l.near = false;
         }
     }
     if (!ONE) __syncthreads();
 
-    // The token in it, sixteen side by side to a thread: weights in whole 2^-43 of the top of the chunk's first bin, so that all sums
-    // agree (what is kept of a chunk has its largest logit in it).
-    const int chosen = ONE ? 0 : l.chosen, first = chosen * kChunk + tid * kEach;
-    if constexpr (!ONE) {
-#pragma unroll
-        for (int j = 0; j < kVectors; ++j) x[j] = load16(row, min(first + j * N, V), V);
-    }
-    const double chosen_edge = ONE ? edge : floor(pos_of(l.tops[chosen], top, s.scale)), from = (chosen_edge + 1.0) * -4.0;
+    // The token in it, sixteen side by side to a thread: weights in whole 2^-50 of the top of the chunk's first bin, so that all sums
+    // agree (what is kept of a chunk has its largest logit in it).  The chunks' masses are made of other roundings, so a draw that comes
+    // near either end of its token, as one does that falls exactly between equal logits, is made again with one weight for
+    // a token everywhere: kAdding takes the sums of the chunks that have tokens with weight, in 2^-43 of the top of the row's first bin, one chunk
+    // after the other, kAgain the token.  Near: by what the roundings may add up to, 2^-51 for each of 8192 tokens here and as much once more where
+    // their sums become binary64; with filters 2^-36 for each chunk (half a unit of an octave's end) and 2^-34 of the row's mass (the bins'
+    // shortfalls), without 2^-43 of it (sums of the same weights in binary64).
+    enum { kFirst, kAdding, kAgain };
+    int state = ONE ? kAgain : kFirst, chosen = ONE ? 0 : l.chosen;
+    u64 goal = 0;  // what of the draw is left in the chosen chunk, of kAgain
     auto is_kept = [&](float y, int i) { return F ? y == y && number_of<T>(key_of(y), i) >= cut : top != kInf || y == top; };
-    // (2^52 more than the weight, which is then in the low bits; NaN and -infinity weigh nothing)
-    auto weight = [&](float y) {
-        const double w = power32(__builtin_fma(pos_of(y, top, s.scale), 4.0, from), l.powers);
-        return __builtin_bit_cast(u64, __builtin_fma(w, 0x1p43, 0x1p52)) - 0x4330000000000000ull;
+    // the first chunk from c on that has tokens with weight
+    auto chunk_from = [&](int c) {
+        while (c < chunks && (l.shift[c] == kBins || !is_kept(l.tops[c], c * kChunk))) ++c;
+        return c;
     };
-    u64 sum = 0;
 #pragma unroll 1
-    for (int j = 0; j < kVectors; ++j) {
-        const u32x4 v = next_vector();
-        uint32_t kept = 0;  // a bit each
+    for (;;) {
+        const int first = chosen * kChunk + tid * kEach;
+        if constexpr (!ONE) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) kept |= (uint32_t)is_kept(bits_of<T>(v, i), first + j * N + i) << i;
-        if (F && !__any(kept)) continue;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const u64 w = weight(bits_of<T>(v, i));
-            sum += kept >> i & 1 ? w : 0;
+            for (int j = 0; j < kVectors; ++j) x[j] = load16(row, min(first + j * N, V), V);
         }
-    }
-    const u64 front = sum_to(sum);
-    if (lane == 63) l.fronts[wave] = front;
-    __syncthreads();
-    u64 total = 0, before = front - sum;
+        const double chosen_edge = state == kFirst ? floor(pos_of(l.tops[chosen], top, s.scale)) : edge, from = (chosen_edge + 1.0) * -4.0;
+        const double units = state == kFirst ? 0x1p50 : 0x1p43;
+        // (2^52 more than the weight, which is then in the low bits; NaN and -infinity weigh nothing)
+        auto weight = [&](float y) {
+            const double w = power32(__builtin_fma(pos_of(y, top, s.scale), 4.0, from), l.powers);
+            return __builtin_bit_cast(u64, __builtin_fma(w, units, 0x1p52)) - 0x4330000000000000ull;
+        };
+        u64 sum = 0;
+#pragma unroll 1
+        for (int j = 0; j < kVectors; ++j) {
+            const u32x4 v = next_vector();
+            uint32_t kept = 0;  // a bit each
 #pragma unroll
-    for (int w = 0; w < NT / 64; ++w) {
-        const u64 f = l.fronts[w];
-        if (w < wave) before += f;
-        total += f;
+            for (int i = 0; i < N; ++i) kept |= (uint32_t)is_kept(bits_of<T>(v, i), first + j * N + i) << i;
+            if (F && !__any(kept)) continue;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const u64 w = weight(bits_of<T>(v, i));
+                sum += kept >> i & 1 ? w : 0;
+            }
+        }
+        const u64 front = sum_to(sum);
+        if (lane == 63) l.fronts[wave] = front;
+        __syncthreads();
+        u64 total = 0, before = front - sum;
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) {
+            const u64 f = l.fronts[w];
+            if (w < wave) before += f;
+            total += f;
+        }
+        if (!ONE && state == kAdding) {
+            if (tid == 0) l.part[chosen] = total;
+            chosen = chunk_from(chosen + 1);
+            __syncthreads();
+            if (chosen < chunks) continue;
+            const u64 m0 = l.part[2 * lane], m1 = l.part[2 * lane + 1], end = sum_to(m0 + m1), aim = share_of(u, lane_of(end, 63));
+            const int at = __ffsll(__ballot(end > aim)) - 1;
+            const u64 start = lane_of(end - m0 - m1, at), middle = start + lane_of(m0, at);
+            const bool second = middle <= aim;
+            chosen = 2 * at + second, goal = aim - (second ? middle : start);
+            state = kAgain;
+            continue;
+        }
+        double rest = 0.0;
+        u64 aim = goal;
+        if constexpr (ONE) {
+            aim = share_of(u, total);
+        } else if (state == kFirst) {
+            rest = l.rest / l.scale[chosen] * units;
+            // (the weights here are those of the bins but where a pos of 2^53 and more leaves the one of its bin's top no bit)
+            if (filters) rest *= eighth((int)(chosen_edge + 1.0 - chosen_edge) - 1);
+            aim = min(rest > 0.0 ? (u64)fmin(rest, 0x1p63) : 0ull, total - 1);
+        }
+        const u64 owner = __ballot(sum > 0 && before <= aim && aim < before + sum);  // one thread of all
+        if (owner) {
+            // its logits again, a lane each
+            const int own = __ffsll(owner) - 1, at = lane_of(first, own), i = at + lane;
+            const u64 start = lane_of(before, own);
+            static_assert(kEach <= 64, "a lane each");
+            float y = -kInf;
+            if (lane < kEach && i < V) y = sizeof(T) == 2 ? __uint_as_float((uint32_t)row[i] << 16) : (float)row[i];
+            const u64 w = is_kept(y, i) ? weight(y) : 0, end = start + sum_to(w);
+            const int token = __ffsll(__ballot(end > aim)) - 1;
+            bool near = false;
+            if (!ONE && state == kFirst && u > 0.0f) {
+                // (nothing lies in front of a draw of 0)
+                const double high = (double)lane_of(end, token), low = high - (double)lane_of(w, token);
+                near = fmin(rest - low, high - rest) * l.scale[chosen] * 0x1p-7 < 0x1p6 + (filters ? chunks * 0x1p7 + l.total * 0x1p9 : l.total);
+            }
+            if (lane == 0) {
+                if (near)
+                    l.near = true;
+                else
+                    a.tokens[r] = at + token;
+            }
+        }
+        if (ONE || state == kAgain) return;
+        __syncthreads();
+        if (!l.near) return;
+        if (tid < kChunksMost) l.part[tid] = 0;
+        __syncthreads();
+        state = kAdding, chosen = chunk_from(0);
     }
-    u64 aim;
-    if constexpr (ONE) {
-        aim = share_of(a.uniform[r], total);
-    } else {
-        double rest = l.rest / l.scale[chosen] * 0x1p43;
-        // (the weights here are those of the bins but where a pos of 2^53 and more leaves the one of its bin's top no bit)
-        if (filters) rest *= eighth((int)(chosen_edge + 1.0 - chosen_edge) - 1);
-        aim = min(rest > 0.0 ? (u64)fmin(rest, 0x1p62) : 0ull, total - 1);
-    }
-    const u64 owner = __ballot(sum > 0 && before <= aim && aim < before + sum);  // one thread of all
-    if (!owner) return;
-    // its logits again, a lane each
-    const int own = __ffsll(owner) - 1, at = lane_of(first, own), i = at + lane;
-    const u64 goal = lane_of(aim - before, own);
-    static_assert(kEach <= 64, "a lane each");
-    float y = -kInf;
-    if (lane < kEach && i < V) y = sizeof(T) == 2 ? __uint_as_float((uint32_t)row[i] << 16) : (float)row[i];
-    const u64 hits = __ballot(sum_to(is_kept(y, i) ? weight(y) : 0) > goal);
-    if (lane == 0) a.tokens[r] = at + __ffsll(hits) - 1;
 }
 
 // Rows of a launch: those of 64 MiB of workspace

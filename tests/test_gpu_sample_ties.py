@@ -102,3 +102,56 @@ def test_draws_between_equal_logits_of_a_short_row(V, parts, dtype):
     for temperature in (1.0, 0.7):
         got = sampled(np.repeat(EIGHTHS[:, None], V, 1), i / parts, dtype, temperature=temperature)
         assert (got == i * V // parts).all(), np.flatnonzero(got != i * V // parts)[:8]
+
+
+@TYPES
+@pytest.mark.parametrize("V,parts", [(16384, 16384), (12288, 4096), (1 << 17, 1 << 17), (8194, 2), (100352, 2048)])
+def test_draws_between_equal_logits_of_a_long_row(V, parts, dtype):
+    r = np.random.default_rng(V)
+    rows = 64
+    for have in ({}, {"temperature": 0.7}, {"top_k": V}, {"top_k": V // 2}, {"temperature": 0.7, "min_p": 0.5}, {"top_p": 0.5}):
+        i = r.integers(0, parts, rows)
+        i[:3] = 0, 1, parts - 1
+        kept = V // 2 if have.get("top_k") == V // 2 or "top_p" in have else V
+        got = sampled(np.repeat(r.choice(EIGHTHS, (rows, 1)), V, 1), i / parts, dtype, **have)
+        assert (got == i * kept // parts).all(), (have, got[got != i * kept // parts][:4])
+
+
+@TYPES
+@pytest.mark.parametrize("V", [100, 8192, 16384, 24576, 32768, 50000])
+def test_half_of_a_mirrored_row(V, dtype):
+    """A row and its mirror image behind it: the draw of a half falls between them, whatever the logits."""
+    r = np.random.default_rng(V)
+    half = r.normal(size=(32, V // 2)) * 2.5
+    half[8:16, : V // 3] -= 12.0   # the parts of the row lie far apart
+    half[16:24, V // 3 :] -= 25.0
+    half[:, -1] = 3.0
+    x = dev(np.concatenate([half, half[:, ::-1]], 1), dtype)
+    values = x.float().cpu().numpy()
+    u = np.full(32, 0.5, np.float32)
+    assert (mq.mq_sample(x, dev(u)).cpu().numpy() == V // 2).all()
+    assert (mq.mq_sample(x, dev(u), dev(np.full(32, 1.7))).cpu().numpy() == V // 2).all()
+    got = mq.mq_sample(x, dev(u), min_p=dev(np.full(32, 0.01))).cpu().numpy()
+    top = values.max(1, keepdims=True).astype(np.float64)
+    kept = np.exp(values - top) >= np.float32(0.01)
+    assert (got == [V // 2 + int(np.argmax(row[V // 2 :])) for row in kept]).all()
+
+
+@TYPES
+def test_draws_of_zero_take_the_first_token_that_is_kept(dtype):
+    r = np.random.default_rng(4)
+    for V in (500, 20000, 60000):
+        x = r.normal(size=(16, V)) * 3
+        u = np.zeros(16, np.float32)
+        for have in ({}, {"top_k": np.full(16, 5, np.int32)}, {"min_p": np.full(16, 0.2, np.float32)}, {"top_p": np.full(16, 0.8, np.float32)}):
+            check(dev(x, dtype), u, have)
+
+
+@TYPES
+def test_the_first_of_the_kept_tokens_weighs_next_to_nothing(dtype):
+    """2^-40 of the largest, in a part of the row by itself: a draw of zero takes it, as its weight is above the 2^-43 that may count as none."""
+    x = np.full((4, 30000), -np.inf)
+    x[:, 100], x[:, 25000] = 0.0, 28.0  # e^-28 = 2^-40.4
+    for have in ({}, {"top_k": np.full(4, 5, np.int32)}, {"min_p": np.full(4, 1e-13, np.float32)}):
+        assert check(dev(x, dtype), np.zeros(4, np.float32), have).tolist() == [100] * 4
+        assert check(dev(x, dtype), np.full(4, 2.0 ** -20, np.float32), have).tolist() == [25000] * 4
