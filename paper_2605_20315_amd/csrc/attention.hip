@@ -1000,8 +1000,8 @@ __global__ __launch_bounds__(kFewThreads, D <= 128 ? 3 : 2) void attend_tree(Kv8
     }
     f32x4 acc[RT][D / 16];
     // the running maximum times the scale, and the sum of the probabilities as the product takes them: that of ones in the values' place
-    // (kLow: none yet; any score is 2^8 above it)
-    constexpr float kLow = -0x1p120f;
+    // (kLow: none yet.  It is the lowest number: any other score is 2^8 above it, and one that is it has a probability of one)
+    constexpr float kLow = -0x1.fffffep127f;
     float mb[RT];
     f32x4 sum[RT];
     const bf16x8 ones = four(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
@@ -1242,7 +1242,7 @@ __global__ __launch_bounds__(kFewThreads, D <= 128 ? 3 : 2) void attend_tree(Kv8
     // The four waves' results, two and two: lane (col, g) holds, of row col, the elements (4g + i) * D / 16 + d for i < 4, d < D / 16
 #pragma unroll
     for (int f = 0; f < RT; ++f) {
-        mb[f] = mb[f] == kLow ? kNone : mb[f];
+        mb[f] = mb[f] == kLow && !(sum[f][0] > 0.0f) ? kNone : mb[f];
         if (g == 0) stat[wave][0][16 * f + col] = mb[f], stat[wave][1][16 * f + col] = sum[f][0];
     }
     __syncthreads();
