@@ -78,6 +78,9 @@ constexpr int64_t kChunkBytes = sizeof(Chunk) + kBins * sizeof(Upto);
 
 struct Setting {
     double scale, inverse;  // pos over logit, and logit over pos
+    // The share of the mass in front of which tokens are kept: top_p, taken down by what the bins' masses and the border's may be apart, so that a
+    // token that has it in front of it in binary64 (temperatures beyond the logits' differences make weights of one) is not kept
+    double share;
     int k;
     float p, min_p;
     bool largest, filters;
@@ -90,6 +93,7 @@ static __device__ __forceinline__ Setting setting_of(const Sample &a, int64_t r)
     s.k = a.top_k ? a.top_k[r] : 0;
     s.p = a.top_p ? a.top_p[r] : 1.0f;
     s.min_p = a.min_p ? a.min_p[r] : 0.0f;
+    s.share = (double)s.p * (1.0 - 0x1p-33);
     s.largest = !(t > 0.0f) || s.k == 1 || !(s.p > 0.0f) || s.min_p != s.min_p || s.min_p > 1.0f;
     if (s.k <= 0 || s.k >= a.V) s.k = 0;
     s.filters = s.k > 0 || s.p < 1.0f || s.min_p > 0.0f;
@@ -490,8 +494,8 @@ static __device__ __forceinline__ Borders borders_of(const Setting &s, double pe
         if (b.part_k) least = b.k > 0 ? masses[b.k - 1] : 0.0;
     }
     if (s.p < 1.0f) {
-        b.p0 = min(bins_below(masses, (double)s.p * least, lane), b.k);
-        b.p1 = min(bins_below(masses, (double)s.p * most, lane), b.k);
+        b.p0 = min(bins_below(masses, s.share * least, lane), b.k);
+        b.p1 = min(bins_below(masses, s.share * most, lane), b.k);
     }
     return b;
 }
@@ -797,9 +801,11 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
         bool whole = false;            // whether all of the last bin is kept
         bool by_mass = false;          // whether a border is where a mass is reached, or a number of tokens
         double limit = 0.0;
-        // How many tokens have the largest logit (of the tokens of the first bin, if those are listed)
+        // How many tokens weigh as much as the largest logit (of the tokens of the first bin, if those are listed)
         auto count_largest = [&] {
-            const u64 least = number_of<T>(key_of(top), 0xfffff);
+            const uint32_t key = lowest(s, top, peak);
+            const u64 least = number_from(key);
+            const float least_logit = value_of(key);
             int c = 0;
             if (listed <= kList) {
 #pragma unroll 1
@@ -809,7 +815,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
                 for (int i0 = tid * N; i0 < V; i0 += NT * N) {
                     const u32x4 x = load16(row, i0, V);
 #pragma unroll
-                    for (int i = 0; i < N; ++i) c += bits_of<T>(x, i) == top;
+                    for (int i = 0; i < N; ++i) c += bits_of<T>(x, i) >= least_logit;
                 }
             }
             c = sum_to(c);
@@ -841,15 +847,15 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, i
             if (task == kNew + kMass) {
                 task = kNew + kRest;
                 if (s.p < 1.0f) {
-                    limit_p = (double)s.p * all;
+                    limit_p = s.share * all;
                     bin_p = min(bins_below(l.masses, limit_p, lane), bin_k);
                     if (bin_p < kBins && bin_p <= bin_m) {
                         task = kMass;
                         look_at(bin_p);
                         limit = (limit_p - mass_to(bin_p)) * (0x1p40 * eighth(-bin_p));
                         by_mass = true;
-                        // Sums of weights of different logits are never equal (an exponential of no such difference is a fraction), but where
-                        // all that count have the same logit the border may fall exactly between two of them, which rounded masses do not
+                        // Sums of different weights are never equal (the exponential of a difference of logits is no fraction), but where
+                        // all that count weigh the same the border may fall exactly between two of them, which rounded masses do not
                         // tell: a number of tokens does, top_p times theirs (24 bits by 20, exact).
                         if (bin_p == 0 && count > 1 && all <= l.masses[0] * (1.0 + 0x1p-33)) {
                             const int same = count_largest();

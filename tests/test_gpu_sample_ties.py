@@ -155,3 +155,33 @@ def test_the_first_of_the_kept_tokens_weighs_next_to_nothing(dtype):
     for have in ({}, {"top_k": np.full(4, 5, np.int32)}, {"min_p": np.full(4, 1e-13, np.float32)}):
         assert check(dev(x, dtype), np.zeros(4, np.float32), have).tolist() == [100] * 4
         assert check(dev(x, dtype), np.full(4, 2.0 ** -20, np.float32), have).tolist() == [25000] * 4
+
+
+# ------------------------------------------------------------------------------------------------ weights of one from different logits
+
+@TYPES
+@pytest.mark.parametrize("V", [8, 512, 8192, 16384])
+def test_an_endless_temperature_makes_all_weights_one(V, dtype):
+    """Kept are the first of the order, top_p of all of them; the draw counts tokens."""
+    r = np.random.default_rng(V)
+    x = dev(r.normal(size=(24, V)) * 3, dtype)
+    order = np.argsort(-x.double().cpu().numpy(), axis=1, kind="stable")
+    for t in (np.inf, 3e38):
+        for p in (0.25, 0.5, 0.75, 1.0):
+            u = r.integers(0, 8, 24) / 8
+            got = mq.mq_sample(x, dev(u), temperature=dev(np.full(24, t)), top_p=dev(np.full(24, p))).cpu().numpy()
+            kept = np.sort(order[:, : int(p * V)], 1)
+            assert (got == kept[np.arange(24), (u * kept.shape[1]).astype(int)]).all(), (t, p)
+
+
+@TYPES
+def test_logits_that_are_nearly_the_same(dtype):
+    """Differences of 2^-90 make weights that are one in binary64."""
+    r = np.random.default_rng(6)
+    for V in (8, 40, 8192, 16384):
+        x = dev(2.0 ** -90 * r.normal(size=(24, V)), dtype)
+        order = np.argsort(-x.double().cpu().numpy(), axis=1, kind="stable")
+        for p in (0.25, 0.5, 0.75):
+            u = np.full(24, 1 - 2 ** -24)
+            got = mq.mq_sample(x, dev(u), top_p=dev(np.full(24, p))).cpu().numpy()
+            assert (got == np.sort(order[:, : int(p * V)], 1)[:, -1]).all(), (V, p)
