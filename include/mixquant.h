@@ -352,7 +352,8 @@ int kv8_attention(const void *q_bf16, int64_t ldq, const uint8_t *k_codes, const
  * as one just below, one below 0 or NaN as 0.  A temperature that is not above 0 gives the first of the order, as a top_p or min_p of NaN does.  NaN
  * and -infinity are never chosen (-1 where a row has nothing else), +infinity has all the mass.  temperature, top_p, min_p: float
  * [rows], top_k: int32 [rows], each or NULL (1, none); uniform: float [rows].  Weights and sums in 64 bits, weights to 2^-34 of
- * their value; those below 2^-43 of the largest may count as none.  rows, V <= 2^20.  Bit-identical from run to run.
+ * their value (where |logit| is below 2^18 times the temperature) and top_p to 2^-32; those below 2^-43 of the largest may count as none.
+ * Tokens of equal logits weigh the same: a border or a draw between two of them falls as defined.  rows, V <= 2^20.  Bit-identical from run to run.
  * workspace: as in nvfp4_matvec, of mq_sample_workspace_bytes(rows, V) bytes (0 for rows of at most 8192 logits).
  *
  * mq_draft_accept: sampled [T]: the token that the model chose behind each new token; tokens [T]: the drafted ones.  From token 0 on the path

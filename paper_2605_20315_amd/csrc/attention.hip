@@ -1468,6 +1468,9 @@ static int plan_attention(const Kv8Attend &a, Launch *out)
 // Few items of two tiles are cut into as many as the GPU holds at a time, others into 512: what comes after a first round then is short.
 // Chunks of 8 tiles at least and histories of three of them, since a join costs 6 us (30 tokens after 300 in one sequence 11.5 us, 17.7 with chunks of two
 // tiles; 5 of 60 to 120 after 100 to 900, heads of 256, 27.7 and 41.3; longer histories the same; with chunks of 12 16 tokens after 8000 21.8 and 20.7).
+// All of this goes by the page table's width, the longest history that the host knows of: with a table for 131072 places the short ones are
+// cut and joined after all (30 tokens after 300 18.9 us, 11.0 with a table as wide as the history; one of 60 after 2000 26.1 and 22.7; 5 of 60 to 120 with
+// heads of 256 41.2 and 27.5; long ones the same).
 static Launch plan_tree(const Kv8TreeAttend &a)
 {
     const int D = a.D;

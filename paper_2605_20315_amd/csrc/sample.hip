@@ -8,6 +8,8 @@
 // floor(pos): the same for every part of a row, whatever the largest logit there, so that parts are counted by themselves and put
 // together by shifting.  Weights in a bin lie between 2^-1/8 and 1 of its top, and a bin's mass is its count less
 // what its weights fall short of one: 64 bits hold both, 2^-34 of a weight fine, and one addition in LDS counts a token.
+// Such masses tell where a border or a draw is to about 2^-30 of them.  Where it falls exactly between two tokens the answer goes by whole
+// numbers: of tokens for top_p (only equal weights have such borders), of one weight a token for the draw.
 //
 // Three kernels.  sample_chunks reads the logits once, a chunk of a row by a workgroup: the largest, the mass, and where the row has
 // filters the count and mass up to each of the 512 bins below the chunk's largest (weights down to 2^-64).  sample_border, several workgroups a row:
@@ -15,7 +17,7 @@
 // tokens, the chunk that the draw falls into, the token.  Without filters the first and the last are all; a row of one chunk needs only the last.
 // 64 rows of 151673 with all filters, BF16: 44 to 46 us (16, 13 and 15 and what lies between); a large copy would read them in 4.  Counting in 64 bits bounds
 // the first (22 vector instructions and an addition in LDS a logit), trips to memory and to a barrier one after another the others, as they do
-// all of one row's 22 us.  500 rows of 100003 in FP32 by temperature alone: 53 to 69 us, 41 by a large copy; reading takes as long as the 20
+// all of one row's 22 us.  500 rows of 100003 in FP32 by temperature alone: 53 to 69 us by card, 41 by a large copy; reading takes as long as the 20
 // instructions of each weight's power of two, and the two overlap in part.
 #include "kv8.h"
 
@@ -57,7 +59,9 @@ struct Borders {
 };
 
 // What is known of a row with filters: the masses and counts up to each bin below its largest logit's, and the tokens, as numbers, of the
-// bins that a border may be in (listed may be more than there is room for)
+// bins that a border may be in (listed may be more than there is room for: then sample_rows reads the row again for each of its passes, by
+// itself.  64 rows of 262144 with logits of deviation 2.2 and top_p of 0.95 62 us at a temperature of 1, 491 at 1.3, where a bin
+// holds more; 64 of 151673 54 us at 1.5, 306 at 2; of equal logits 1810)
 constexpr int kList = 4096;
 struct Row {
     double masses[kBins];
@@ -640,7 +644,7 @@ struct RowLds {
 // once, from memory: so everything that looks at tokens stands here once, in loops.  512 threads, since much of it is done by every wave alike and four
 // waves a SIMD wait for each other there (a pass over a border's tokens 1.2 us, 1.7 with 1024).  F: rows may have filters.
 // ONE: rows of one chunk, of which it does all in one launch (sample_chunks' counts and sample_border's tokens included): a
-// row of 8192 with all filters 12.4 us, 24.1 by three kernels; 500 of 8000 20.2 and 36.5.  (Rows of two chunks the same way gain little, 22 and 24:
+// row of 8192 with all filters 11 to 12.4 us by card, 24.1 by three kernels; 500 of 8000 20.2 to 23.5 and 36.5.  (Rows of two chunks the same way gain little, 22 and 24:
 // a compute unit's own instructions bound it.)
 template <class T, bool F, bool ONE>
 __global__ __launch_bounds__(kRowThreads) void sample_rows(Sample a, Tables t, int64_t row0, int chunks)
